@@ -514,6 +514,85 @@ int psk_calibrate_gather(const float *table, int64_t table_elems, const int32_t 
 int psk_calibrate_gather_lds(const float *table, int32_t table_elems, const uint16_t *idx, int64_t n, float *out,
                              void *stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * Products with weights in 4 bits, and a mixture of experts for a few tokens.
+ *
+ * Differences from the conventions at the top: operands have one of the types below; vectors are rows (X is n x cols, row t at
+ * X + t*ldx; Y is n x rows likewise; leading dimensions count elements and may be larger than the row; no alignment beyond the
+ * element's is asked of X and Y).  Sums are held in 32 bits (the router's in 64) and rounded once to the type of Y.  The order of
+ * every sum is fixed.
+ */
+typedef enum { PSK_F32 = 0, PSK_F16 = 1, PSK_BF16 = 2 } psk_type;
+
+#define PSK_MAX_VECTORS (1 << 20)       /* largest n */
+#define PSK_MOE_MAX_EXPERTS 1024
+#define PSK_MOE_MAX_TOP_K 64
+
+/*
+ * `count` matrices of rows x cols weights, (q - z) * s, with codes q of 4 bits and a scale s (and zero point z) for every `group`
+ * columns of a row.  Element (i, j) of matrix m: q is the low half (j even) or the high half (j odd) of the byte
+ * codes[m*stride_codes + i*ld_codes + j/2]; s = scales[m*stride_scales + i*ld_scales + j/group]; z the byte at the same place of
+ * `zeros` (0 .. 255; 8 where zeros is NULL).
+ *  - group is a power of two, 32 or more (one that is not less than cols gives a scale per row).
+ *  - codes are 16-byte aligned, ld_codes and stride_codes multiples of 16, and the ceil(cols/32)*16 first bytes of a row are
+ *    readable (what they hold from column cols on is of no account).
+ *  - scale_type is PSK_F32 or the type of the activations.
+ */
+typedef struct {
+    int64_t count, rows, cols;
+    int32_t group, scale_type;
+    const uint8_t *codes;
+    const void *scales;
+    const uint8_t *zeros;
+    int64_t ld_codes, ld_scales, stride_codes, stride_scales;
+} psk_q4;
+
+/*
+ * Y = X A^T: Y[t][i] = sum_j A[i][j] X[t][j] for one matrix in 4 bits (count = 1) and n vectors of `type`; n = 1 is the
+ * matrix-vector product.  cols = 0 gives zeros.
+ * Activations in 32 bits keep all their bits (each is multiplied in three parts).  Y has the type of X.
+ */
+size_t psk_gemm_q4_workspace_bytes(int64_t rows, int64_t cols, int64_t n, int type);
+int psk_gemm_q4(const psk_q4 *A, int64_t n, int type, const void *X, int64_t ldx, void *Y, int64_t ldy, void *workspace,
+                size_t workspace_bytes, void *stream);
+
+/*
+ * The gating matrix of a mixture of experts: n x experts with top_k entries stored per row, crd[t*top_k + s] (expert) and
+ * vals[t*top_k + s] (gate), s = 0 .. top_k-1.
+ *   l(t,e) = sum_j X[t][j] W[e][j]                     p = softmax of l(t,:), or 1 / (1 + exp(-l))
+ * The top_k experts with the largest l are taken, or with a bias (float[experts], NULL: none) those with the largest p + bias,
+ * the larger ones first, equal ones by their index; one whose bias is -infinity is never taken.  Where fewer remain, the rest
+ * of the row is crd = -1, vals = 0.  What is no number comes last.  gate = p, divided by the sum of the taken p with normalise,
+ * times factor.  Logits and scores are computed in 64 bits, so the choice does not depend on the order of a sum.
+ * wtype is PSK_F32 or `type`.
+ */
+enum { PSK_SCORE_SOFTMAX = 0, PSK_SCORE_SIGMOID = 1 };
+size_t psk_moe_route_workspace_bytes(int64_t n, int64_t experts);
+int psk_moe_route(int64_t n, int64_t dim, int64_t experts, int32_t top_k, int score, int normalise, float factor, int type,
+                  const void *X, int64_t ldx, int wtype, const void *W, int64_t ldw, const float *bias, int32_t *crd, float *vals,
+                  void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The layer: Y(t,:) = sum_s vals[t,s] * W2_e (act(W1_e X(t,:)) * (W3_e X(t,:))), e = crd[t,s], for n tokens of `type` (PSK_F16 or
+ * PSK_BF16).  An entry outside [0, experts) stands for none; a token without entries gets zeros.  An expert may occur
+ * twice in a row.  W1, W3: inter x dim, W2: dim x inter for each expert.
+ * Made for a few tokens: the matrices of the experts that occur are read once for up to 64 entries of an expert.
+ * psk_moe_experts: weights of `type`, matrix e of W1 and W3 at stride1*e elements, rows ld1 apart (W2: stride2, ld2); bases 16-byte aligned,
+ * strides and leading dimensions multiples of 8.
+ * psk_moe_experts_q4: weights in 4 bits, count = experts in all three, W1 and W3 alike in rows and cols, all with one scale_type.
+ * With PSK_F16 and 16-bit weights, values between the two products of 2^24 and more become infinite.
+ * The workspace is for both.
+ */
+enum { PSK_ACT_SILU = 0, PSK_ACT_GELU = 1 };   /* v / (1 + exp(-v));  v (1 + erf(v / sqrt 2)) / 2 */
+size_t psk_moe_workspace_bytes(int64_t n, int64_t dim, int64_t inter, int64_t experts, int32_t top_k);
+int psk_moe_experts(int64_t n, int64_t dim, int64_t inter, int64_t experts, int32_t top_k, int act, int type, const void *X,
+                    int64_t ldx, const int32_t *crd, const float *vals, const void *W1, const void *W3, int64_t ld1,
+                    int64_t stride1, const void *W2, int64_t ld2, int64_t stride2, void *Y, int64_t ldy, void *workspace,
+                    size_t workspace_bytes, void *stream);
+int psk_moe_experts_q4(int64_t n, int32_t top_k, int act, int type, const void *X, int64_t ldx, const int32_t *crd,
+                       const float *vals, const psk_q4 *W1, const psk_q4 *W3, const psk_q4 *W2, void *Y, int64_t ldy,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -35,6 +35,8 @@ EXPORTS = [
     "psk_slab_mem_bytes", "psk_slab_build_workspace_bytes", "psk_slab_spmv_workspace_bytes", "psk_slab_build_csr",
     "psk_spmv_slab", "psk_slab_mem_bytes_f64", "psk_slab_build_workspace_bytes_f64", "psk_slab_build_csr_f64",
     "psk_spmv_slab_f64", "psk_cu_trace_set", "psk_calibrate_stream_read", "psk_calibrate_gather", "psk_calibrate_gather_lds",
+    "psk_gemm_q4_workspace_bytes", "psk_gemm_q4", "psk_moe_route_workspace_bytes", "psk_moe_route", "psk_moe_workspace_bytes",
+    "psk_moe_experts", "psk_moe_experts_q4",
 ]
 
 
@@ -46,6 +48,19 @@ class psk_slab(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in ("rows", "cols", "nnz", "nslabs", "nslots", "nchunks", "npairs", "nq")] + \
                [(n, ctypes.c_int32) for n in ("slab_cols", "chunk", "tile", "value_bytes")] + \
                [(n, ctypes.c_void_p) for n in ("svals", "scol", "chunk_pair", "slab_chunk", "qpos", "qidx", "qtile_row")]
+
+
+PSK_F32, PSK_F16, PSK_BF16 = 0, 1, 2
+PSK_SCORE_SOFTMAX, PSK_SCORE_SIGMOID = 0, 1
+PSK_ACT_SILU, PSK_ACT_GELU = 0, 1
+PSK_MAX_VECTORS, PSK_MOE_MAX_EXPERTS, PSK_MOE_MAX_TOP_K = 1 << 20, 1024, 64
+
+
+class psk_q4(ctypes.Structure):
+    """Mirror of the C struct psk_q4 (host memory; the pointers are device addresses)."""
+    _fields_ = [(n, ctypes.c_int64) for n in ("count", "rows", "cols")] + [(n, ctypes.c_int32) for n in ("group", "scale_type")] + \
+               [(n, ctypes.c_void_p) for n in ("codes", "scales", "zeros")] + \
+               [(n, ctypes.c_int64) for n in ("ld_codes", "ld_scales", "stride_codes", "stride_scales")]
 
 
 class PskError(RuntimeError):
@@ -158,6 +173,17 @@ def lib() -> ctypes.CDLL:
         L.psk_spmv_csr_rowsplit.restype = ci
         L.psk_spmm_csr_rowsplit.argtypes = [i64, i64, i64, p, p, p, p, i32, i64, p, i64, p]
         L.psk_spmm_csr_rowsplit.restype = ci
+        q4, f32 = ctypes.POINTER(psk_q4), ctypes.c_float
+        L.psk_gemm_q4_workspace_bytes.argtypes, L.psk_gemm_q4_workspace_bytes.restype = [i64, i64, i64, ci], sz
+        L.psk_gemm_q4.argtypes, L.psk_gemm_q4.restype = [q4, i64, ci, p, i64, p, i64, p, sz, p], ci
+        L.psk_moe_route_workspace_bytes.argtypes, L.psk_moe_route_workspace_bytes.restype = [i64, i64], sz
+        L.psk_moe_route.argtypes = [i64, i64, i64, i32, ci, ci, f32, ci, p, i64, ci, p, i64, p, p, p, p, sz, p]
+        L.psk_moe_route.restype = ci
+        L.psk_moe_workspace_bytes.argtypes, L.psk_moe_workspace_bytes.restype = [i64, i64, i64, i64, i32], sz
+        L.psk_moe_experts.argtypes = [i64, i64, i64, i64, i32, ci, ci, p, i64, p, p, p, p, i64, i64, p, i64, i64, p, i64, p, sz, p]
+        L.psk_moe_experts.restype = ci
+        L.psk_moe_experts_q4.argtypes = [i64, i32, ci, ci, p, i64, p, p, q4, q4, q4, p, i64, p, sz, p]
+        L.psk_moe_experts_q4.restype = ci
         if _marshal is None:
             native = _native_side()
             if native is not None:
@@ -643,3 +669,182 @@ def psk_cu_trace_set(records) -> None:
     n = 0 if records is None else records.numel() // 3
     st = lib().psk_cu_trace_set(_ptr(records, torch.int64) if records is not None else None, n)
     _check(st, "psk_cu_trace_set")
+
+
+_TYPES = {torch.float32: PSK_F32, torch.float16: PSK_F16, torch.bfloat16: PSK_BF16}
+
+
+def _type(t, what):
+    try:
+        return _TYPES[t.dtype]
+    except KeyError:
+        raise ValueError("%s: dtype %s is not one of float32, float16, bfloat16" % (what, t.dtype)) from None
+
+
+def _rows(t, rows, cols, dtype, what):
+    """(address, leading dimension) of a matrix of rows x cols."""
+    if t.dim() != 2 or tuple(t.shape) != (rows, cols):
+        raise ValueError("%s: expected a tensor of %d x %d, got %s" % (what, rows, cols, tuple(t.shape)))
+    return _ptr(t, dtype), (int(t.stride(0)) if rows > 1 else max(int(t.stride(0)), cols))
+
+
+def _gating_ptrs(crd, vals, n, top_k, what):
+    for t, dtype in ((crd, torch.int32), (vals, torch.float32)):
+        if tuple(t.shape) != (n, top_k) or not t.is_contiguous():
+            raise ValueError("%s: crd and vals must be contiguous tensors of %d x %d" % (what, n, top_k))
+    return _ptr(crd, torch.int32), _ptr(vals, torch.float32)
+
+
+def _one_device(what, *tensors):
+    """A call runs on the current device: all of its tensors have to be there."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != here:
+            raise ValueError("%s: a tensor is on cuda:%d, the current device is cuda:%d" % (what, t.get_device(), here))
+
+
+class Q4:
+    """One or more matrices in 4 bits: the C struct (`desc`) and the tensors it points into.
+
+    codes: uint8, rows x bytes or count x rows x bytes, two columns to a byte, the low half first; a row holds a multiple of 16
+    bytes, ceil(cols / 32) * 16 at least.  scales: (count x) rows x ceil(cols / group).  zeros: uint8 laid out as the scales, or
+    None for 8 everywhere."""
+
+    def __init__(self, codes, scales, zeros=None, cols=None, group=128):
+        if codes.dtype != torch.uint8 or (zeros is not None and zeros.dtype != torch.uint8):
+            raise ValueError("codes and zeros must be uint8")
+        if codes.dim() not in (2, 3) or scales.dim() != codes.dim():
+            raise ValueError("codes and scales must both have two dimensions, or three for several matrices")
+        if group < 32 or group & (group - 1):
+            raise ValueError("group must be a power of two, 32 or more")
+        cols = 2 * codes.shape[-1] if cols is None else int(cols)
+        groups = (cols + group - 1) // group
+        if cols < 0 or codes.shape[-1] < (cols + 31) // 32 * 16:
+            raise ValueError("a row of codes must hold %d bytes for %d columns" % ((cols + 31) // 32 * 16, cols))
+        if tuple(scales.shape) != tuple(codes.shape[:-1]) + (groups,):
+            raise ValueError("scales must have the shape %s" % (tuple(codes.shape[:-1]) + (groups,),))
+        if zeros is not None and (zeros.shape != scales.shape or zeros.stride() != scales.stride()):
+            raise ValueError("zeros must be laid out as the scales")
+        self.codes, self.scales, self.zeros = codes, scales, zeros
+        d = self.desc = psk_q4()
+        d.count, d.rows, d.cols, d.group, d.scale_type = codes.shape[0] if codes.dim() == 3 else 1, codes.shape[-2], cols, group, _type(scales, "scales")
+        d.codes, d.scales, d.zeros = _ptr(codes, torch.uint8), _ptr(scales), _ptr(zeros)
+        d.ld_codes = max(int(codes.stride(-2)), codes.shape[-1]) if codes.shape[-2] <= 1 else int(codes.stride(-2))
+        d.ld_scales = max(int(scales.stride(-2)), groups) if codes.shape[-2] <= 1 else int(scales.stride(-2))
+        if codes.dim() == 3 and codes.shape[0] > 1:
+            d.stride_codes, d.stride_scales = int(codes.stride(0)), int(scales.stride(0))
+
+
+def psk_gemm_q4_workspace_bytes(rows: int, cols: int, n: int, type: int) -> int:
+    return int(lib().psk_gemm_q4_workspace_bytes(int(rows), int(cols), int(n), int(type)))
+
+
+def psk_gemm_q4_workspace(A: Q4, X, stream=None):
+    """A byte tensor that suits psk_gemm_q4 with vectors like X (n x cols)."""
+    n = psk_gemm_q4_workspace_bytes(A.desc.rows, A.desc.cols, X.shape[0], _type(X, "X"))
+    if n == 0:
+        raise ValueError("invalid arguments for psk_gemm_q4_workspace_bytes")
+    return _alloc_bytes(n, X.device, stream)
+
+
+def psk_gemm_q4(A: Q4, X, Y, ws=None, stream=None):
+    """Y (n x rows) = X (n x cols) A^T for one matrix in 4 bits."""
+    n, type = X.shape[0], _type(X, "psk_gemm_q4")
+    x, ldx = _rows(X, n, A.desc.cols, X.dtype, "psk_gemm_q4: X")
+    y, ldy = _rows(Y, n, A.desc.rows, X.dtype, "psk_gemm_q4: Y")
+    _one_device("psk_gemm_q4", X, Y, A.codes, A.scales, A.zeros, ws)
+    if ws is None:
+        ws = psk_gemm_q4_workspace(A, X, stream)
+    st = lib().psk_gemm_q4(ctypes.byref(A.desc), n, type, x, ldx, y, ldy, _ptr(ws), ws.numel(), _stream(stream))
+    if st:
+        _check(st, "psk_gemm_q4")
+    return Y
+
+
+def psk_moe_route_workspace_bytes(n: int, experts: int) -> int:
+    return int(lib().psk_moe_route_workspace_bytes(int(n), int(experts)))
+
+
+def psk_moe_route_workspace(n, experts, device="cuda", stream=None):
+    b = psk_moe_route_workspace_bytes(n, experts)
+    if b == 0:
+        raise ValueError("invalid arguments for psk_moe_route_workspace_bytes")
+    return _alloc_bytes(b, device, stream)
+
+
+def psk_moe_route(X, W, crd, vals, score=PSK_SCORE_SOFTMAX, bias=None, normalise=True, factor=1.0, ws=None, stream=None):
+    """(crd, vals): the gating matrix of the tokens X (n x dim) for the router weights W (experts x dim); top_k = crd.shape[1]."""
+    n, dim, experts = X.shape[0], X.shape[1], W.shape[0]
+    type, wtype, top_k = _type(X, "psk_moe_route"), _type(W, "psk_moe_route"), crd.shape[1]
+    x, ldx = _rows(X, n, dim, X.dtype, "psk_moe_route: X")
+    w, ldw = _rows(W, experts, dim, W.dtype, "psk_moe_route: W")
+    c, v = _gating_ptrs(crd, vals, n, top_k, "psk_moe_route")
+    if bias is not None and (tuple(bias.shape) != (experts,) or not bias.is_contiguous()):
+        raise ValueError("psk_moe_route: bias must be a contiguous tensor of %d" % experts)
+    _one_device("psk_moe_route", X, W, crd, vals, bias, ws)
+    if ws is None:
+        ws = psk_moe_route_workspace(n, experts, X.device, stream)
+    st = lib().psk_moe_route(n, dim, experts, top_k, int(score), int(bool(normalise)), float(factor), type, x, ldx, wtype, w, ldw,
+                             _ptr(bias, torch.float32), c, v, _ptr(ws), ws.numel(), _stream(stream))
+    if st:
+        _check(st, "psk_moe_route")
+    return crd, vals
+
+
+def psk_moe_workspace_bytes(n: int, dim: int, inter: int, experts: int, top_k: int) -> int:
+    return int(lib().psk_moe_workspace_bytes(int(n), int(dim), int(inter), int(experts), int(top_k)))
+
+
+def psk_moe_workspace(n, dim, inter, experts, top_k, device="cuda", stream=None):
+    b = psk_moe_workspace_bytes(n, dim, inter, experts, top_k)
+    if b == 0:
+        raise ValueError("invalid arguments for psk_moe_workspace_bytes")
+    return _alloc_bytes(b, device, stream)
+
+
+def _experts_of(W, experts, rows, cols, dtype, what):
+    """(address, leading dimension, stride between experts)."""
+    if tuple(W.shape) != (experts, rows, cols):
+        raise ValueError("%s: expected a tensor of %d x %d x %d, got %s" % (what, experts, rows, cols, tuple(W.shape)))
+    return _ptr(W, dtype), (int(W.stride(1)) if rows > 1 else (cols + 7) // 8 * 8), (int(W.stride(0)) if experts > 1 else 0)
+
+
+def psk_moe_experts(X, crd, vals, W1, W3, W2, Y, act=PSK_ACT_SILU, ws=None, stream=None):
+    """Y (n x dim) = the layer for the tokens X with the gating matrix (crd, vals), weights of the type of X: W1, W3 experts x inter x dim
+    (strided alike), W2 experts x dim x inter."""
+    n, dim = X.shape
+    experts, inter = W1.shape[0], W1.shape[1]
+    type, top_k = _type(X, "psk_moe_experts"), crd.shape[1]
+    x, ldx = _rows(X, n, dim, X.dtype, "psk_moe_experts: X")
+    y, ldy = _rows(Y, n, dim, X.dtype, "psk_moe_experts: Y")
+    c, v = _gating_ptrs(crd, vals, n, top_k, "psk_moe_experts")
+    w1, ld1, stride1 = _experts_of(W1, experts, inter, dim, X.dtype, "psk_moe_experts: W1")
+    w3, ld3, stride3 = _experts_of(W3, experts, inter, dim, X.dtype, "psk_moe_experts: W3")
+    w2, ld2, stride2 = _experts_of(W2, experts, dim, inter, X.dtype, "psk_moe_experts: W2")
+    if (ld1, stride1) != (ld3, stride3):
+        raise ValueError("psk_moe_experts: W1 and W3 must have the same strides")
+    _one_device("psk_moe_experts", X, crd, vals, W1, W3, W2, Y, ws)
+    if ws is None:
+        ws = psk_moe_workspace(n, dim, inter, experts, top_k, X.device, stream)
+    st = lib().psk_moe_experts(n, dim, inter, experts, top_k, int(act), type, x, ldx, c, v, w1, w3, ld1, stride1, w2, ld2, stride2, y, ldy,
+                               _ptr(ws), ws.numel(), _stream(stream))
+    if st:
+        _check(st, "psk_moe_experts")
+    return Y
+
+
+def psk_moe_experts_q4(X, crd, vals, W1: Q4, W3: Q4, W2: Q4, Y, act=PSK_ACT_SILU, ws=None, stream=None):
+    """The layer with weights in 4 bits."""
+    n, dim = X.shape
+    type, top_k = _type(X, "psk_moe_experts_q4"), crd.shape[1]
+    x, ldx = _rows(X, n, W1.desc.cols, X.dtype, "psk_moe_experts_q4: X")
+    y, ldy = _rows(Y, n, W2.desc.rows, X.dtype, "psk_moe_experts_q4: Y")
+    c, v = _gating_ptrs(crd, vals, n, top_k, "psk_moe_experts_q4")
+    _one_device("psk_moe_experts_q4", X, crd, vals, Y, ws, *(t for w in (W1, W3, W2) for t in (w.codes, w.scales, w.zeros)))
+    if ws is None:
+        ws = psk_moe_workspace(n, dim, W1.desc.rows, W1.desc.count, top_k, X.device, stream)
+    st = lib().psk_moe_experts_q4(n, top_k, int(act), type, x, ldx, c, v, ctypes.byref(W1.desc), ctypes.byref(W3.desc), ctypes.byref(W2.desc), y,
+                                  ldy, _ptr(ws), ws.numel(), _stream(stream))
+    if st:
+        _check(st, "psk_moe_experts_q4")
+    return Y

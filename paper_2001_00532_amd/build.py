@@ -22,8 +22,9 @@ OBJDIR_TRACE = os.path.join(HERE, "_build_trace")
 OUT_MARSHAL = os.path.join(HERE, "_marshal.so")
 MARSHAL_FOR = os.path.join(OBJDIR, "marshal_built_for")
 
-SOURCES = ["api.hip", "partition.hip", "spmv_csr.hip", "spmm.hip", "spmv_bcsr.hip", "mttkrp.hip", "spmv_csr_f64.hip", "spmv_csr_divide.hip", "spmv_bcsr_g.hip", "spmm_narrow.hip", "spmm_blocks.hip", "slab.hip", "api_slab.hip", "calibrate.hip"]
-HEADERS = ["psk_dev.h", "psk_internal.h", os.path.join("..", "..", "include", "psk.h")]
+SOURCES = ["api.hip", "partition.hip", "spmv_csr.hip", "spmm.hip", "spmv_bcsr.hip", "mttkrp.hip", "spmv_csr_f64.hip", "spmv_csr_divide.hip", "spmv_bcsr_g.hip", "spmm_narrow.hip", "spmm_blocks.hip", "slab.hip", "api_slab.hip", "calibrate.hip",
+           "gemm_q4.hip", "moe_route.hip", "moe.hip", "api_serving.hip"]
+HEADERS = ["psk_dev.h", "psk_mfma.h", "psk_internal.h", os.path.join("..", "..", "include", "psk.h")]
 
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",

@@ -1,0 +1,305 @@
+"""The router and the layer of a mixture of experts against the plain form in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+
+import serving_ref as R
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+import paper_2001_00532_amd as psk  # noqa: E402
+
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+PARTS = {"f16": 2.0 ** -22, "bf16": 2.0 ** -16}
+
+
+# ------------------------------------------------------------------ router
+def routed(x, w, top_k, **kw):
+    n = x.shape[0]
+    crd = torch.full((n, top_k), 99, dtype=torch.int32, device="cuda")
+    vals = torch.full((n, top_k), 99.0, device="cuda")
+    psk.psk_moe_route(x.cuda(), w.cuda(), crd, vals, **{k: v.cuda() if torch.is_tensor(v) else v for k, v in kw.items()})
+    return crd.cpu(), vals.cpu()
+
+
+def compare_route(x, w, top_k, score, bias, normalise, factor, what):
+    ids, gates = R.route(x, w, top_k, score, bias, normalise, factor)
+    crd, vals = routed(x, w, top_k, score=score, bias=bias, normalise=normalise, factor=factor)
+    assert torch.equal(crd, ids), what
+    # rounding to 32 bits; the 64-bit logits behind differ by far less
+    R.check(vals, gates, gates.abs() * 2.0 ** -23 + 1e-40, what)
+
+
+@pytest.mark.parametrize("dtype,wtype", [("f16", "f16"), ("bf16", "bf16"), ("f32", "f32"), ("f16", "f32"), ("bf16", "f32")])
+@pytest.mark.parametrize("n,dim,experts,top_k,score,bias,normalise", [
+    (1, 1, 1, 1, 0, False, True), (1, 300, 64, 6, 0, False, True), (9, 77, 65, 8, 1, True, True), (3, 1025, 8, 8, 0, True, False),
+    (17, 64, 200, 3, 1, False, False), (2, 40, 1024, 64, 0, False, True)])
+def test_route(dtype, wtype, n, dim, experts, top_k, score, bias, normalise):
+    rng = np.random.default_rng(n * 100 + experts)
+    x = torch.from_numpy(rng.standard_normal((n, dim))).to(TYPES[dtype])
+    w = torch.from_numpy(rng.standard_normal((experts, dim)) / math.sqrt(dim)).to(TYPES[wtype])
+    b = torch.from_numpy(rng.uniform(-0.3, 0.3, experts)).float() if bias else None
+    compare_route(x, w, top_k, score, b, normalise, 1.0 if normalise else 2.5, "%s %s %d experts" % (dtype, wtype, experts))
+
+
+@pytest.mark.parametrize("score", [0, 1])
+def test_equal_logits_go_to_the_lowest_index(score):
+    """Equal rows of the router's weights; and logits that differ in the last bits of a long sum only."""
+    rng = np.random.default_rng(3)
+    x = torch.from_numpy(rng.standard_normal((5, 200))).float()
+    w = torch.from_numpy(rng.standard_normal((1, 200))).float().repeat(70, 1)
+    w[40] = w[40] + 1e-3 * x[2]                              # for token 2 a larger logit
+    crd, _ = routed(x, w, 4, score=score)
+    assert crd[2].tolist() == [40, 0, 1, 2]
+    for t in (0, 1, 3, 4):
+        assert crd[t].tolist() in ([0, 1, 2, 3], [40, 0, 1, 2])
+    compare_route(x, w, 4, score, None, True, 1.0, "ties")
+    big = torch.zeros(1, 200)
+    big[0, 0], big[0, 1] = 1.0, 2.0 ** -40
+    w = torch.zeros(3, 200)
+    w[:, 0] = 1.0
+    w[2, 1] = 1.0                                            # larger by 2^-40: invisible in 32 bits
+    crd, _ = routed(big, w, 2, score=score)
+    assert crd[0].tolist() == [2, 0]
+
+
+@pytest.mark.parametrize("score", [0, 1])
+def test_experts_that_are_never_taken_and_rows_that_are_no_numbers(score):
+    rng = np.random.default_rng(4)
+    x = torch.from_numpy(rng.standard_normal((4, 50))).float()
+    w = torch.from_numpy(rng.standard_normal((10, 50))).float()
+    bias = torch.zeros(10)
+    bias[[0, 3, 4, 5, 6, 7, 9]] = -math.inf
+    crd, vals = routed(x, w, 6, score=score, bias=bias, normalise=True)
+    for t in range(4):
+        assert sorted(crd[t, :3].tolist()) == [1, 2, 8] and crd[t, 3:].tolist() == [-1, -1, -1]
+        assert vals[t, 3:].tolist() == [0, 0, 0] and abs(float(vals[t].sum()) - 1) < 1e-6
+    compare_route(x, w, 6, score, bias, True, 1.0, "few experts")
+    bias[:] = -math.inf
+    crd, vals = routed(x, w, 6, score=score, bias=bias, normalise=True)
+    assert bool((crd == -1).all()) and bool((vals == 0).all())
+    x[1, 7] = float("nan")
+    crd, vals = routed(x, w, 3, score=score)
+    assert crd[1].tolist() == [0, 1, 2] and bool(torch.isnan(vals[1]).all())
+    assert bool(torch.isfinite(vals[[0, 2, 3]]).all())
+    x[1] = 0
+    x[1, 7], w[:, 7] = 1e30, 1e30 * torch.sign(w[:, 7])      # logits of +-1e60
+    compare_route(x, w, 3, score, None, False, 1.0, "far logits")
+
+
+def test_route_strides():
+    rng = np.random.default_rng(5)
+    x, w = torch.from_numpy(rng.standard_normal((5, 90))).half(), torch.from_numpy(rng.standard_normal((12, 95))).half()
+    a, b = routed(x[:, 3:80].contiguous(), w[:, 5:82].contiguous(), 4)
+    xd, wd = x.cuda(), w.cuda()
+    crd, vals = torch.empty(5, 4, dtype=torch.int32, device="cuda"), torch.empty(5, 4, device="cuda")
+    psk.psk_moe_route(xd[:, 3:80], wd[:, 5:82], crd, vals)
+    assert torch.equal(crd.cpu(), a) and torch.equal(vals.cpu(), b)
+
+
+# ------------------------------------------------------------------ layer
+def gating(rng, n, experts, top_k, kind="random"):
+    crd = np.full((n, top_k), -1, dtype=np.int32)
+    for t in range(n):
+        k = min(top_k, experts)
+        crd[t, :k] = rng.choice(experts, size=k, replace=False)
+    if kind == "holes":
+        crd[rng.random((n, top_k)) < 0.5] = -1
+        crd[n // 2] = -1
+        crd[0, 0] = experts                                  # outside: no expert
+        crd[n - 1, -1] = -2 ** 31
+    elif kind == "none":
+        crd[:] = -1
+    elif kind == "one":
+        crd[:] = -1
+        crd[:, top_k // 2] = experts - 1
+    elif kind == "twice":
+        crd[:] = rng.integers(0, experts, (n, 1))
+    return torch.from_numpy(crd), torch.from_numpy(rng.uniform(0.05, 1.0, (n, top_k)).astype(np.float32))
+
+
+def run16(x, crd, vals, w1, w3, w2, act=0):
+    n, dim = x.shape
+    buf = torch.full((n + 2, dim + 3), 77.0, dtype=x.dtype, device="cuda")
+    y = buf[1:n + 1, :dim]
+    psk.psk_moe_experts(x.cuda(), crd.cuda(), vals.cuda(), w1.cuda(), w3.cuda(), w2.cuda(), y, act=act)
+    torch.cuda.synchronize()
+    assert bool((buf[0] == 77).all()) and bool((buf[n + 1] == 77).all()) and bool((buf[:, dim:] == 77).all()), "wrote past Y"
+    return y
+
+
+def padded(rng, shape, scale, dtype):
+    """Weights whose rows are a multiple of 8 apart, NaN behind them."""
+    e, r, c = shape
+    buf = torch.full((e, r, (c + 7) // 8 * 8 + 8), float("nan"), dtype=dtype)
+    buf[:, :, :c] = torch.from_numpy(rng.standard_normal(shape) * scale).to(dtype)
+    return buf.cuda()[:, :, :c]
+
+
+def doubles(w):
+    return [m.cpu().double() for m in w]
+
+
+SHAPES = [(1, 32, 16, 4, 2, "random"), (1, 8, 1, 1, 1, "random"), (3, 100, 45, 5, 3, "holes"), (17, 64, 130, 3, 2, "random"), (6, 200, 72, 70, 8, "random"),
+          (40, 72, 24, 2, 2, "random"), (5, 40, 33, 6, 2, "none"), (70, 48, 40, 3, 2, "one"), (9, 520, 260, 4, 4, "twice"), (130, 24, 24, 2, 3, "one")]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,dim,inter,experts,top_k,kind", SHAPES)
+def test_layer(dtype, n, dim, inter, experts, top_k, kind):
+    t = TYPES[dtype]
+    rng = np.random.default_rng(n * 31 + dim)
+    x = torch.from_numpy(rng.standard_normal((n, dim))).to(t)
+    crd, vals = gating(rng, n, experts, top_k, kind)
+    w1, w3 = padded(rng, (experts, inter, dim), 1 / math.sqrt(dim), t), padded(rng, (experts, inter, dim), 1 / math.sqrt(dim), t)
+    w2 = padded(rng, (experts, dim, inter), 1 / math.sqrt(inter), t)
+    for act in (0, 1):
+        ref, bound = R.layer(x, crd, vals, doubles(w1), doubles(w3), doubles(w2), act, t, PARTS[dtype])
+        R.check(run16(x, crd, vals, w1, w3, w2, act), ref, bound, "%s act %d %s" % (dtype, act, kind))
+
+
+def q4_of(w, cols, group):
+    return psk.Q4(*(None if t is None else t.cuda() for t in w), cols=cols, group=group)
+
+
+def q4_doubles(w, cols, group):
+    return [R.dequantised(w[0][e], w[1][e], None if w[2] is None else w[2][e], cols, group) for e in range(w[0].shape[0])]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("groups,scale32", [((128, 128), False), ((32, 64), False), ((64, 32), True)])
+@pytest.mark.parametrize("n,dim,inter,experts,top_k,kind", SHAPES)
+def test_layer_q4(dtype, groups, scale32, n, dim, inter, experts, top_k, kind):
+    t = TYPES[dtype]
+    st = torch.float32 if scale32 else t
+    rng = np.random.default_rng(n * 37 + dim)
+    x = torch.from_numpy(rng.standard_normal((n, dim))).to(t)
+    crd, vals = gating(rng, n, experts, top_k, kind)
+    g1, g2 = groups
+    w1 = R.q4_weights(rng, inter, dim, g1, True, st, experts, scale=0.4 / math.sqrt(dim))
+    w3 = R.q4_weights(rng, inter, dim, g1, False, st, experts, scale=0.4 / math.sqrt(dim), pad=1)
+    w2 = R.q4_weights(rng, dim, inter, g2, True, st, experts, scale=0.4 / math.sqrt(inter))
+    y = torch.full((n, dim), 77.0, dtype=t, device="cuda")
+    psk.psk_moe_experts_q4(x.cuda(), crd.cuda(), vals.cuda(), q4_of(w1, dim, g1), q4_of(w3, dim, g1), q4_of(w2, inter, g2), y)
+    ref, bound = R.layer(x, crd, vals, q4_doubles(w1, dim, g1), q4_doubles(w3, dim, g1), q4_doubles(w2, inter, g2), 0, t, 2.0 ** -16)
+    R.check(y, ref, bound, "q4 %s %s" % (dtype, kind))
+
+
+def test_matrices_with_groups_and_zero_points_of_their_own():
+    """Each of the three matrices has its own group, and zero points or none."""
+    rng = np.random.default_rng(16)
+    n, dim, inter, experts, t = 6, 300, 150, 4, torch.float16
+    x = torch.from_numpy(rng.standard_normal((n, dim))).to(t)
+    crd, vals = gating(rng, n, experts, 2)
+    for groups, zeros in (((32, 128, 64), (True, False, False)), ((256, 64, 128), (False, True, True)), ((128, 1024, 32), (True, True, False))):
+        w = [R.q4_weights(rng, r, c, g, z, t, experts, scale=0.4 / math.sqrt(c))
+             for (r, c), g, z in zip(((inter, dim), (inter, dim), (dim, inter)), groups, zeros)]
+        y = torch.full((n, dim), 77.0, dtype=t, device="cuda")
+        psk.psk_moe_experts_q4(x.cuda(), crd.cuda(), vals.cuda(), *(q4_of(m, c, g) for m, c, g in zip(w, (dim, dim, inter), groups)), y)
+        ref, bound = R.layer(x, crd, vals, *(q4_doubles(m, c, g) for m, c, g in zip(w, (dim, dim, inter), groups)), 0, t, 2.0 ** -16)
+        R.check(y, ref, bound, "groups %s" % (groups,))
+
+
+def test_more_positions_than_one_pair_of_launches_takes():
+    """3000 tokens with two experts each: 6000 positions."""
+    rng = np.random.default_rng(11)
+    n, dim, inter, experts = 3000, 24, 16, 5
+    x = torch.from_numpy(rng.standard_normal((n, dim))).bfloat16()
+    crd = torch.from_numpy(rng.integers(-1, experts, (n, 2)).astype(np.int32))
+    vals = torch.from_numpy(rng.uniform(0.1, 1, (n, 2)).astype(np.float32))
+    w = [padded(rng, s, 0.3, torch.bfloat16) for s in ((experts, inter, dim), (experts, inter, dim), (experts, dim, inter))]
+    ref, bound = R.layer(x, crd, vals, *map(doubles, w), 0, torch.bfloat16, PARTS["bf16"])
+    R.check(run16(x, crd, vals, *w), ref, bound, "6000 positions")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_a_token_that_is_no_number_spoils_its_own_row(dtype):
+    rng = np.random.default_rng(12)
+    t, n, dim, inter, experts = TYPES[dtype], 8, 40, 24, 2
+    x = torch.from_numpy(rng.standard_normal((n, dim))).to(t)
+    crd, vals = gating(rng, n, experts, 2)
+    w = [padded(rng, s, 0.2, t) for s in ((experts, inter, dim), (experts, inter, dim), (experts, dim, inter))]
+    clean = run16(x, crd, vals, *w).clone()
+    x[3, 5], x[6, 39] = float("nan"), float("inf")
+    got = run16(x, crd, vals, *w)
+    keep = [0, 1, 2, 4, 5, 7]
+    assert torch.equal(got[keep], clean[keep])
+    assert bool(torch.isnan(got[3]).all()) and not bool(torch.isfinite(got[6]).any())
+
+
+def test_values_between_the_products_beyond_the_range_of_f16():
+    """h of about 10^6 with small weights behind it: Y is an ordinary number."""
+    rng = np.random.default_rng(13)
+    n, dim, inter = 2, 64, 32
+    x = torch.from_numpy(rng.uniform(20, 40, (n, dim))).half()
+    w1 = torch.from_numpy(rng.uniform(0.5, 1.0, (1, inter, dim))).half()
+    w2 = torch.from_numpy(rng.standard_normal((1, dim, inter)) * 1e-5).half()
+    crd, vals = torch.zeros(n, 1, dtype=torch.int32), torch.ones(n, 1)
+    ref, bound = R.layer(x, crd, vals, doubles(w1), doubles(w1), doubles(w2), 0, torch.float16, PARTS["f16"])
+    R.check(run16(x, crd, vals, w1, w1, w2), ref, bound, "large h")
+
+
+def test_one_matrix_holds_both_halves():
+    """W1 and W3 as the halves of one tensor, experts a stride apart."""
+    rng = np.random.default_rng(14)
+    n, dim, inter, experts = 4, 48, 32, 3
+    both = torch.from_numpy(rng.standard_normal((experts, 2 * inter, dim)) * 0.2).bfloat16().cuda()
+    w2 = torch.from_numpy(rng.standard_normal((experts, dim, inter)) * 0.2).bfloat16().cuda()
+    x = torch.from_numpy(rng.standard_normal((n, dim))).bfloat16()
+    crd, vals = gating(rng, n, experts, 2)
+    a = run16(x, crd, vals, both[:, :inter], both[:, inter:], w2)
+    b = run16(x, crd, vals, both[:, :inter].contiguous(), both[:, inter:].contiguous(), w2)
+    assert torch.equal(a, b)
+
+
+# ------------------------------------------------------------------ together
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_a_serving_step(dtype):
+    """A projection in 4 bits, the router on what it gives and the layer in 4 bits, eager on a side stream and captured; every
+    replay follows new activations and another number of padded tokens, with eager work in between."""
+    t = TYPES[dtype]
+    rng = np.random.default_rng(15)
+    n, dim, inter, experts, top_k, group = 5, 256, 96, 12, 3, 64
+    wp = R.q4_weights(rng, dim, dim, group, True, t, scale=0.5 / math.sqrt(dim))
+    w1, w3 = (R.q4_weights(rng, inter, dim, group, True, t, experts, scale=0.4 / math.sqrt(dim)) for _ in range(2))
+    w2 = R.q4_weights(rng, dim, inter, group, True, t, experts, scale=0.4 / math.sqrt(inter))
+    wr = torch.from_numpy(rng.standard_normal((experts, dim)) / math.sqrt(dim)).to(t)
+    P, A1, A3, A2, wrd = q4_of(wp, dim, group), q4_of(w1, dim, group), q4_of(w3, dim, group), q4_of(w2, inter, group), wr.cuda()
+    x, z, y = (torch.zeros(n, dim, dtype=t, device="cuda") for _ in range(3))
+    crd, vals = torch.zeros(n, top_k, dtype=torch.int32, device="cuda"), torch.zeros(n, top_k, device="cuda")
+    ws = (psk.psk_gemm_q4_workspace(P, x), psk.psk_moe_route_workspace(n, experts), psk.psk_moe_workspace(n, dim, inter, experts, top_k))
+
+    def step():
+        psk.psk_gemm_q4(P, x, z, ws=ws[0])
+        psk.psk_moe_route(z, wrd, crd, vals, ws=ws[1])
+        psk.psk_moe_experts_q4(z, crd, vals, A1, A3, A2, y, ws=ws[2])
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    dense = q4_doubles(w1, dim, group), q4_doubles(w3, dim, group), q4_doubles(w2, inter, group)
+    for rep in range(4):
+        xh = torch.from_numpy(rng.standard_normal((n, dim))).to(t)
+        x.copy_(xh)
+        for b in ws:
+            b.fill_(0xFF)
+        y.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        ref, bound = R.gemm(R.dequantised(*wp, dim, group), xh, t)
+        R.check(z, ref, bound, "projection %d" % rep)
+        ids, gates = R.route(z.cpu(), wr, top_k, 0, None, True, 1.0)
+        assert torch.equal(crd.cpu(), ids)
+        R.check(vals, gates, gates.abs() * 2.0 ** -23 + 1e-40, "gates %d" % rep)
+        ref, bound = R.layer(z.cpu(), crd.cpu(), vals.cpu(), *dense, 0, t, 2.0 ** -16)
+        R.check(y, ref, bound, "layer %d" % rep)
+        kept = y.clone()
+        step()
+        assert torch.equal(kept, y)

@@ -1,0 +1,178 @@
+"""Products with 4-bit weights against the plain form in 64 bits."""
+import numpy as np
+import pytest
+
+import serving_ref as R
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+import paper_2001_00532_amd as psk  # noqa: E402
+
+TYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def dev(*ts):
+    return [None if t is None else t.cuda() for t in ts]
+
+
+def product(w, x, cols, group, ldy=None):
+    """psk_gemm_q4 into a buffer with guards around Y's rows; returns Y."""
+    n, rows = x.shape[0], w[0].shape[0]
+    A = psk.Q4(*dev(*w), cols=cols, group=group)
+    pad = 0 if ldy is None else ldy - rows
+    buf = torch.full((n + 2, rows + pad), 77.0, dtype=x.dtype, device="cuda")
+    Y = buf[1:n + 1, :rows]
+    psk.psk_gemm_q4(A, x, Y)
+    torch.cuda.synchronize()
+    assert bool((buf[0] == 77).all()) and bool((buf[n + 1] == 77).all()) and bool((buf[:, rows:] == 77).all()), "wrote past Y"
+    return Y
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("rows,cols,n,group,zeros,scale32", [
+    (1, 1, 1, 32, False, False), (16, 32, 1, 32, True, False), (17, 31, 2, 32, True, True), (15, 33, 5, 64, False, False),
+    (40, 127, 6, 128, True, False), (33, 128, 16, 64, False, True), (100, 129, 17, 32, True, False), (64, 1000, 3, 128, True, True),
+    (50, 2051, 1, 64, True, False), (48, 4100, 33, 256, False, False), (20, 640, 64, 32, True, False), (35, 300, 65, 4096, True, False),
+    (18, 1100, 130, 128, False, False), (8, 16400, 1, 128, True, False)])
+def test_products(dtype, rows, cols, n, group, zeros, scale32):
+    t = TYPES[dtype]
+    rng = np.random.default_rng(rows * 1000 + cols)
+    w = R.q4_weights(rng, rows, cols, group, zeros, torch.float32 if scale32 else t)
+    x = torch.from_numpy(rng.standard_normal((n, cols))).to(t)
+    ref, bound = R.gemm(R.dequantised(*w, cols, group), x, t)
+    R.check(product(w, x.cuda(), cols, group), ref, bound, "%s %dx%dx%d" % (dtype, rows, cols, n))
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+def test_strides_and_what_lies_behind_the_rows(dtype):
+    """Rows of X that start at odd elements between NaN, rows of codes and scales farther apart than they need, Y in a wider buffer."""
+    t, rows, cols, n, group = TYPES[dtype], 37, 205, 7, 64
+    rng = np.random.default_rng(5)
+    codes, scales, zeros = R.q4_weights(rng, rows, cols, group, True, t, pad=2)
+    wide = torch.full((rows, 9), float("nan"), dtype=t)
+    wz = torch.full((rows, 9), 200, dtype=torch.uint8)
+    wide[:, 2:6], wz[:, 2:6] = scales, zeros
+    buf = torch.full((n, cols + 11), float("nan"), dtype=t)
+    x = torch.from_numpy(rng.standard_normal((n, cols))).to(t)
+    buf[:, 3:3 + cols] = x
+    ref, bound = R.gemm(R.dequantised(codes, scales, zeros, cols, group), x, t)
+    ws, wzd, xd = wide.cuda(), wz.cuda(), buf.cuda()
+    y = torch.full((n, rows + 5), 77.0, dtype=t, device="cuda")
+    A = psk.Q4(codes.cuda(), ws[:, 2:6], wzd[:, 2:6], cols=cols, group=group)
+    psk.psk_gemm_q4(A, xd[:, 3:3 + cols], y[:, :rows])
+    R.check(y[:, :rows], ref, bound, "strided " + dtype)
+    assert bool((y[:, rows:] == 77).all())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+def test_special_values(dtype):
+    """An infinity or NaN spoils its own vector only, and only where the plain form is spoiled; zero points up to 255; a scale that is
+    infinite spoils its own row."""
+    t, rows, cols, n, group = TYPES[dtype], 33, 165, 9, 32
+    rng = np.random.default_rng(6)
+    codes, scales, zeros = R.q4_weights(rng, rows, cols, group, True, t)
+    zeros[3] = 255
+    scales[5, -1] = float("inf")
+    x = torch.from_numpy(rng.standard_normal((n, cols))).to(t)
+    x[1, 17], x[2, 40], x[4, 164] = float("inf"), float("nan"), float("-inf")
+    x[6] = 0
+    x[7, 3], x[7, 4] = torch.finfo(t).max, -torch.finfo(t).max
+    x[8] = torch.finfo(t).smallest_normal * 8
+    w = R.dequantised(codes, scales, zeros, cols, group)
+    ref, bound = R.gemm(w, x, t)
+    ref = ref.to(t).double() if dtype != "f32" else ref
+    over = ref.abs() > torch.finfo(t).max
+    ref[over] = torch.sign(ref[over]) * float("inf")
+    got = product((codes, scales, zeros), x.cuda(), cols, group)
+    # the row with the infinite scale is NaN or infinite as the signs of its last group fall: compared by itself
+    keep = [i for i in range(rows) if i != 5]
+    R.check(got[:, keep], ref[:, keep], bound[:, keep], "special " + dtype)
+    assert not bool(torch.isfinite(got[:6, 5]).any())
+
+
+def test_vectors_of_32_bits_keep_their_bits():
+    """Values whose low bits matter: sums that cancel to the last bits of the activations."""
+    rows, cols = 16, 256
+    codes = torch.zeros(rows, 128, dtype=torch.uint8)
+    codes[:, :] = 0x79                                     # even columns +1, odd ones -1
+    scales = torch.ones(rows, 2)
+    a = torch.from_numpy(np.random.default_rng(7).uniform(1, 2, 128)).float()
+    x = torch.empty(1, cols)
+    x[0, 0::2], x[0, 1::2] = torch.nextafter(a, a + 1), a
+    ref = (x[0, 0::2].double() - x[0, 1::2].double()).sum()
+    got = product((codes, scales, None), x.cuda(), cols, 128)[0, 0].item()
+    # parts of 8 bits: the first ones and the second ones cancel exactly pair by pair or leave steps of 2^-23, all sums are below
+    # 2^9 and multiples of 2^-23 where they are not exact: 2^-23 2^9 2^-23 per term at the very most
+    assert abs(got - float(ref)) <= 256 * 2.0 ** -14 * 2.0 ** -23 * 2 ** 9, (got, float(ref))
+
+
+def test_empty_products():
+    x = torch.zeros(3, 64, device="cuda", dtype=torch.float16)
+    codes, scales = torch.zeros(8, 32, dtype=torch.uint8, device="cuda"), torch.ones(8, 2, device="cuda", dtype=torch.float16)
+    A = psk.Q4(codes, scales, cols=64, group=32)
+    psk.psk_gemm_q4(A, x[:0], torch.empty(0, 8, device="cuda", dtype=torch.float16))
+    psk.psk_gemm_q4(psk.Q4(codes[:0], scales[:0], cols=64, group=32), x, torch.empty(3, 0, device="cuda", dtype=torch.float16))
+    y = torch.full((3, 8), 5.0, device="cuda", dtype=torch.float16)
+    psk.psk_gemm_q4(psk.Q4(codes, scales[:, :0], cols=0, group=32), x[:, :0], y)
+    assert bool((y == 0).all())
+
+
+def test_codes_beyond_four_gigabytes():
+    """A vocabulary's worth of rows whose offsets pass 32 bits; the first and last rows and some in between are checked."""
+    rows, cols, group, n = (1 << 20) + 37, 8192 + 64, 128, 3
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    codes = torch.randint(0, 256, (rows, (cols + 31) // 32 * 16), generator=g, device="cuda", dtype=torch.uint8)
+    scales = torch.rand(rows, (cols + group - 1) // group, generator=g, device="cuda").to(torch.bfloat16)
+    x = torch.randn(n, cols, generator=g, device="cuda").to(torch.bfloat16)
+    y = torch.zeros(n, rows, device="cuda", dtype=torch.bfloat16)
+    psk.psk_gemm_q4(psk.Q4(codes, scales, cols=cols, group=group), x, y)
+    torch.cuda.synchronize()
+    for r in (0, 12345, (1 << 31) // codes.shape[1], (1 << 32) // codes.shape[1] + 1, rows - 16):
+        part = slice(r, r + 16)
+        ref, bound = R.gemm(R.dequantised(codes[part].cpu(), scales[part].cpu(), None, cols, group), x.cpu(), torch.bfloat16)
+        R.check(y[:, part], ref, bound, "rows from %d" % r)
+
+
+@pytest.mark.parametrize("n", [1, 20])
+def test_other_stream_and_graph(n):
+    """On a stream that is not the current one, and captured: replays follow the activations, with eager work in between."""
+    rng = np.random.default_rng(8)
+    rows, cols, group = 200, 600, 128
+    w = R.q4_weights(rng, rows, cols, group, True, torch.float16)
+    A = psk.Q4(*dev(*w), cols=cols, group=group)
+    x = torch.zeros(n, cols, dtype=torch.float16, device="cuda")
+    y = torch.zeros(n, rows, dtype=torch.float16, device="cuda")
+    ws = psk.psk_gemm_q4_workspace(A, x)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    psk.psk_gemm_q4(A, x, y, ws=ws, stream=side)
+    psk.psk_gemm_q4(A, x, y, stream=side)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        psk.psk_gemm_q4(A, x, y, ws=ws)
+    for rep in range(4):
+        xh = torch.from_numpy(rng.standard_normal((n, cols))).half()
+        x.copy_(xh)
+        y.fill_(float("nan"))
+        ws.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        ref, bound = R.gemm(R.dequantised(*w, cols, group), xh, torch.float16)
+        R.check(y, ref, bound, "replay %d" % rep)
+        eager = torch.zeros_like(y)
+        psk.psk_gemm_q4(A, x, eager)
+        assert torch.equal(eager, y)
+
+
+def test_results_do_not_change_from_run_to_run():
+    rng = np.random.default_rng(9)
+    w = R.q4_weights(rng, 500, 3000, 64, True, torch.bfloat16)
+    x = torch.from_numpy(rng.standard_normal((11, 3000))).bfloat16().cuda()
+    first = product(w, x, 3000, 64).clone()
+    for _ in range(5):
+        assert torch.equal(first, product(w, x, 3000, 64))
+    # a vector's result does not depend on the ones beside it
+    assert torch.equal(first[4:5], product(w, x[4:5], 3000, 64))
