@@ -12,54 +12,70 @@ namespace {
 
 constexpr int KW = 8;
 
-template <int XT, int S, int GB, int NT>
+template <int XT> struct Vectors { typedef Plain16<XT> type; };
+template <> struct Vectors<F32> { typedef Parts32 type; };
+
+// Up to four vectors, 16 R rows.
+template <int XT, int S, int GB, int R>
+__global__ __launch_bounds__(64 * KW) void k_gemv_q4(WeightsQ4 A, int n, const void *X, int64_t ldx, void *Y, int64_t ldy)
+{
+    constexpr int T = XT == F16 ? F16 : BF16;
+    __shared__ float lds[KW * R * 64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, m = lane & 15;
+    const int row0 = blockIdx.x * (16 * R);
+    SpanQ4<T, R, GB, S> span;
+#pragma unroll
+    for (int r = 0; r < R; ++r) span.set(r, A, 0, min(row0 + 16 * r + m, A.rows - 1), quarter);
+    typename Vectors<XT>::type x;
+    x.set(X, min(m >> 2, n - 1) * ldx + 32 * (m & 3) + 8 * quarter);
+    float y[R];
+    few_product(span, x, A.cols, wave, KW, lane, y);
+    put_few<R>(lds, wave, lane, y);
+    __syncthreads();
+    for (int o = threadIdx.x; o < 64 * R; o += 64 * KW) {
+        const int r = o >> 6, v = o >> 4 & 3, i = o & 15;
+        if (v < n && row0 + 16 * r + i < A.rows) store_as<XT>(Y, v * ldy + row0 + 16 * r + i, get_sum<KW, R, 4>(lds, r, v, i));
+    }
+}
+
+// NT tiles of 16 vectors, 16 R rows.
+template <int XT, int S, int GB, int R, int NT>
 __global__ __launch_bounds__(64 * KW) void k_gemm_q4(WeightsQ4 A, int n, const void *X, int64_t ldx, void *Y, int64_t ldy)
 {
-    constexpr int T = XT == F16 ? F16 : BF16, PER = XT == F32 ? 5 : 16;
-    __shared__ float lds[KW * NT * 256];
+    constexpr int T = XT == F16 ? F16 : BF16;
+    __shared__ float lds[KW * R * NT * 256];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, m = lane & 15;
-    const int row0 = blockIdx.x * 16, t0 = blockIdx.y * (PER * NT);
-    SpanQ4<T, 1, GB, S> span;
-    span.set(0, A, 0, min(row0 + m, A.rows - 1), quarter);
-    v4f acc[1][NT];
+    const int row0 = blockIdx.x * (16 * R), t0 = blockIdx.y * (16 * NT);
+    SpanQ4<T, R, GB, S> span;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) acc[0][t] = v4f{0, 0, 0, 0};
-    if constexpr (XT == F32) {
-        Rows32<NT> x;
-        x.cols = A.cols;
-        x.part = m % 3;
+    for (int r = 0; r < R; ++r) span.set(r, A, 0, min(row0 + 16 * r + m, A.rows - 1), quarter);
+    typename Vectors<XT>::type x[NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) x.p[t] = static_cast<const float *>(X) + (int64_t)min(t0 + PER * t + m / 3, n - 1) * ldx;
-        span_product<SpanQ4<T, 1, GB, S>, NT>(span, x, A.cols, wave, KW, quarter, acc);
-    } else {
-        Rows16<NT> x;
-        x.cols = A.cols;
+    for (int t = 0; t < NT; ++t) x[t].set(X, min(t0 + 16 * t + m, n - 1) * ldx + 8 * quarter);
+    v4f acc[R][NT], flat[R * NT];
+    tile_product<SpanQ4<T, R, GB, S>, NT>(span, x, A.cols, wave, KW, lane, acc);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) x.p[t] = static_cast<const unsigned short *>(X) + (int64_t)min(t0 + PER * t + m, n - 1) * ldx;
-        span_product<SpanQ4<T, 1, GB, S>, NT>(span, x, A.cols, wave, KW, quarter, acc);
-    }
-    put_sums<NT>(lds, wave, lane, acc[0]);
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) flat[r * NT + t] = acc[r][t];
+    put_sums<R * NT>(lds, wave, lane, flat);
     __syncthreads();
-    for (int o = threadIdx.x; o < NT * PER * 16; o += 64 * KW) {
-        const int tile = o / (PER * 16), v = o / 16 % PER, i = o % 16;
-        if (t0 + tile * PER + v >= n || row0 + i >= A.rows) continue;
-        float y;
-        if constexpr (XT == F32)
-            y = get_sum<KW, NT>(lds, tile, 3 * v, i) + (get_sum<KW, NT>(lds, tile, 3 * v + 1, i) + get_sum<KW, NT>(lds, tile, 3 * v + 2, i));
-        else
-            y = get_sum<KW, NT>(lds, tile, v, i);
-        store_as<XT>(Y, (int64_t)(t0 + tile * PER + v) * ldy + row0 + i, y);
+    for (int o = threadIdx.x; o < R * NT * 256; o += 64 * KW) {
+        const int k = o >> 8, v = t0 + 16 * (k % NT) + (o >> 4 & 15), i = row0 + 16 * (k / NT) + (o & 15);
+        if (v < n && i < A.rows) store_as<XT>(Y, v * ldy + i, get_sum<KW, R * NT, 16>(lds, k, o >> 4 & 15, o & 15));
     }
 }
 
 template <int XT, int S, int GB>
 void by_vectors(const WeightsQ4 &A, int n, const void *X, int64_t ldx, void *Y, int64_t ldy, hipStream_t s)
 {
-    constexpr int PER = XT == F32 ? 5 : 16;
-    const int tiles = (n + PER - 1) / PER, rows = (A.rows + 15) / 16;
-    if (tiles <= 1) PSK_LAUNCH((k_gemm_q4<XT, S, GB, 1>), dim3(rows, 1), dim3(64 * KW), 0, s, A, n, X, ldx, Y, ldy);
-    else if (tiles == 2) PSK_LAUNCH((k_gemm_q4<XT, S, GB, 2>), dim3(rows, 1), dim3(64 * KW), 0, s, A, n, X, ldx, Y, ldy);
-    else PSK_LAUNCH((k_gemm_q4<XT, S, GB, 4>), dim3(rows, (tiles + 3) / 4), dim3(64 * KW), 0, s, A, n, X, ldx, Y, ldy);
+    const int rows = (A.rows + 15) / 16;
+    if (n <= 4) {
+        if (rows >= 2048) PSK_LAUNCH((k_gemv_q4<XT, S, GB, 2>), dim3((rows + 1) / 2), dim3(64 * KW), 0, s, A, n, X, ldx, Y, ldy);
+        else PSK_LAUNCH((k_gemv_q4<XT, S, GB, 1>), dim3(rows), dim3(64 * KW), 0, s, A, n, X, ldx, Y, ldy);
+    } else if (n <= 16) PSK_LAUNCH((k_gemm_q4<XT, S, GB, 1, 1>), dim3(rows, 1), dim3(64 * KW), 0, s, A, n, X, ldx, Y, ldy);
+    else if (n <= 32) PSK_LAUNCH((k_gemm_q4<XT, S, GB, 2, 2>), dim3((rows + 1) / 2, 1), dim3(64 * KW), 0, s, A, n, X, ldx, Y, ldy);
+    else PSK_LAUNCH((k_gemm_q4<XT, S, GB, 2, 4>), dim3((rows + 1) / 2, (n + 63) / 64), dim3(64 * KW), 0, s, A, n, X, ldx, Y, ldy);
 }
 template <int XT, int S>
 void by_group(const WeightsQ4 &A, int n, const void *X, int64_t ldx, void *Y, int64_t ldy, hipStream_t s)

@@ -4,14 +4,14 @@
 //
 // G is a sparse matrix with top_k entries per row (crd, vals); position p = t * top_k + slot.  Bound by reading the matrices of
 // the experts that occur, each once, so the unit of work is (expert that occurs, 16 rows of its matrices) with all positions of
-// that expert: they are the vectors of one set of matrix instructions.  Two launches:
+// that expert: they are the vectors of one set of matrix instructions.  Three launches:
 //   k_moe_up    h[p] = act(W1_e x_t) * (W3_e x_t)
-//   k_moe_down  P[p] = W2_e h[p]; the workgroup that is the last of its 16 rows adds up Y from P, in the order of the slots
+//   k_moe_down  P[p] = W2_e h[p]
+//   k_moe_join  Y(t,:) = sum of G(t,e) P[p] in the order of the slots
 // Every workgroup finds its expert and that one's positions itself from crd (at most kMoePositions of them).
 //
-// h goes to memory as two 16-bit numbers, the nearest one and the nearest one to what is left: rounding to one of them would cost as
-// much accuracy as rounding Y does, and the second one costs a matrix instruction where the matrix cores wait for memory.
-// f16 has too small a range for that: there h is scaled by 2^-8 (|h| up to 2^24 is finite) and what is left by 2^11.
+// h goes to memory as two 16-bit numbers (Halves): rounding to one of them would cost as much accuracy as rounding Y does, and the
+// second one costs a matrix instruction where the matrix cores wait for memory.
 #include "psk_internal.h"
 #include "psk_mfma.h"
 #include "../../include/psk.h"
@@ -62,22 +62,6 @@ __device__ __forceinline__ Found find(FindSpace &f, int positions, int experts, 
     return r;
 }
 
-// ---- h
-template <int T> struct Half2 {                              // f16
-    static constexpr float scale = 0x1p-8f, rest = 0x1p11f;
-};
-template <> struct Half2<BF16> {
-    static constexpr float scale = 1.0f, rest = 1.0f;
-};
-template <int T>
-__device__ __forceinline__ void split(float h, unsigned short &a, unsigned short &b)
-{
-    const float v = h * Half2<T>::scale;
-    a = narrow<T>(v);
-    const float w = widen<T>(a), r = (v - w) * Half2<T>::rest;
-    b = __builtin_isfinite(w) ? narrow<T>(r) : (unsigned short)0;
-}
-
 template <int ACT>
 __device__ __forceinline__ float activate(float v)
 {
@@ -86,175 +70,162 @@ __device__ __forceinline__ float activate(float v)
 }
 
 struct UpArgs {
-    int n, experts, top_k, dim, inter, counters;
+    int n, experts, top_k, dim, inter;
     const int *crd;
     const unsigned short *X;
     int64_t ldx;
-    unsigned short *h, *rest;
-    int64_t ldh;
-    int *done;
+    unsigned short *h;
+    int64_t ldh, rest;                                       // rest: from h to the second parts
 };
 struct DownArgs {
     int n, experts, top_k, dim, inter;
     const int *crd;
-    const float *vals;
-    const unsigned short *h, *rest;
-    int64_t ldh;
+    const unsigned short *h;
+    int64_t ldh, rest;
     float *P;
-    int *done;
-    void *Y;
-    int64_t ldy;
 };
 
-// NT tiles of 16 positions, 16 rows of W1 and of W3.  HT: type of the parts of h.
+// 16 rows of W1 and of W3 with `count` positions: up to four (NT = 0) or NT tiles of 16.  HT: type of the parts of h.
 template <class SPAN, int HT, int ACT, int NT, class W>
-__device__ __forceinline__ void up_tiles(const UpArgs &a, const W &w1, const W &w3, int expert, const unsigned short *list, int count, int row0, float *lds)
+__device__ __forceinline__ void up_rows(const UpArgs &a, const W &w1, const W &w3, int expert, const unsigned short *list, int count, int row0, float *lds)
 {
+    constexpr int V = NT ? 16 : 4, TILES = NT ? NT : 1;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, m = lane & 15;
     SPAN span;
     span.set(0, w1, expert, min(row0 + m, a.inter - 1), quarter);
     span.set(1, w3, expert, min(row0 + m, a.inter - 1), quarter);
-    Rows16<NT> x;
-    x.cols = a.dim;
-    v4f acc[2][NT];
+    Plain16<SPAN::T> x[TILES];
+    if constexpr (NT == 0) {
+        x[0].set(a.X, list[min(m >> 2, count - 1)] / a.top_k * a.ldx + 32 * (m & 3) + 8 * quarter);
+        float y[2];
+        few_product(span, x[0], a.dim, wave, KW, lane, y);
+        put_few<2>(lds, wave, lane, y);
+    } else {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        x.p[t] = a.X + (int64_t)(list[min(16 * t + m, count - 1)] / a.top_k) * a.ldx;
-        acc[0][t] = acc[1][t] = v4f{0, 0, 0, 0};
+        for (int t = 0; t < NT; ++t) x[t].set(a.X, list[min(16 * t + m, count - 1)] / a.top_k * a.ldx + 8 * quarter);
+        v4f acc[2][TILES], flat[2 * TILES];
+        tile_product<SPAN, TILES>(span, x, a.dim, wave, KW, lane, acc);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) { flat[t] = acc[0][t]; flat[NT + t] = acc[1][t]; }
+        put_sums<2 * TILES>(lds, wave, lane, flat);
     }
-    span_product<SPAN, NT>(span, x, a.dim, wave, KW, quarter, acc);
-    v4f flat[2 * NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) { flat[t] = acc[0][t]; flat[NT + t] = acc[1][t]; }
-    put_sums<2 * NT>(lds, wave, lane, flat);
     __syncthreads();
-    for (int o = threadIdx.x; o < NT * 256; o += THREADS) {
-        const int t = o >> 8, v = o >> 4 & 15, i = o & 15;
-        if (16 * t + v >= count || row0 + i >= a.inter) continue;
-        const float h = activate<ACT>(get_sum<KW, 2 * NT>(lds, t, v, i)) * get_sum<KW, 2 * NT>(lds, NT + t, v, i);
+    for (int o = threadIdx.x; o < TILES * V * 16; o += THREADS) {
+        const int t = o / (V * 16), v = o / 16 % V, i = o & 15;
+        if (V * t + v >= count || row0 + i >= a.inter) continue;
+        const float h = activate<ACT>(get_sum<KW, 2 * TILES, V>(lds, t, v, i)) * get_sum<KW, 2 * TILES, V>(lds, TILES + t, v, i);
         unsigned short p, q;
-        split<HT>(h, p, q);
-        const int64_t at = list[16 * t + v] * a.ldh + row0 + i;
+        Halves<HT>::split(h, p, q);
+        const int64_t at = list[V * t + v] * a.ldh + row0 + i;
         a.h[at] = p;
-        a.rest[at] = q;
+        a.h[at + a.rest] = q;
     }
 }
 
-template <class SPAN, int HT, int ACT, class W>
+template <class SPAN, int HT, int ACT, int MOST, class W>
 __global__ __launch_bounds__(THREADS) void k_moe_up(UpArgs a, W w1, W w3)
 {
     __shared__ FindSpace f;
-    __shared__ float lds[KW * 8 * 256];
-    if (blockIdx.x == 0 && blockIdx.y == 0)
-        for (int i = threadIdx.x; i < a.counters; i += THREADS) a.done[i] = 0;
+    __shared__ float lds[KW * (MOST ? MOST * 512 : 128)];
     const Found g = find(f, a.n * a.top_k, a.experts, a.crd, blockIdx.y);
     if (g.expert < 0) return;
     const int row0 = blockIdx.x * 16;
-    for (int p0 = 0; p0 < g.count; p0 += 64) {
+    for (int p0 = 0; p0 < g.count; p0 += MOST ? 16 * MOST : 4) {
         const int c = g.count - p0;
-        if (c <= 16) up_tiles<SPAN, HT, ACT, 1>(a, w1, w3, g.expert, f.list + p0, c, row0, lds);
-        else if (c <= 32) up_tiles<SPAN, HT, ACT, 2>(a, w1, w3, g.expert, f.list + p0, c, row0, lds);
-        else up_tiles<SPAN, HT, ACT, 4>(a, w1, w3, g.expert, f.list + p0, c, row0, lds);
+        if (!MOST || c <= 4) up_rows<SPAN, HT, ACT, 0>(a, w1, w3, g.expert, f.list + p0, c, row0, lds);
+        else if (MOST == 1 || c <= 16) up_rows<SPAN, HT, ACT, 1>(a, w1, w3, g.expert, f.list + p0, c, row0, lds);
+        else if constexpr (MOST > 1) up_rows<SPAN, HT, ACT, MOST>(a, w1, w3, g.expert, f.list + p0, c, row0, lds);
         __syncthreads();
     }
 }
 
-// NT tiles of 16 positions, 16 rows of W2; both parts of h are vectors.
+// 16 rows of W2 likewise, from both parts of h.
 template <class SPAN, int NT, class W>
-__device__ __forceinline__ void down_tiles(const DownArgs &a, const W &w2, int expert, const unsigned short *list, int count, int row0, float *lds)
+__device__ __forceinline__ void down_rows(const DownArgs &a, const W &w2, int expert, const unsigned short *list, int count, int row0, float *lds)
 {
-    constexpr int T = SPAN::T;
+    constexpr int V = NT ? 16 : 4, TILES = NT ? NT : 1;
+    typedef Halves<SPAN::T> H;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, m = lane & 15;
     SPAN span;
     span.set(0, w2, expert, min(row0 + m, a.dim - 1), quarter);
-    Rows16<2 * NT> x;
-    x.cols = a.inter;
-    v4f acc[1][2 * NT];
+    H x[TILES];
+    if constexpr (NT == 0) {
+        x[0].set(a.h, list[min(m >> 2, count - 1)] * a.ldh + 32 * (m & 3) + 8 * quarter, a.rest);
+        float y[1];
+        few_product(span, x[0], a.inter, wave, KW, lane, y);
+        put_few<1>(lds, wave, lane, y);
+    } else {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int64_t at = list[min(16 * t + m, count - 1)] * a.ldh;
-        x.p[t] = a.h + at;
-        x.p[NT + t] = a.rest + at;
-        acc[0][t] = acc[0][NT + t] = v4f{0, 0, 0, 0};
+        for (int t = 0; t < NT; ++t) x[t].set(a.h, list[min(16 * t + m, count - 1)] * a.ldh + 8 * quarter, a.rest);
+        v4f acc[1][TILES];
+        tile_product<SPAN, TILES>(span, x, a.inter, wave, KW, lane, acc);
+        put_sums<TILES>(lds, wave, lane, acc[0]);
     }
-    span_product<SPAN, 2 * NT>(span, x, a.inter, wave, KW, quarter, acc);
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) acc[0][t][i] = fmaf(acc[0][NT + t][i], 1.0f / Half2<T>::rest, acc[0][t][i]) * (1.0f / Half2<T>::scale);
-    v4f flat[NT];
-#pragma unroll
-    for (int t = 0; t < NT; ++t) flat[t] = acc[0][t];
-    put_sums<NT>(lds, wave, lane, flat);
     __syncthreads();
-    for (int o = threadIdx.x; o < NT * 256; o += THREADS) {
-        const int t = o >> 8, v = o >> 4 & 15, i = o & 15;
-        if (16 * t + v >= count || row0 + i >= a.dim) continue;
-        // read by a workgroup that may run on another die: past this die's L2
-        __hip_atomic_store(a.P + (int64_t)list[16 * t + v] * a.dim + row0 + i, get_sum<KW, NT>(lds, t, v, i), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int o = threadIdx.x; o < TILES * V * 16; o += THREADS) {
+        const int t = o / (V * 16), v = o / 16 % V, i = o & 15;
+        if (V * t + v >= count || row0 + i >= a.dim) continue;
+        a.P[(int64_t)list[V * t + v] * a.dim + row0 + i] = get_sum<KW, TILES, V>(lds, t, v, i) * (1.0f / H::scale);
     }
 }
 
-template <class SPAN, int YT, class W>
+template <class SPAN, int MOST, class W>
 __global__ __launch_bounds__(THREADS) void k_moe_down(DownArgs a, W w2)
 {
     __shared__ FindSpace f;
-    __shared__ float lds[KW * 4 * 256];
-    __shared__ int last;
+    __shared__ float lds[KW * (MOST ? MOST * 256 : 64)];
     const Found g = find(f, a.n * a.top_k, a.experts, a.crd, blockIdx.y);
-    if (g.expert < 0 && !(g.active == 0 && blockIdx.y == 0)) return;
+    if (g.expert < 0) return;
     const int row0 = blockIdx.x * 16;
-    for (int p0 = 0; p0 < g.count; p0 += 64) {
+    for (int p0 = 0; p0 < g.count; p0 += MOST ? 16 * MOST : 4) {
         const int c = g.count - p0;
-        if (c <= 16) down_tiles<SPAN, 1>(a, w2, g.expert, f.list + p0, c, row0, lds);
-        else if (c <= 32) down_tiles<SPAN, 2>(a, w2, g.expert, f.list + p0, c, row0, lds);
-        else down_tiles<SPAN, 4>(a, w2, g.expert, f.list + p0, c, row0, lds);
+        if (!MOST || c <= 4) down_rows<SPAN, 0>(a, w2, g.expert, f.list + p0, c, row0, lds);
+        else if (MOST == 1 || c <= 16) down_rows<SPAN, 1>(a, w2, g.expert, f.list + p0, c, row0, lds);
+        else if constexpr (MOST > 1) down_rows<SPAN, MOST>(a, w2, g.expert, f.list + p0, c, row0, lds);
         __syncthreads();
-    }
-    if (threadIdx.x == 0)
-        last = g.active == 0 || __hip_atomic_fetch_add(a.done + blockIdx.x, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == g.active - 1;
-    __syncthreads();
-    if (!last) return;
-    for (int o = threadIdx.x; o < a.n * 16; o += THREADS) {
-        const int t = o >> 4, i = o & 15;
-        if (row0 + i >= a.dim) continue;
-        float y = 0;
-        for (int s = 0; s < a.top_k; ++s) {
-            const int p = t * a.top_k + s;
-            if ((unsigned)a.crd[p] >= (unsigned)a.experts) continue;
-            y = fmaf(a.vals[p], __hip_atomic_load(a.P + (int64_t)p * a.dim + row0 + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT), y);
-        }
-        store_as<YT>(a.Y, t * a.ldy + row0 + i, y);
     }
 }
 
+// A lane per element of Y.
+template <int YT>
+__global__ __launch_bounds__(256) void k_moe_join(int dim, int experts, int top_k, const int *__restrict__ crd, const float *__restrict__ vals,
+                                                  const float *__restrict__ P, void *Y, int64_t ldy)
+{
+    const int i = blockIdx.x * 256 + threadIdx.x, t = blockIdx.y;
+    if (i >= dim) return;
+    float y = 0;
+    for (int s = 0; s < top_k; ++s) {
+        const int p = t * top_k + s;
+        if ((unsigned)crd[p] < (unsigned)experts) y = fmaf(vals[p], P[(int64_t)p * dim + i], y);
+    }
+    store_as<YT>(Y, t * ldy + i, y);
+}
+
 struct Space {
-    unsigned short *h, *rest;
+    unsigned short *h;
     float *P;
-    int *done;
-    int64_t ldh;
+    int64_t ldh, rest;
     size_t bytes;
 };
 Space carve_moe(void *base, int64_t positions, int64_t dim, int64_t inter)
 {
     Space w;
     w.ldh = (inter + 7) / 8 * 8;
-    const size_t a = align256((size_t)positions * w.ldh * 2), b = align256((size_t)positions * dim * 4), c = align256((size_t)((dim + 15) / 16) * 4);
+    const size_t a = align256((size_t)positions * w.ldh * 2), b = align256((size_t)positions * dim * 4);
     char *p = static_cast<char *>(base);
     w.h = reinterpret_cast<unsigned short *>(p);
-    w.rest = reinterpret_cast<unsigned short *>(p + a);
+    w.rest = (int64_t)(a / 2);
     w.P = reinterpret_cast<float *>(p + 2 * a);
-    w.done = reinterpret_cast<int *>(p + 2 * a + b);
-    w.bytes = 2 * a + b + c;
+    w.bytes = 2 * a + b;
     return w;
 }
 
 // tokens of one pair of launches
 int tokens_at_once(int64_t n, int top_k) { return (int)(n < kMoePositions / top_k ? n : kMoePositions / top_k); }
 
-// UP, DOWN: the spans of the two steps.  HT: type of the parts of h, which are the operands of the second step.
-template <class UP, class DOWN, int YT, class W>
-hipError_t launch(const MoeCall &c, const W &w1, const W &w3, const W &w2, hipStream_t s)
+// UP, DOWN: the spans of the two steps.  MOST: tiles of positions at once, 0: four positions.
+template <class UP, class DOWN, int YT, int MOST, class W>
+hipError_t launch_most(const MoeCall &c, const W &w1, const W &w3, const W &w2, hipStream_t s)
 {
     const int at_once = tokens_at_once(c.n, c.top_k);
     const Space w = carve_moe(c.workspace, (int64_t)at_once * c.top_k, c.dim, c.inter);
@@ -262,16 +233,22 @@ hipError_t launch(const MoeCall &c, const W &w1, const W &w3, const W &w2, hipSt
         const int n = (int)(c.n - t0 < at_once ? c.n - t0 : at_once);
         const int slots = n * c.top_k < c.experts ? n * c.top_k : c.experts;
         const int *crd = c.crd + t0 * c.top_k;
-        const UpArgs u = {n, c.experts, c.top_k, c.dim, c.inter, (c.dim + 15) / 16, crd, static_cast<const unsigned short *>(c.X) + t0 * c.ldx, c.ldx,
-                          w.h, w.rest, w.ldh, w.done};
-        const DownArgs d = {n, c.experts, c.top_k, c.dim, c.inter, crd, c.vals + t0 * c.top_k, w.h, w.rest, w.ldh, w.P, w.done,
-                            static_cast<unsigned short *>(c.Y) + t0 * c.ldy, c.ldy};
+        const UpArgs u = {n, c.experts, c.top_k, c.dim, c.inter, crd, static_cast<const unsigned short *>(c.X) + t0 * c.ldx, c.ldx, w.h, w.ldh, w.rest};
+        const DownArgs d = {n, c.experts, c.top_k, c.dim, c.inter, crd, w.h, w.ldh, w.rest, w.P};
         const dim3 up((c.inter + 15) / 16, slots), down((c.dim + 15) / 16, slots);
-        if (c.act == PSK_ACT_SILU) PSK_LAUNCH((k_moe_up<UP, DOWN::T, PSK_ACT_SILU, W>), up, dim3(THREADS), 0, s, u, w1, w3);
-        else PSK_LAUNCH((k_moe_up<UP, DOWN::T, PSK_ACT_GELU, W>), up, dim3(THREADS), 0, s, u, w1, w3);
-        PSK_LAUNCH((k_moe_down<DOWN, YT, W>), down, dim3(THREADS), 0, s, d, w2);
+        if (c.act == PSK_ACT_SILU) PSK_LAUNCH((k_moe_up<UP, DOWN::T, PSK_ACT_SILU, MOST, W>), up, dim3(THREADS), 0, s, u, w1, w3);
+        else PSK_LAUNCH((k_moe_up<UP, DOWN::T, PSK_ACT_GELU, MOST, W>), up, dim3(THREADS), 0, s, u, w1, w3);
+        PSK_LAUNCH((k_moe_down<DOWN, MOST, W>), down, dim3(THREADS), 0, s, d, w2);
+        PSK_LAUNCH(k_moe_join<YT>, dim3((c.dim + 255) / 256, n), dim3(256), 0, s, c.dim, c.experts, c.top_k, crd, c.vals + t0 * c.top_k, w.P,
+                   static_cast<unsigned short *>(c.Y) + t0 * c.ldy, c.ldy);
     }
     return take_launch_status();
+}
+
+template <class UP, class DOWN, int YT, class W>
+hipError_t launch(const MoeCall &c, const W &w1, const W &w3, const W &w2, hipStream_t s)
+{
+    return c.n <= 4 ? launch_most<UP, DOWN, YT, 0>(c, w1, w3, w2, s) : launch_most<UP, DOWN, YT, 2>(c, w1, w3, w2, s);
 }
 
 template <int T, int S, int G1>

@@ -62,12 +62,12 @@ __device__ __forceinline__ bool before(double ka, int ia, double kb, int ib)
     return ia < ib;
 }
 
-// A wave per token; lane l has experts l, l + 64, ...
-template <int SCORE>
+// A wave per token; lane l has experts l, l + 64, ..., PER of them.
+template <int SCORE, int PER>
 __global__ __launch_bounds__(64) void k_route_choose(int experts, int top_k, int normalise, float factor, const double *logits, const float *bias,
                                                       int *crd, float *vals)
 {
-    constexpr int PER = PSK_MOE_MAX_EXPERTS / WAVE, NONE = 0x7fffffff;
+    constexpr int NONE = 0x7fffffff;
     const int lane = threadIdx.x;
     const int64_t t = blockIdx.x;
     const double *row = logits + t * experts;
@@ -136,6 +136,17 @@ __global__ __launch_bounds__(64) void k_route_choose(int experts, int top_k, int
     }
 }
 
+template <int SCORE>
+void choose(int n, int experts, int top_k, int normalise, float factor, const double *logits, const float *bias, int *crd, float *vals, hipStream_t s)
+{
+#define PSK_CHOOSE(PER) PSK_LAUNCH((k_route_choose<SCORE, PER>), dim3(n), dim3(64), 0, s, experts, top_k, normalise, factor, logits, bias, crd, vals)
+    if (experts <= 64) PSK_CHOOSE(1);
+    else if (experts <= 128) PSK_CHOOSE(2);
+    else if (experts <= 256) PSK_CHOOSE(4);
+    else PSK_CHOOSE(PSK_MOE_MAX_EXPERTS / WAVE);
+#undef PSK_CHOOSE
+}
+
 template <int XT, int WT>
 void logits_of(int n, int dim, int experts, const void *X, int64_t ldx, const void *W, int64_t ldw, double *logits, hipStream_t s)
 {
@@ -153,10 +164,8 @@ hipError_t launch_moe_route(int n, int dim, int experts, int top_k, int score, i
     else if (type == F16) logits_of<F16, F32>(n, dim, experts, X, ldx, W, ldw, logits, s);
     else if (wtype == BF16) logits_of<BF16, BF16>(n, dim, experts, X, ldx, W, ldw, logits, s);
     else logits_of<BF16, F32>(n, dim, experts, X, ldx, W, ldw, logits, s);
-    if (score == PSK_SCORE_SOFTMAX)
-        PSK_LAUNCH(k_route_choose<PSK_SCORE_SOFTMAX>, dim3(n), dim3(64), 0, s, experts, top_k, normalise, factor, logits, bias, crd, vals);
-    else
-        PSK_LAUNCH(k_route_choose<PSK_SCORE_SIGMOID>, dim3(n), dim3(64), 0, s, experts, top_k, normalise, factor, logits, bias, crd, vals);
+    if (score == PSK_SCORE_SOFTMAX) choose<PSK_SCORE_SOFTMAX>(n, experts, top_k, normalise, factor, logits, bias, crd, vals, s);
+    else choose<PSK_SCORE_SIGMOID>(n, experts, top_k, normalise, factor, logits, bias, crd, vals, s);
     return take_launch_status();
 }
 

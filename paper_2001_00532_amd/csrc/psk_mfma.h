@@ -8,6 +8,7 @@
 // Sums are held in 32 bits.
 #pragma once
 #include "psk_dev.h"
+#include <type_traits>
 
 namespace psk {
 
@@ -61,46 +62,104 @@ __device__ __forceinline__ v4u load8(const unsigned short *p, int k, int cols)
 }
 
 // ---- vectors
-// Sixteen vectors of 16 bits per tile, one row pointer per lane and tile.
-template <int NT>
-struct Rows16 {
-    const unsigned short *p[NT];
-    int cols;
-    __device__ __forceinline__ v4u load(int t, int k) const { return load8(p[t], k, cols); }
+// Few vectors, up to four: row 4v + j of the first operand is block j (32 columns) of four blocks of vector v, so one load per lane
+// brings four blocks.  The instruction that multiplies it by block j of the weights leaves the product of the two in element j
+// of the lanes of quarter v (and products of blocks that do not belong together in the other elements).
+// Tiles: row m of an operand is vector m of the tile, four loads for four blocks.
+// A vector may have several parts whose products add up; P of them, the last one with a factor of its own if LO (see Halves).
+template <int T>
+struct Plain16 {                                           // 16 bits
+    static constexpr int P = 1;
+    static constexpr bool LO = false;
+    struct Raw { v4u v; };
+    const unsigned short *p;
+    __device__ __forceinline__ void set(const void *X, int64_t at) { p = static_cast<const unsigned short *>(X) + at; }
+    template <bool TAIL>
+    __device__ __forceinline__ void load(Raw &r, int k, int left) const { r.v = TAIL ? load8(p, k, left) : *reinterpret_cast<const v4u_u *>(p + k); }
+    static __device__ __forceinline__ void operands(const Raw &r, v4u (&x)[P]) { x[0] = r.v; }
 };
-
-// Vectors of 32 bits as three rows of bf16 each: v = a + b + c with 8 significant bits in each, cut off and not rounded, so the
-// sum is exact and a value near the largest does not become infinite.  Rows 3v, 3v + 1, 3v + 2 of a tile are the parts of
-// vector v (5 vectors per tile); their sums are added up at the end.  Infinity and NaN stand in the first part alone.
-template <int NT>
-struct Rows32 {
-    const float *p[NT];
-    int cols, part;
-    __device__ __forceinline__ v4u load(int t, int k) const
+// 32 bits as three parts of bf16: v = a + b + c with 8 significant bits in each, cut off and not rounded, so the sum is exact and a
+// value near the largest does not become infinite.  Infinity and NaN stand in the first part alone.
+struct Parts32 {
+    static constexpr int P = 3;
+    static constexpr bool LO = false;
+    struct Raw { v4f_e a, b; };
+    const float *p;
+    __device__ __forceinline__ void set(const void *X, int64_t at) { p = static_cast<const float *>(X) + at; }
+    template <bool TAIL>
+    __device__ __forceinline__ void load(Raw &r, int k, int left) const
     {
-        float v[8];
-        if (k + 8 <= cols) {
-            const v4f_e a = *reinterpret_cast<const v4f_e *>(p[t] + k), b = *reinterpret_cast<const v4f_e *>(p[t] + k + 4);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+        if (!TAIL || k + 8 <= left) {
+            r.a = *reinterpret_cast<const v4f_e *>(p + k);
+            r.b = *reinterpret_cast<const v4f_e *>(p + k + 4);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = k + i < cols ? p[t][k + i] : 0.0f;
+            for (int i = 0; i < 4; ++i) {
+                r.a[i] = k + i < left ? p[k + i] : 0.0f;
+                r.b[i] = k + 4 + i < left ? p[k + 4 + i] : 0.0f;
+            }
         }
-        v4u r;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = part_of(v[2 * i]) >> 16 | (part_of(v[2 * i + 1]) & 0xffff0000u);
-        return r;
     }
-    __device__ __forceinline__ unsigned part_of(float v) const
+    static __device__ __forceinline__ void operands(const Raw &r, v4u (&x)[P])
     {
-        const unsigned u = __builtin_bit_cast(unsigned, v);
-        if ((u & 0x7f800000u) == 0x7f800000u) return part ? 0u : (u & 0x7fffffu ? 0x7fc00000u : u);
-        const float a = __builtin_bit_cast(float, u & 0xffff0000u), r = v - a;
-        const float b = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, r) & 0xffff0000u);
-        return __builtin_bit_cast(unsigned, part == 0 ? a : (part == 1 ? b : r - b));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            unsigned part[2][P];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const float v = __builtin_canonicalizef(i < 2 ? r.a[2 * i + e] : r.b[2 * i - 4 + e]);      // a NaN keeps its first bit
+                const float a = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, v) & 0xffff0000u), d = v - a;
+                const float rest = __builtin_isfinite(v) ? d : 0.0f;
+                const float b = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, rest) & 0xffff0000u), c = rest - b;
+                part[e][0] = __builtin_bit_cast(unsigned, a);
+                part[e][1] = __builtin_bit_cast(unsigned, b);
+                part[e][2] = __builtin_bit_cast(unsigned, c);
+            }
+#pragma unroll
+            for (int q = 0; q < P; ++q) x[q][i] = __builtin_amdgcn_perm(part[1][q], part[0][q], 0x07060302u);
+        }
     }
 };
+// Two 16-bit numbers per value, the nearest one and the nearest one to what is left, in two arrays.  f16 has too small a range for
+// that: the value is scaled by 2^-8 (up to 2^24 it is finite) and what is left by 2^11, and the second sum is kept apart.
+template <int T>
+struct Halves {
+    static constexpr int P = 2;
+    static constexpr bool LO = T == F16;
+    static constexpr float scale = T == F16 ? 0x1p-8f : 1.0f, rest = T == F16 ? 0x1p11f : 1.0f;
+    struct Raw { v4u v[2]; };
+    const unsigned short *p;
+    int64_t apart;                                         // from the first array to the second one
+    __device__ __forceinline__ void set(const unsigned short *h, int64_t at, int64_t to_rest) { p = h + at; apart = to_rest; }
+    template <bool TAIL>
+    __device__ __forceinline__ void load(Raw &r, int k, int left) const
+    {
+        r.v[0] = TAIL ? load8(p, k, left) : *reinterpret_cast<const v4u_u *>(p + k);
+        r.v[1] = TAIL ? load8(p + apart, k, left) : *reinterpret_cast<const v4u_u *>(p + apart + k);
+    }
+    static __device__ __forceinline__ void operands(const Raw &r, v4u (&x)[P]) { x[0] = r.v[0]; x[1] = r.v[1]; }
+    static __device__ __forceinline__ void split(float h, unsigned short &a, unsigned short &b)
+    {
+        const float v = h * scale;
+        a = narrow<T>(v);
+        const float w = widen<T>(a), r = (v - w) * rest;
+        b = __builtin_isfinite(w) ? narrow<T>(r) : (unsigned short)0;
+    }
+};
+// Sum of products of the parts with weights w.
+template <int T, class X>
+__device__ __forceinline__ v4f product(const v4u (&x)[X::P], v4u w, v4f c)
+{
+#pragma unroll
+    for (int q = 0; q < X::P; ++q)
+        if (!(X::LO && q == X::P - 1)) c = mfma16<T>(x[q], w, c);
+    if constexpr (X::LO) {
+        const v4f d = mfma16<T>(x[X::P - 1], w, v4f{0, 0, 0, 0});
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[e] = fmaf(d[e], 1.0f / X::rest, c[e]);
+    }
+    return c;
+}
 
 // ---- weights of 16 bits: count matrices of rows x cols
 struct Weights16 {
@@ -110,34 +169,57 @@ struct Weights16 {
 };
 template <int T_, int R_>
 struct Span16 {
-    static constexpr int T = T_, R = R_, CH = 64;         // columns of a chunk: two pieces of 64 bytes per row
+    static constexpr int T = T_, R = R_, CH = 128, PIECES = 1;        // columns of a chunk: 256 bytes per row; pieces of 128 columns
     const unsigned short *p[R];
-    int cols;
-    struct Regs { v4u w[R][2]; };
+    int left;                                              // columns from the lane's first one on
+    struct Regs { v4u w[R][4]; };
+    struct Few { v4f d[R][4]; };
     __device__ __forceinline__ void set(int r, const Weights16 &W, int64_t m, int row, int quarter)
     {
         p[r] = W.base + m * W.stride + (int64_t)row * W.ld + 8 * quarter;
-        cols = W.cols - 8 * quarter;
+        left = W.cols - 8 * quarter;
     }
+    template <bool TAIL>
     __device__ __forceinline__ void load(Regs &g, int c) const
     {
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) g.w[r][j] = load8(p[r], c * CH + 32 * j, cols);
+            for (int j = 0; j < 4; ++j)
+                g.w[r][j] = TAIL ? load8(p[r], c * CH + 32 * j, left) : __builtin_nontemporal_load(reinterpret_cast<const v4u *>(p[r] + c * CH + 32 * j));
     }
-    template <int NT, class X>
-    __device__ __forceinline__ void apply(const Regs &g, int c, int quarter, const X &x, v4f (&acc)[R][NT]) const
+    static __device__ __forceinline__ void clear(Few &f)
     {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f.d[r][j] = v4f{0, 0, 0, 0};
+    }
+    static __device__ __forceinline__ float finish(const Few &f, int r) { return (f.d[r][0][0] + f.d[r][1][1]) + (f.d[r][2][2] + f.d[r][3][3]); }
+    template <bool TAIL, class X>
+    __device__ __forceinline__ void few(const Regs &g, int, const typename X::Raw (&raw)[PIECES], Few &f) const
+    {
+        v4u x[X::P];
+        X::operands(raw[0], x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int r = 0; r < R; ++r) f.d[r][j] = product<T, X>(x, g.w[r][j], f.d[r][j]);
+    }
+    template <bool TAIL, int NT, class X>
+    __device__ __forceinline__ void tiles(const Regs &g, int c, const X (&x)[NT], int xleft, v4f (&acc)[R][NT]) const
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                const v4u xv = x.load(t, c * CH + 32 * j + 8 * quarter);
+                typename X::Raw raw;
+                x[t].template load<TAIL>(raw, c * CH + 32 * j, xleft);
+                v4u xv[X::P];
+                X::operands(raw, xv);
 #pragma unroll
-                for (int r = 0; r < R; ++r) acc[r][t] = mfma16<T>(xv, g.w[r][j], acc[r][t]);
+                for (int r = 0; r < R; ++r) acc[r][t] = product<T, X>(xv, g.w[r][j], acc[r][t]);
             }
-        }
     }
 };
 
@@ -213,94 +295,208 @@ __device__ __forceinline__ v4u code_order(v4u x)           // eight elements in 
 // GB: blocks of 32 columns that share a scale for certain (1, 2, 4).  S: type of the scales.  T: type of the operands.
 template <int T_, int R_, int GB, int S>
 struct SpanQ4 {
-    static constexpr int T = T_, R = R_, CH = 128, NG = 4 / GB;
+    static constexpr int T = T_, R = R_, CH = 256, PIECES = 2, NG = 8 / GB;       // columns of a chunk: a line of 128 bytes per row
+    typedef typename std::conditional<S == F32, float, unsigned short>::type Scale;
     const unsigned char *q[R], *z[R];
-    const void *s[R];
-    int cols, offset, shift[R], last[R];
+    const Scale *s[R];
+    int cols, offset, shift[R];
     bool zeros[R];
-    struct Regs { v4u w[R]; float s[R][NG]; int z[R][NG]; };
+    struct Regs { v4u w[R][PIECES]; Scale s[R][NG]; unsigned z[R][NG]; };
+    struct Few { float y[R]; };
     __device__ __forceinline__ void set(int r, const WeightsQ4 &W, int64_t m, int row, int quarter)
     {
         q[r] = W.codes + m * W.stride_codes + (int64_t)row * W.ld_codes + 16 * quarter;
         const int64_t at = m * W.stride_scales + (int64_t)row * W.ld_scales;
-        s[r] = static_cast<const char *>(W.scales) + at * (S == F32 ? 4 : 2);
+        s[r] = static_cast<const Scale *>(W.scales) + at;
         zeros[r] = W.zeros != nullptr;
         z[r] = W.zeros + (zeros[r] ? at : 0);
         cols = W.cols;
         shift[r] = W.shift;
-        last[r] = (W.cols - 1) >> W.shift;
         offset = 32 * quarter;
     }
+    // Nothing is computed from what is loaded, so that it can be requested a chunk ahead.
+    template <bool TAIL>
     __device__ __forceinline__ void load(Regs &g, int c) const
     {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            g.w[r] = v4u{0, 0, 0, 0};
-            if (c * CH + offset < cols) g.w[r] = __builtin_nontemporal_load(reinterpret_cast<const v4u *>(q[r] + c * (CH / 2)));
 #pragma unroll
-            for (int i = 0; i < NG; ++i) {
-                const int at = min((c * CH + 32 * GB * i) >> shift[r], last[r]);
-                if constexpr (S == F32) g.s[r][i] = static_cast<const float *>(s[r])[at];
-                else g.s[r][i] = widen<S>(static_cast<const unsigned short *>(s[r])[at]);
-                g.z[r][i] = zeros[r] ? (int)z[r][at] : 8;
+            for (int h = 0; h < PIECES; ++h) {
+                if constexpr (TAIL) g.w[r][h] = v4u{0, 0, 0, 0};
+                if (!TAIL || c * CH + 128 * h + offset < cols)
+                    g.w[r][h] = __builtin_nontemporal_load(reinterpret_cast<const v4u *>(q[r] + c * (CH / 2) + 64 * h));
+            }
+#pragma unroll
+            for (int i = 0; i < NG; ++i) g.s[r][i] = s[r][group<TAIL>(r, c, i)];
+            if (zeros[r]) {
+#pragma unroll
+                for (int i = 0; i < NG; ++i) g.z[r][i] = z[r][group<TAIL>(r, c, i)];
+            } else {
+#pragma unroll
+                for (int i = 0; i < NG; ++i) g.z[r][i] = 8;
             }
         }
     }
-    template <int NT, class X>
-    __device__ __forceinline__ void apply(const Regs &g, int c, int quarter, const X &x, v4f (&acc)[R][NT]) const
+    template <bool TAIL>
+    __device__ __forceinline__ int group(int r, int c, int i) const
     {
-        v4u w[R];
+        const int at = c * CH + 32 * GB * i;
+        return (TAIL ? min(at, cols - 1) : at) >> shift[r];
+    }
+    static __device__ __forceinline__ float factor(Scale v)
+    {
+        float f;
+        if constexpr (S == F32) f = v;
+        else f = widen<S>(v);
+        return T == BF16 ? f * 0x1p9f : f;
+    }
+    static __device__ __forceinline__ void clear(Few &f)
+    {
 #pragma unroll
-        for (int r = 0; r < R; ++r) w[r] = transpose_quarters(g.w[r]);
+        for (int r = 0; r < R; ++r) f.y[r] = 0;
+    }
+    static __device__ __forceinline__ float finish(const Few &f, int r) { return f.y[r]; }
+    // A block past the last column is left out: zero times an infinite scale would be no number.
+    template <bool TAIL, class X>
+    __device__ __forceinline__ void few(const Regs &g, int c, const typename X::Raw (&raw)[PIECES], Few &f) const
+    {
 #pragma unroll
-        for (int i = 0; i < NG; ++i) {
-            if (c * CH + 32 * GB * i >= cols) break;
-            v4f sum[R][NT];
+        for (int h = 0; h < PIECES; ++h) {
+            if (TAIL && c * CH + 128 * h >= cols) break;
+            v4u x[X::P];
+            X::operands(raw[h], x);
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) sum[r][t] = v4f{0, 0, 0, 0};
-#pragma unroll
-            for (int b = 0; b < GB; ++b) {
-                v4u wv[R];
-#pragma unroll
-                for (int r = 0; r < R; ++r) wv[r] = dequantise(w[r][i * GB + b], Zero<T>(g.z[r][i]));
-#pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const v4u xv = code_order<T>(x.load(t, c * CH + 32 * (i * GB + b) + 8 * quarter));
-#pragma unroll
-                    for (int r = 0; r < R; ++r) sum[r][t] = mfma16<T>(xv, wv[r], sum[r][t]);
-                }
-            }
+            for (int q = 0; q < X::P; ++q) x[q] = code_order<T>(x[q]);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                const float f = T == BF16 ? g.s[r][i] * 0x1p9f : g.s[r][i];
+                const v4u w = transpose_quarters(g.w[r][h]);
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                for (int i = 0; i < 4 / GB; ++i) {
+                    if (TAIL && c * CH + 128 * h + 32 * GB * i >= cols) break;
+                    const Zero<T> zero(g.z[r][h * 4 / GB + i]);
+                    float sum = 0;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[r][t][e] = fmaf(sum[r][t][e], f, acc[r][t][e]);
+                    for (int b = 0; b < GB; ++b) {
+                        const int j = i * GB + b;
+                        const v4f d = product<T, X>(x, dequantise(w[j], zero), v4f{0, 0, 0, 0});
+                        sum = b ? sum + d[j] : d[j];
+                    }
+                    f.y[r] = fmaf(sum, factor(g.s[r][h * 4 / GB + i]), f.y[r]);
+                }
+            }
+        }
+    }
+    template <bool TAIL, int NT, class X>
+    __device__ __forceinline__ void tiles(const Regs &g, int c, const X (&x)[NT], int xleft, v4f (&acc)[R][NT]) const
+    {
+#pragma unroll
+        for (int h = 0; h < PIECES; ++h) {
+            if (TAIL && c * CH + 128 * h >= cols) break;
+            v4u w[R];
+#pragma unroll
+            for (int r = 0; r < R; ++r) w[r] = transpose_quarters(g.w[r][h]);
+#pragma unroll
+            for (int i = 0; i < 4 / GB; ++i) {
+                if (TAIL && c * CH + 128 * h + 32 * GB * i >= cols) break;
+                v4f sum[R][NT];
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) sum[r][t] = v4f{0, 0, 0, 0};
+#pragma unroll
+                for (int b = 0; b < GB; ++b) {
+                    const int j = i * GB + b;
+                    v4u wv[R];
+#pragma unroll
+                    for (int r = 0; r < R; ++r) wv[r] = dequantise(w[r][j], Zero<T>(g.z[r][h * 4 / GB + i]));
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        typename X::Raw raw;
+                        x[t].template load<TAIL>(raw, c * CH + 128 * h + 32 * j, xleft);
+                        v4u xv[X::P];
+                        X::operands(raw, xv);
+#pragma unroll
+                        for (int q = 0; q < X::P; ++q) xv[q] = code_order<T>(xv[q]);
+#pragma unroll
+                        for (int r = 0; r < R; ++r) sum[r][t] = product<T, X>(xv, wv[r], sum[r][t]);
+                    }
+                }
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const float f = factor(g.s[r][h * 4 / GB + i]);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[r][t][e] = fmaf(sum[r][t][e], f, acc[r][t][e]);
+                }
             }
         }
     }
 };
 
-// Chunks first, first + step, ... of the columns, one chunk of weights requested ahead.
-template <class SPAN, int NT, class X>
-__device__ __forceinline__ void span_product(const SPAN &s, const X &x, int cols, int first, int step, int quarter, v4f (&acc)[SPAN::R][NT])
+// Chunks first, first + step, ... of the columns, weights (and the few vectors) requested a chunk ahead.  The last chunk, if it is
+// not whole, comes after the others and is the only one whose loads look at where the columns end.
+template <class SPAN, class LOAD, class APPLY>
+__device__ __forceinline__ void chunks(int cols, int first, int step, LOAD load, APPLY apply)
 {
-    const int n = (cols + SPAN::CH - 1) / SPAN::CH;
-    if (first >= n) return;
-    typename SPAN::Regs g;
-    s.load(g, first);
-    for (int c = first; c < n; c += step) {
-        typename SPAN::Regs next;
-        if (c + step < n) s.load(next, c + step);
-        s.template apply<NT, X>(g, c, quarter, x, acc);
-        g = next;
+    const int whole = cols / SPAN::CH;
+    int c = first;
+    if (c < whole) {
+        load(0, c);
+        for (;;) {
+            if (c + step < whole) load(1, c + step);
+            apply(0, c);
+            c += step;
+            if (c >= whole) break;
+            if (c + step < whole) load(0, c + step);
+            apply(1, c);
+            c += step;
+            if (c >= whole) break;
+        }
+    }
+}
+template <class SPAN, class X>
+__device__ __forceinline__ void few_product(const SPAN &s, const X &x, int cols, int first, int step, int lane, float (&y)[SPAN::R])
+{
+    typename SPAN::Regs g[2];
+    typename X::Raw raw[2][SPAN::PIECES];
+    typename SPAN::Few f;
+    SPAN::clear(f);
+    const int xleft = cols - 32 * (lane & 3) - 8 * (lane >> 4), whole = cols / SPAN::CH;
+    chunks<SPAN>(cols, first, step,
+        [&](int b, int c) {
+            s.template load<false>(g[b], c);
+#pragma unroll
+            for (int h = 0; h < SPAN::PIECES; ++h) x.template load<false>(raw[b][h], c * SPAN::CH + 128 * h, xleft);
+        },
+        [&](int b, int c) { s.template few<false, X>(g[b], c, raw[b], f); });
+    if (whole * SPAN::CH < cols && whole % step == first) {
+        s.template load<true>(g[0], whole);
+#pragma unroll
+        for (int h = 0; h < SPAN::PIECES; ++h) x.template load<true>(raw[0][h], whole * SPAN::CH + 128 * h, xleft);
+        s.template few<true, X>(g[0], whole, raw[0], f);
+    }
+#pragma unroll
+    for (int r = 0; r < SPAN::R; ++r) y[r] = SPAN::finish(f, r);
+}
+template <class SPAN, int NT, class X>
+__device__ __forceinline__ void tile_product(const SPAN &s, const X (&x)[NT], int cols, int first, int step, int lane, v4f (&acc)[SPAN::R][NT])
+{
+    typename SPAN::Regs g[2];
+#pragma unroll
+    for (int r = 0; r < SPAN::R; ++r)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[r][t] = v4f{0, 0, 0, 0};
+    const int xleft = cols - 8 * (lane >> 4), whole = cols / SPAN::CH;
+    chunks<SPAN>(cols, first, step, [&](int b, int c) { s.template load<false>(g[b], c); },
+                 [&](int b, int c) { s.template tiles<false, NT, X>(g[b], c, x, xleft, acc); });
+    if (whole * SPAN::CH < cols && whole % step == first) {
+        s.template load<true>(g[0], whole);
+        s.template tiles<true, NT, X>(g[0], whole, x, xleft, acc);
     }
 }
 
-// Sums of the W waves of a workgroup, in the order of the waves: tile t of `sums` as 16 vectors x 16 rows.
+// Sums of the W waves of a workgroup, in the order of the waves.  Tiles: 16 vectors x 16 rows each; few vectors: 4 x 16.
 template <int TILES>
 __device__ __forceinline__ void put_sums(float *lds, int wave, int lane, const v4f (&acc)[TILES])
 {
@@ -309,12 +505,19 @@ __device__ __forceinline__ void put_sums(float *lds, int wave, int lane, const v
 #pragma unroll
         for (int i = 0; i < 4; ++i) lds[((wave * TILES + t) * 16 + 4 * (lane >> 4) + i) * 16 + (lane & 15)] = acc[t][i];
 }
-template <int W, int TILES>
+template <int R>
+__device__ __forceinline__ void put_few(float *lds, int wave, int lane, const float (&y)[R])
+{
+#pragma unroll
+    for (int r = 0; r < R; ++r) lds[(wave * R + r) * 64 + lane] = y[r];
+}
+// V: vectors of a tile (16, or 4)
+template <int W, int TILES, int V>
 __device__ __forceinline__ float get_sum(const float *lds, int t, int m, int n)
 {
     float v = 0;
 #pragma unroll
-    for (int w = 0; w < W; ++w) v += lds[((w * TILES + t) * 16 + m) * 16 + n];
+    for (int w = 0; w < W; ++w) v += lds[((w * TILES + t) * V + m) * 16 + n];
     return v;
 }
 
