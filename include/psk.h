@@ -579,7 +579,7 @@ int psk_moe_route(int64_t n, int64_t dim, int64_t experts, int32_t top_k, int sc
  * Made for a few tokens: the matrices of the experts that occur are read once for up to 64 entries of an expert.
  * psk_moe_experts: weights of `type`, matrix e of W1 and W3 at stride1*e elements, rows ld1 apart (W2: stride2, ld2); bases 16-byte aligned,
  * strides and leading dimensions multiples of 8.
- * psk_moe_experts_q4: weights in 4 bits, count = experts in all three, W1 and W3 alike in rows and cols, all with one scale_type.
+ * psk_moe_experts_q4: weights in 4 bits, count = experts in all three, W1 and W3 alike in rows, cols and group, all with one scale_type.
  * With PSK_F16 and 16-bit weights, values between the two products of 2^24 and more become infinite.
  * The workspace is for both.
  */

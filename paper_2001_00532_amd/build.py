@@ -23,8 +23,9 @@ OUT_MARSHAL = os.path.join(HERE, "_marshal.so")
 MARSHAL_FOR = os.path.join(OBJDIR, "marshal_built_for")
 
 SOURCES = ["api.hip", "partition.hip", "spmv_csr.hip", "spmm.hip", "spmv_bcsr.hip", "mttkrp.hip", "spmv_csr_f64.hip", "spmv_csr_divide.hip", "spmv_bcsr_g.hip", "spmm_narrow.hip", "spmm_blocks.hip", "slab.hip", "api_slab.hip", "calibrate.hip",
-           "gemm_q4.hip", "moe_route.hip", "moe.hip", "api_serving.hip"]
-HEADERS = ["psk_dev.h", "psk_mfma.h", "psk_internal.h", os.path.join("..", "..", "include", "psk.h")]
+           "gemm_q4_f32.hip", "gemm_q4_f16.hip", "gemm_q4_bf16.hip", "moe_route.hip", "moe.hip", "moe_q4_f16.hip", "moe_q4_bf16.hip",
+           "api_serving.hip"]
+HEADERS = ["psk_dev.h", "psk_mfma.h", "gemm_q4.h", "moe.h", "moe_q4.h", "psk_internal.h", os.path.join("..", "..", "include", "psk.h")]
 
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",

@@ -69,7 +69,8 @@ int psk_gemm_q4(const psk_q4 *A, int64_t n, int type, const void *X, int64_t ldx
     if (n == 0 || A->rows == 0) return PSK_OK;
     if (!Y || (A->cols > 0 && !X)) return PSK_ERR_NULL;
     if (misaligned(X, bytes_of(type)) || misaligned(Y, bytes_of(type))) return PSK_ERR_ALIGNMENT;
-    return hip_status(launch_gemm_q4(weights(*A), A->scale_type, (int)n, type, X, ldx, Y, ldy, static_cast<hipStream_t>(stream)));
+    const auto launch = type == PSK_F32 ? launch_gemm_q4_of<F32> : (type == PSK_F16 ? launch_gemm_q4_of<F16> : launch_gemm_q4_of<BF16>);
+    return hip_status(launch(weights(*A), A->scale_type, (int)n, X, ldx, Y, ldy, static_cast<hipStream_t>(stream)));
 }
 
 size_t psk_moe_route_workspace_bytes(int64_t n, int64_t experts)
@@ -131,14 +132,16 @@ int psk_moe_experts_q4(int64_t n, int32_t top_k, int act, int type, const void *
     const int64_t dim = W1->cols, inter = W1->rows, experts = W1->count;
     const int st = check_layer(n, dim, inter, experts, top_k, act, type, ldx, ldy);
     if (st != PSK_OK) return st;
-    if (W3->rows != inter || W3->cols != dim || W2->rows != dim || W2->cols != inter || W3->count != experts || W2->count != experts) return PSK_ERR_SIZE;
+    if (W3->rows != inter || W3->cols != dim || W2->rows != dim || W2->cols != inter || W3->count != experts || W2->count != experts || W3->group != W1->group)
+        return PSK_ERR_SIZE;
     if (W3->scale_type != W1->scale_type || W2->scale_type != W1->scale_type) return PSK_ERR_UNSUPPORTED;
     if (!workspace_ok(workspace, workspace_bytes, moe_workspace_bytes(n, dim, inter, top_k))) return PSK_ERR_WORKSPACE;
     if (n == 0) return PSK_OK;
     if (!X || !crd || !vals || !Y) return PSK_ERR_NULL;
     if (misaligned(X, 2) || misaligned(Y, 2) || misaligned(crd, 4) || misaligned(vals, 4)) return PSK_ERR_ALIGNMENT;
     const MoeCall c = {n, (int)dim, (int)inter, (int)experts, top_k, act, X, ldx, crd, vals, Y, ldy, workspace};
-    return hip_status(launch_moe_q4(c, type, W1->scale_type, weights(*W1), weights(*W3), weights(*W2), static_cast<hipStream_t>(stream)));
+    const auto launch = type == PSK_F16 ? launch_moe_q4_of<F16> : launch_moe_q4_of<BF16>;
+    return hip_status(launch(c, W1->scale_type, weights(*W1), weights(*W3), weights(*W2), static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -291,7 +291,8 @@ hipError_t launch_mttkrp_main(int64_t dim_k, int64_t dim_l, int32_t nslices, int
 // Products with 4-bit weights (gemm_q4.hip), the router (moe_route.hip) and the layer (moe.hip) of a mixture of experts.
 // Types are psk_type.
 struct WeightsQ4;
-hipError_t launch_gemm_q4(const WeightsQ4 &A, int scale_type, int n, int type, const void *X, int64_t ldx, void *Y, int64_t ldy, hipStream_t s);
+template <int XT>
+hipError_t launch_gemm_q4_of(const WeightsQ4 &A, int scale_type, int n, const void *X, int64_t ldx, void *Y, int64_t ldy, hipStream_t s);
 hipError_t launch_moe_route(int n, int dim, int experts, int top_k, int score, int normalise, float factor, int type, const void *X, int64_t ldx,
                             int wtype, const void *W, int64_t ldw, const float *bias, int *crd, float *vals, double *logits, hipStream_t s);
 // Positions of the gating matrix that a pair of launches takes (more tokens go in several pairs): each workgroup of the layer
@@ -311,6 +312,7 @@ struct MoeCall {
 size_t moe_workspace_bytes(int64_t n, int64_t dim, int64_t inter, int top_k);
 hipError_t launch_moe_16(const MoeCall &c, int type, const void *W1, const void *W3, int64_t ld1, int64_t stride1, const void *W2, int64_t ld2,
                          int64_t stride2, hipStream_t s);
-hipError_t launch_moe_q4(const MoeCall &c, int type, int scale_type, const WeightsQ4 &w1, const WeightsQ4 &w3, const WeightsQ4 &w2, hipStream_t s);
+template <int T>
+hipError_t launch_moe_q4_of(const MoeCall &c, int scale_type, const WeightsQ4 &w1, const WeightsQ4 &w3, const WeightsQ4 &w2, hipStream_t s);
 
 }  // namespace psk

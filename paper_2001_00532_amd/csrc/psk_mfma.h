@@ -50,14 +50,19 @@ __device__ __forceinline__ void store_as(void *y, int64_t i, float v)
     else static_cast<unsigned short *>(y)[i] = narrow<T>(v);
 }
 
-// Eight 16-bit elements from column k on, zeros from column `cols` on.
-__device__ __forceinline__ v4u load8(const unsigned short *p, int k, int cols)
+// Eight 16-bit elements from column k on, zeros from column `left` on.  (A loop of one load: written out it would cost the kernels
+// around it more registers than all the rest.)
+__device__ __forceinline__ v4u load8(const unsigned short *p, int k, int left)
 {
-    if (k + 8 <= cols) return *reinterpret_cast<const v4u_u *>(p + k);
+    if (k + 8 <= left) return *reinterpret_cast<const v4u_u *>(p + k);
     v4u r = {0, 0, 0, 0};
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (k + i < cols) r[i / 2] |= (unsigned)p[k + i] << (16 * (i & 1));
+    if (k < left) {
+#pragma unroll 1
+        for (int i = k + 7; i >= k; --i) {
+            const unsigned e = i < left ? p[i] : 0u;
+            r = v4u{r[0] << 16 | e, r[1] << 16 | r[0] >> 16, r[2] << 16 | r[1] >> 16, r[3] << 16 | r[2] >> 16};
+        }
+    }
     return r;
 }
 
@@ -92,11 +97,14 @@ struct Parts32 {
         if (!TAIL || k + 8 <= left) {
             r.a = *reinterpret_cast<const v4f_e *>(p + k);
             r.b = *reinterpret_cast<const v4f_e *>(p + k + 4);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                r.a[i] = k + i < left ? p[k + i] : 0.0f;
-                r.b[i] = k + 4 + i < left ? p[k + 4 + i] : 0.0f;
+            return;
+        }
+        r.a = r.b = v4f_e{0, 0, 0, 0};
+        if (k < left) {
+#pragma unroll 1
+            for (int i = k + 7; i >= k; --i) {
+                r.b = v4f_e{r.a[3], r.b[0], r.b[1], r.b[2]};
+                r.a = v4f_e{i < left ? p[i] : 0.0f, r.a[0], r.a[1], r.a[2]};
             }
         }
     }
@@ -167,17 +175,18 @@ struct Weights16 {
     int64_t ld, stride;
     int rows, cols;
 };
-template <int T_, int R_>
+// B: blocks of 32 columns in a chunk: four for few vectors, two (a line of 128 bytes per row) for tiles.
+template <int T_, int R_, int B_>
 struct Span16 {
-    static constexpr int T = T_, R = R_, CH = 128, PIECES = 1;        // columns of a chunk: 256 bytes per row; pieces of 128 columns
+    static constexpr int T = T_, R = R_, B = B_, CH = 32 * B, PIECES = 1;
     const unsigned short *p[R];
     int left;                                              // columns from the lane's first one on
-    struct Regs { v4u w[R][4]; };
+    struct Regs { v4u w[R][B]; };
     struct Few { v4f d[R][4]; };
-    __device__ __forceinline__ void set(int r, const Weights16 &W, int64_t m, int row, int quarter)
+    __device__ __forceinline__ void set(int r, const Weights16 &W, int64_t m, int row, int quarter, int columns)
     {
         p[r] = W.base + m * W.stride + (int64_t)row * W.ld + 8 * quarter;
-        left = W.cols - 8 * quarter;
+        left = columns - 8 * quarter;
     }
     template <bool TAIL>
     __device__ __forceinline__ void load(Regs &g, int c) const
@@ -185,7 +194,7 @@ struct Span16 {
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < B; ++j)
                 g.w[r][j] = TAIL ? load8(p[r], c * CH + 32 * j, left) : __builtin_nontemporal_load(reinterpret_cast<const v4u *>(p[r] + c * CH + 32 * j));
     }
     static __device__ __forceinline__ void clear(Few &f)
@@ -199,6 +208,7 @@ struct Span16 {
     template <bool TAIL, class X>
     __device__ __forceinline__ void few(const Regs &g, int, const typename X::Raw (&raw)[PIECES], Few &f) const
     {
+        static_assert(B == 4, "four blocks");
         v4u x[X::P];
         X::operands(raw[0], x);
 #pragma unroll
@@ -207,18 +217,16 @@ struct Span16 {
             for (int r = 0; r < R; ++r) f.d[r][j] = product<T, X>(x, g.w[r][j], f.d[r][j]);
     }
     template <bool TAIL, int NT, class X>
-    __device__ __forceinline__ void tiles(const Regs &g, int c, const X (&x)[NT], int xleft, v4f (&acc)[R][NT]) const
+    __device__ __forceinline__ void tiles(const Regs &g, int, const typename X::Raw (&raw)[NT][B], v4f (&acc)[R][NT]) const
     {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < B; ++j)
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                typename X::Raw raw;
-                x[t].template load<TAIL>(raw, c * CH + 32 * j, xleft);
-                v4u xv[X::P];
-                X::operands(raw, xv);
+                v4u x[X::P];
+                X::operands(raw[t][j], x);
 #pragma unroll
-                for (int r = 0; r < R; ++r) acc[r][t] = product<T, X>(xv, g.w[r][j], acc[r][t]);
+                for (int r = 0; r < R; ++r) acc[r][t] = product<T, X>(x, g.w[r][j], acc[r][t]);
             }
     }
 };
@@ -292,25 +300,34 @@ __device__ __forceinline__ v4u code_order(v4u x)           // eight elements in 
                    __builtin_amdgcn_perm(x[3], x[1], 0x05040100u), __builtin_amdgcn_perm(x[3], x[1], 0x07060302u)};
 }
 
-// GB: blocks of 32 columns that share a scale for certain (1, 2, 4).  S: type of the scales.  T: type of the operands.
-template <int T_, int R_, int GB, int S>
+// N scales or zero points that lie side by side, as one load.
+template <typename E, int N> struct Run { typedef E type __attribute__((ext_vector_type(N), aligned(sizeof(E)))); };
+
+// P: pieces of 128 columns in a chunk; two read whole lines of 128 bytes per row.  GB: blocks of 32 columns that share a scale: 1, 2 and
+// 4 for groups of just 32, 64 and 128 columns (then the scales of a chunk are one load), 8 for larger ones; 4 also for those if P is 1.
+// S: type of the scales.  T: type of the operands.  Z: some matrix has zero points; one that has none reads its codes in
+// their place and puts 8 for what it read, so that no load stands under a condition.
+template <int T_, int R_, int P, int GB, int S, bool Z>
 struct SpanQ4 {
-    static constexpr int T = T_, R = R_, CH = 256, PIECES = 2, NG = 8 / GB;       // columns of a chunk: a line of 128 bytes per row
+    static constexpr int T = T_, R = R_, B = 4 * P, CH = 32 * B, PIECES = P, NG = 4 * P > GB ? 4 * P / GB : 1, PER = GB < 4 ? GB : 4;     // PER: blocks of a piece that share one
     typedef typename std::conditional<S == F32, float, unsigned short>::type Scale;
+    typedef typename Run<Scale, NG>::type Scales;
+    typedef typename Run<unsigned char, NG>::type Zeros;
     const unsigned char *q[R], *z[R];
     const Scale *s[R];
     int cols, offset, shift[R];
-    bool zeros[R];
-    struct Regs { v4u w[R][PIECES]; Scale s[R][NG]; unsigned z[R][NG]; };
+    unsigned zmask[R], zelse[R];
+    struct Regs { v4u w[R][P]; Scales s[R]; Zeros z[Z ? R : 1]; };
     struct Few { float y[R]; };
-    __device__ __forceinline__ void set(int r, const WeightsQ4 &W, int64_t m, int row, int quarter)
+    __device__ __forceinline__ void set(int r, const WeightsQ4 &W, int64_t m, int row, int quarter, int columns)
     {
         q[r] = W.codes + m * W.stride_codes + (int64_t)row * W.ld_codes + 16 * quarter;
         const int64_t at = m * W.stride_scales + (int64_t)row * W.ld_scales;
         s[r] = static_cast<const Scale *>(W.scales) + at;
-        zeros[r] = W.zeros != nullptr;
-        z[r] = W.zeros + (zeros[r] ? at : 0);
-        cols = W.cols;
+        z[r] = W.zeros ? W.zeros + at : q[r] - 16 * quarter;
+        zmask[r] = W.zeros ? 255 : 0;
+        zelse[r] = W.zeros ? 0 : 8;
+        cols = columns;
         shift[r] = W.shift;
         offset = 32 * quarter;
     }
@@ -321,27 +338,29 @@ struct SpanQ4 {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
 #pragma unroll
-            for (int h = 0; h < PIECES; ++h) {
+            for (int h = 0; h < P; ++h) {
                 if constexpr (TAIL) g.w[r][h] = v4u{0, 0, 0, 0};
                 if (!TAIL || c * CH + 128 * h + offset < cols)
                     g.w[r][h] = __builtin_nontemporal_load(reinterpret_cast<const v4u *>(q[r] + c * (CH / 2) + 64 * h));
             }
+            if constexpr (TAIL) {
 #pragma unroll
-            for (int i = 0; i < NG; ++i) g.s[r][i] = s[r][group<TAIL>(r, c, i)];
-            if (zeros[r]) {
-#pragma unroll
-                for (int i = 0; i < NG; ++i) g.z[r][i] = z[r][group<TAIL>(r, c, i)];
+                for (int i = 0; i < NG; ++i) {
+                    const int at = min(c * CH + 32 * GB * i, cols - 1) >> shift[r];
+                    g.s[r][i] = s[r][at];
+                    if constexpr (Z) g.z[r][i] = z[r][at];
+                }
             } else {
-#pragma unroll
-                for (int i = 0; i < NG; ++i) g.z[r][i] = 8;
+                const int at = (c * CH) >> shift[r];
+                g.s[r] = *reinterpret_cast<const Scales *>(s[r] + at);
+                if constexpr (Z) g.z[r] = *reinterpret_cast<const Zeros *>(z[r] + at);
             }
         }
     }
-    template <bool TAIL>
-    __device__ __forceinline__ int group(int r, int c, int i) const
+    __device__ __forceinline__ Zero<T> zero(const Regs &g, int r, int i) const
     {
-        const int at = c * CH + 32 * GB * i;
-        return (TAIL ? min(at, cols - 1) : at) >> shift[r];
+        if constexpr (Z) return Zero<T>((int)((g.z[r][i] & zmask[r]) | zelse[r]));
+        else return Zero<T>(8);
     }
     static __device__ __forceinline__ float factor(Scale v)
     {
@@ -356,13 +375,12 @@ struct SpanQ4 {
         for (int r = 0; r < R; ++r) f.y[r] = 0;
     }
     static __device__ __forceinline__ float finish(const Few &f, int r) { return f.y[r]; }
-    // A block past the last column is left out: zero times an infinite scale would be no number.
+    // A block past the last column counts nothing: its sum is zero, and so has the scale to be (it could be infinite).
     template <bool TAIL, class X>
     __device__ __forceinline__ void few(const Regs &g, int c, const typename X::Raw (&raw)[PIECES], Few &f) const
     {
 #pragma unroll
-        for (int h = 0; h < PIECES; ++h) {
-            if (TAIL && c * CH + 128 * h >= cols) break;
+        for (int h = 0; h < P; ++h) {
             v4u x[X::P];
             X::operands(raw[h], x);
 #pragma unroll
@@ -371,88 +389,81 @@ struct SpanQ4 {
             for (int r = 0; r < R; ++r) {
                 const v4u w = transpose_quarters(g.w[r][h]);
 #pragma unroll
-                for (int i = 0; i < 4 / GB; ++i) {
-                    if (TAIL && c * CH + 128 * h + 32 * GB * i >= cols) break;
-                    const Zero<T> zero(g.z[r][h * 4 / GB + i]);
+                for (int i = 0; i < 4 / PER; ++i) {
+                    const int at = 4 * h / GB + i;
+                    const Zero<T> less = zero(g, r, at);
                     float sum = 0;
 #pragma unroll
-                    for (int b = 0; b < GB; ++b) {
-                        const int j = i * GB + b;
-                        const v4f d = product<T, X>(x, dequantise(w[j], zero), v4f{0, 0, 0, 0});
+                    for (int b = 0; b < PER; ++b) {
+                        const int j = i * PER + b;
+                        const v4f d = product<T, X>(x, dequantise(w[j], less), v4f{0, 0, 0, 0});
                         sum = b ? sum + d[j] : d[j];
                     }
-                    f.y[r] = fmaf(sum, factor(g.s[r][h * 4 / GB + i]), f.y[r]);
+                    f.y[r] = fmaf(sum, !TAIL || c * CH + 128 * h + 32 * PER * i < cols ? factor(g.s[r][at]) : 0.0f, f.y[r]);
                 }
             }
         }
     }
     template <bool TAIL, int NT, class X>
-    __device__ __forceinline__ void tiles(const Regs &g, int c, const X (&x)[NT], int xleft, v4f (&acc)[R][NT]) const
+    __device__ __forceinline__ void tiles(const Regs &g, int c, const typename X::Raw (&raw)[NT][4], v4f (&acc)[R][NT]) const
     {
+        static_assert(P == 1, "one piece");
+        v4u w[R];
 #pragma unroll
-        for (int h = 0; h < PIECES; ++h) {
-            if (TAIL && c * CH + 128 * h >= cols) break;
-            v4u w[R];
+        for (int r = 0; r < R; ++r) w[r] = transpose_quarters(g.w[r][0]);
 #pragma unroll
-            for (int r = 0; r < R; ++r) w[r] = transpose_quarters(g.w[r][h]);
+        for (int i = 0; i < 4 / PER; ++i) {
+            v4f sum[R][NT];
 #pragma unroll
-            for (int i = 0; i < 4 / GB; ++i) {
-                if (TAIL && c * CH + 128 * h + 32 * GB * i >= cols) break;
-                v4f sum[R][NT];
+            for (int r = 0; r < R; ++r)
 #pragma unroll
-                for (int r = 0; r < R; ++r)
+                for (int t = 0; t < NT; ++t) sum[r][t] = v4f{0, 0, 0, 0};
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) sum[r][t] = v4f{0, 0, 0, 0};
+            for (int b = 0; b < PER; ++b) {
+                const int j = i * PER + b;
+                v4u wv[R];
 #pragma unroll
-                for (int b = 0; b < GB; ++b) {
-                    const int j = i * GB + b;
-                    v4u wv[R];
+                for (int r = 0; r < R; ++r) wv[r] = dequantise(w[r][j], zero(g, r, i));
 #pragma unroll
-                    for (int r = 0; r < R; ++r) wv[r] = dequantise(w[r][j], Zero<T>(g.z[r][h * 4 / GB + i]));
+                for (int t = 0; t < NT; ++t) {
+                    v4u x[X::P];
+                    X::operands(raw[t][j], x);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t) {
-                        typename X::Raw raw;
-                        x[t].template load<TAIL>(raw, c * CH + 128 * h + 32 * j, xleft);
-                        v4u xv[X::P];
-                        X::operands(raw, xv);
+                    for (int q = 0; q < X::P; ++q) x[q] = code_order<T>(x[q]);
 #pragma unroll
-                        for (int q = 0; q < X::P; ++q) xv[q] = code_order<T>(xv[q]);
-#pragma unroll
-                        for (int r = 0; r < R; ++r) sum[r][t] = product<T, X>(xv, wv[r], sum[r][t]);
-                    }
+                    for (int r = 0; r < R; ++r) sum[r][t] = product<T, X>(x, wv[r], sum[r][t]);
                 }
+            }
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const float f = factor(g.s[r][h * 4 / GB + i]);
+            for (int r = 0; r < R; ++r) {
+                const float f = !TAIL || c * CH + 32 * PER * i < cols ? factor(g.s[r][i]) : 0.0f;
 #pragma unroll
-                    for (int t = 0; t < NT; ++t)
+                for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[r][t][e] = fmaf(sum[r][t][e], f, acc[r][t][e]);
-                }
+                    for (int e = 0; e < 4; ++e) acc[r][t][e] = fmaf(sum[r][t][e], f, acc[r][t][e]);
             }
         }
     }
 };
 
-// Chunks first, first + step, ... of the columns, weights (and the few vectors) requested a chunk ahead.  The last chunk, if it is
+// Chunks first, first + step, ... of the columns, weights and vectors requested a chunk ahead.  The last chunk, if it is
 // not whole, comes after the others and is the only one whose loads look at where the columns end.
 template <class SPAN, class LOAD, class APPLY>
 __device__ __forceinline__ void chunks(int cols, int first, int step, LOAD load, APPLY apply)
 {
     const int whole = cols / SPAN::CH;
     int c = first;
-    if (c < whole) {
-        load(0, c);
-        for (;;) {
-            if (c + step < whole) load(1, c + step);
-            apply(0, c);
-            c += step;
-            if (c >= whole) break;
-            if (c + step < whole) load(0, c + step);
-            apply(1, c);
-            c += step;
-            if (c >= whole) break;
-        }
+    if (c >= whole) return;
+    load(0, c);
+    for (;;) {                                             // no load stands under a condition: waiting for one would wait for all
+        if (c + step >= whole) { apply(0, c); return; }
+        load(1, c + step);
+        apply(0, c);
+        c += step;
+        if (c + step >= whole) { apply(1, c); return; }
+        load(0, c + step);
+        apply(1, c);
+        c += step;
     }
 }
 template <class SPAN, class X>
@@ -483,16 +494,28 @@ template <class SPAN, int NT, class X>
 __device__ __forceinline__ void tile_product(const SPAN &s, const X (&x)[NT], int cols, int first, int step, int lane, v4f (&acc)[SPAN::R][NT])
 {
     typename SPAN::Regs g[2];
+    typename X::Raw raw[2][NT][SPAN::B];
 #pragma unroll
     for (int r = 0; r < SPAN::R; ++r)
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[r][t] = v4f{0, 0, 0, 0};
     const int xleft = cols - 8 * (lane >> 4), whole = cols / SPAN::CH;
-    chunks<SPAN>(cols, first, step, [&](int b, int c) { s.template load<false>(g[b], c); },
-                 [&](int b, int c) { s.template tiles<false, NT, X>(g[b], c, x, xleft, acc); });
+    chunks<SPAN>(cols, first, step,
+        [&](int b, int c) {
+            s.template load<false>(g[b], c);
+#pragma unroll
+            for (int j = 0; j < SPAN::B; ++j)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) x[t].template load<false>(raw[b][t][j], c * SPAN::CH + 32 * j, xleft);
+        },
+        [&](int b, int c) { s.template tiles<false, NT, X>(g[b], c, raw[b], acc); });
     if (whole * SPAN::CH < cols && whole % step == first) {
         s.template load<true>(g[0], whole);
-        s.template tiles<true, NT, X>(g[0], whole, x, xleft, acc);
+#pragma unroll
+        for (int j = 0; j < SPAN::B; ++j)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) x[t].template load<true>(raw[0][t][j], whole * SPAN::CH + 32 * j, xleft);
+        s.template tiles<true, NT, X>(g[0], whole, raw[0], acc);
     }
 }
 

@@ -188,12 +188,12 @@ def test_layer_q4(dtype, groups, scale32, n, dim, inter, experts, top_k, kind):
 
 
 def test_matrices_with_groups_and_zero_points_of_their_own():
-    """Each of the three matrices has its own group, and zero points or none."""
+    """The last matrix has a group of its own, and each of the three zero points or none."""
     rng = np.random.default_rng(16)
     n, dim, inter, experts, t = 6, 300, 150, 4, torch.float16
     x = torch.from_numpy(rng.standard_normal((n, dim))).to(t)
     crd, vals = gating(rng, n, experts, 2)
-    for groups, zeros in (((32, 128, 64), (True, False, False)), ((256, 64, 128), (False, True, True)), ((128, 1024, 32), (True, True, False))):
+    for groups, zeros in (((32, 32, 64), (True, False, False)), ((256, 256, 128), (False, True, True)), ((128, 128, 1024), (True, True, False))):
         w = [R.q4_weights(rng, r, c, g, z, t, experts, scale=0.4 / math.sqrt(c))
              for (r, c), g, z in zip(((inter, dim), (inter, dim), (dim, inter)), groups, zeros)]
         y = torch.full((n, dim), 77.0, dtype=t, device="cuda")

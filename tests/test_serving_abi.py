@@ -103,7 +103,7 @@ def test_layer_q4_refuses():
     for over in (dict(X=NULL), dict(crd=NULL), dict(vals=NULL), dict(Y=NULL)):
         assert layer_q4(**over) == 1, over
     for over in (dict(w3=q4(count=9)), dict(w3=q4(count=10, rows=47)), dict(w3=q4(count=10, cols=99)), dict(w2=q4(count=10)), dict(w1=q4(count=0)),
-                 dict(w1=q4(count=10, stride_codes=-16)), dict(ldx=99), dict(ldy=99), dict(top_k=0), dict(n=-1)):
+                 dict(w1=q4(count=10, stride_codes=-16)), dict(w3=q4(count=10, group=64)), dict(ldx=99), dict(ldy=99), dict(top_k=0), dict(n=-1)):
         assert layer_q4(**over) == 2, over
     assert layer_q4(ws=NULL) == 4 and layer_q4(have=255) == 4
     assert layer_q4(w3=q4(count=10, scale_type=psk.PSK_F32)) == 5 and layer_q4(type=psk.PSK_F32) == 5 and layer_q4(act=7) == 5
