@@ -55,7 +55,8 @@ extern "C" {
 size_t psk_gemm_q4_workspace_bytes(int64_t rows, int64_t cols, int64_t n, int type)
 {
     if (rows < 0 || cols < 0 || rows > kMaxEdge || cols > kMaxEdge || n < 0 || n > PSK_MAX_VECTORS || !type_ok(type)) return 0;
-    return 256;
+    // more than four vectors: their copy in the order of the operands, vectors of 32 bits in three parts
+    return n <= 4 ? 256 : (size_t)((n + 15) / 16) * copied_blocks((int)cols) * (type == PSK_F32 ? 3 : 1) * 1024 + 256;
 }
 
 int psk_gemm_q4(const psk_q4 *A, int64_t n, int type, const void *X, int64_t ldx, void *Y, int64_t ldy, void *workspace,
@@ -70,7 +71,7 @@ int psk_gemm_q4(const psk_q4 *A, int64_t n, int type, const void *X, int64_t ldx
     if (!Y || (A->cols > 0 && !X)) return PSK_ERR_NULL;
     if (misaligned(X, bytes_of(type)) || misaligned(Y, bytes_of(type))) return PSK_ERR_ALIGNMENT;
     const auto launch = type == PSK_F32 ? launch_gemm_q4_of<F32> : (type == PSK_F16 ? launch_gemm_q4_of<F16> : launch_gemm_q4_of<BF16>);
-    return hip_status(launch(weights(*A), A->scale_type, (int)n, X, ldx, Y, ldy, static_cast<hipStream_t>(stream)));
+    return hip_status(launch(weights(*A), A->scale_type, (int)n, X, ldx, Y, ldy, workspace, static_cast<hipStream_t>(stream)));
 }
 
 size_t psk_moe_route_workspace_bytes(int64_t n, int64_t experts)
@@ -99,7 +100,7 @@ int psk_moe_route(int64_t n, int64_t dim, int64_t experts, int32_t top_k, int sc
 size_t psk_moe_workspace_bytes(int64_t n, int64_t dim, int64_t inter, int64_t experts, int32_t top_k)
 {
     if (check_layer(n, dim, inter, experts, top_k, PSK_ACT_SILU, PSK_F16, dim, dim) != PSK_OK) return 0;
-    return moe_workspace_bytes(n, dim, inter, top_k);
+    return moe_workspace_bytes(n, dim, inter, experts, top_k);
 }
 
 int psk_moe_experts(int64_t n, int64_t dim, int64_t inter, int64_t experts, int32_t top_k, int act, int type, const void *X,
@@ -110,7 +111,7 @@ int psk_moe_experts(int64_t n, int64_t dim, int64_t inter, int64_t experts, int3
     const int st = check_layer(n, dim, inter, experts, top_k, act, type, ldx, ldy);
     if (st != PSK_OK) return st;
     if (ld1 < dim || ld2 < inter || stride1 < 0 || stride2 < 0) return PSK_ERR_SIZE;
-    if (!workspace_ok(workspace, workspace_bytes, moe_workspace_bytes(n, dim, inter, top_k))) return PSK_ERR_WORKSPACE;
+    if (!workspace_ok(workspace, workspace_bytes, moe_workspace_bytes(n, dim, inter, experts, top_k))) return PSK_ERR_WORKSPACE;
     if (n == 0) return PSK_OK;
     if (!X || !crd || !vals || !W1 || !W3 || !W2 || !Y) return PSK_ERR_NULL;
     if (misaligned(X, 2) || misaligned(Y, 2) || misaligned(crd, 4) || misaligned(vals, 4) || misaligned(W1, 16) || misaligned(W3, 16) || misaligned(W2, 16) ||
@@ -135,7 +136,7 @@ int psk_moe_experts_q4(int64_t n, int32_t top_k, int act, int type, const void *
     if (W3->rows != inter || W3->cols != dim || W2->rows != dim || W2->cols != inter || W3->count != experts || W2->count != experts || W3->group != W1->group)
         return PSK_ERR_SIZE;
     if (W3->scale_type != W1->scale_type || W2->scale_type != W1->scale_type) return PSK_ERR_UNSUPPORTED;
-    if (!workspace_ok(workspace, workspace_bytes, moe_workspace_bytes(n, dim, inter, top_k))) return PSK_ERR_WORKSPACE;
+    if (!workspace_ok(workspace, workspace_bytes, moe_workspace_bytes(n, dim, inter, experts, top_k))) return PSK_ERR_WORKSPACE;
     if (n == 0) return PSK_OK;
     if (!X || !crd || !vals || !Y) return PSK_ERR_NULL;
     if (misaligned(X, 2) || misaligned(Y, 2) || misaligned(crd, 4) || misaligned(vals, 4)) return PSK_ERR_ALIGNMENT;

@@ -4,11 +4,14 @@
 //
 // G is a sparse matrix with top_k entries per row (crd, vals); position p = t * top_k + slot.  Bound by reading the matrices of
 // the experts that occur, each once, so the unit of work is (expert that occurs, 16 rows of its matrices) with all positions of
-// that expert: they are the vectors of one set of matrix instructions.  Three launches:
+// that expert: they are the vectors of one set of matrix instructions.  Launches:
+//   k_moe_sort  (more than four tokens) the positions of each expert, and its tokens copied into the order of the operands
 //   k_moe_up    h[p] = act(W1_e x_t) * (W3_e x_t)
 //   k_moe_down  P[p] = W2_e h[p]
 //   k_moe_join  Y(t,:) = sum of G(t,e) P[p] in the order of the slots
-// Every workgroup finds its expert and that one's positions itself from crd (at most kMoePositions of them).
+// (Adding up Y in the last workgroup of its rows that is done saves the last launch, 3 us, but the fences that this takes between
+// dies made k_moe_down five times as slow.)
+// Up to four tokens, every workgroup finds its expert and that one's positions itself from crd.
 //
 // h goes to memory as two 16-bit numbers (Halves): rounding to one of them would cost as much accuracy as rounding Y does, and the
 // second one costs a matrix instruction where the matrix cores wait for memory.
@@ -25,34 +28,44 @@ constexpr int THREADS = 64 * KW;
 
 // ---- which expert, which positions
 struct Found {
-    int expert, count, active;                               // active: experts that occur
+    int expert, count, first, tile;                          // of the j-th expert that occurs: its positions, and those and their tiles of 16 before it
 };
+template <int MOST>
 struct FindSpace {
     int seen[PSK_MOE_MAX_EXPERTS];
     int count;
-    unsigned short list[kMoePositions];
+    unsigned short list[MOST];
 };
 // The j-th expert that occurs (in the order of the experts) and its positions in `list`.  expert -1: fewer occur.
-__device__ __forceinline__ Found find(FindSpace &f, int positions, int experts, const int *__restrict__ crd, int j)
+template <int MOST>
+__device__ __forceinline__ Found find(FindSpace<MOST> &f, int positions, int experts, const int *__restrict__ crd, int j)
 {
     for (int e = threadIdx.x; e < experts; e += THREADS) f.seen[e] = 0;
     if (threadIdx.x == 0) f.count = 0;
     __syncthreads();
     for (int p = threadIdx.x; p < positions; p += THREADS) {
         const int e = crd[p];
-        if ((unsigned)e < (unsigned)experts) f.seen[e] = 1;
+        if ((unsigned)e < (unsigned)experts) atomicAdd(&f.seen[e], 1);
     }
     __syncthreads();
-    Found r = {-1, 0, 0};
+    Found r = {-1, 0, 0, 0};
     const int lane = threadIdx.x & 63;
-    for (int e0 = 0; e0 < experts; e0 += WAVE) {
-        unsigned long long b = __ballot(e0 + lane < experts && f.seen[min(e0 + lane, experts - 1)] != 0);
+    int active = 0;
+    for (int e0 = 0; e0 < experts && r.expert < 0; e0 += WAVE) {
+        const int mine = e0 + lane < experts ? f.seen[e0 + lane] : 0;
+        unsigned long long b = __ballot(mine != 0);
         const int c = __popcll(b);
-        if (r.expert < 0 && j < r.active + c) {
-            for (int skip = j - r.active; skip; --skip) b &= b - 1;
+        unsigned long long before = ~0ull;                   // lanes whose experts come before the j-th
+        if (j < active + c) {
+            for (int skip = j - active; skip; --skip) b &= b - 1;
             r.expert = e0 + __ffsll(b) - 1;
+            before = (1ull << (r.expert - e0)) - 1;
         }
-        r.active += c;
+        active += c;
+        int sum = before >> lane & 1 ? mine | (mine + 15) / 16 << 16 : 0;        // at most kMoePositions of either
+        for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d, WAVE);
+        r.first += sum & 0xffff;
+        r.tile += sum >> 16;
     }
     if (r.expert >= 0) {
         for (int p = threadIdx.x; p < positions; p += THREADS)
@@ -69,125 +82,200 @@ __device__ __forceinline__ float activate(int act, float v)
     return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
 }
 
-struct UpArgs {
+struct Call {
     int n, experts, top_k, dim, inter, act;
     const int *crd;
     const unsigned short *X;
     int64_t ldx;
+    // h: row p with both parts apart by `rest` (few), or the order of the operands (tiles)
     unsigned short *h;
-    int64_t ldh, rest;                                       // rest: from h to the second parts
-};
-struct DownArgs {
-    int n, experts, top_k, dim, inter;
-    const int *crd;
-    const unsigned short *h;
     int64_t ldh, rest;
     float *P;
+    Found *found;                                            // tiles: per slot
+    int *list;                                               // tiles: positions, expert after expert
+    v4u *copy;                                               // tiles: the tokens in the order of the operands
 };
 
-// 16 rows of W1 and of W3 with `count` positions: up to four (NT = 0) or NT tiles of 16.  HT: type of the parts of h.
-template <class SPAN, int HT, int NT, class W>
-__device__ __forceinline__ void up_rows(const UpArgs &a, const W &w1, const W &w3, int expert, const unsigned short *list, int count, int row0, float *lds)
+// ---- up to four tokens
+constexpr int FEW = 4;
+template <class SPAN, int HT, class W>
+__global__ __launch_bounds__(THREADS, 3) void k_moe_up_few(Call a, W w1, W w3)
 {
-    constexpr int V = NT ? 16 : 4, TILES = NT ? NT : 1;
-    int lane = threadIdx.x & 63, cols = a.dim;
-    // what would be the same for the next positions of this expert is not kept for them: it costs more registers than time
-    asm volatile("" : "+v"(lane), "+s"(cols), "+s"(row0));
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, m = lane & 15;
-    SPAN span;
-    span.set(0, w1, expert, min(row0 + m, a.inter - 1), quarter, cols);
-    span.set(1, w3, expert, min(row0 + m, a.inter - 1), quarter, cols);
-    Plain16<SPAN::T> x[TILES];
-    if constexpr (NT == 0) {
-        x[0].set(a.X, list[min(m >> 2, count - 1)] / a.top_k * a.ldx + 32 * (m & 3) + 8 * quarter);
+    __shared__ FindSpace<FEW * PSK_MOE_MAX_TOP_K> f;
+    __shared__ float lds[KW * 128];
+    __shared__ v4u places[KW * EXCHANGE];
+    const Found g = find(f, a.n * a.top_k, a.experts, a.crd, blockIdx.y);
+    if (g.expert < 0) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = blockIdx.x * 16;
+    for (int p0 = 0; p0 < g.count; p0 += 4) {                // more than four: an expert that occurs twice in a row
+        const unsigned short *list = f.list + p0;
+        const int count = g.count - p0;
+        int lane = threadIdx.x & 63, cols = a.dim;
+        // what would be the same for the next positions is not kept for them: it costs more registers than time
+        asm volatile("" : "+v"(lane), "+s"(cols));
+        SPAN span;
+        span.set(0, w1, g.expert, row0, a.inter, lane, cols);
+        span.set(1, w3, g.expert, row0, a.inter, lane, cols);
+        Plain16<SPAN::T> x;
+        x.set(a.X, list[min(lane >> 2 & 3, count - 1)] / a.top_k * a.ldx + few_column<SPAN>(lane));
         float y[2];
-        few_product(span, x[0], cols, wave, KW, lane, y);
+        few_product(span, x, cols, wave, KW, lane, Exchange(places + EXCHANGE * wave, lane), y);
         put_few<2>(lds, wave, lane, y);
-    } else {
+        __syncthreads();
+        const int v = threadIdx.x >> 4, i = threadIdx.x & 15;
+        if (v < 4 && v < count && row0 + i < a.inter) {
+            const float h = activate(a.act, get_sum<KW, 2, 4>(lds, 0, v, i)) * get_sum<KW, 2, 4>(lds, 1, v, i);
+            unsigned short p, q;
+            Halves<HT>::split(h, p, q);
+            const int64_t at = list[v] * a.ldh + row0 + i;
+            a.h[at] = p;
+            a.h[at + a.rest] = q;
+        }
+        __syncthreads();
+    }
+}
+template <class SPAN, class W>
+__global__ __launch_bounds__(THREADS, 3) void k_moe_down_few(Call a, W w2)
+{
+    __shared__ FindSpace<FEW * PSK_MOE_MAX_TOP_K> f;
+    __shared__ float lds[KW * 64];
+    __shared__ v4u places[KW * EXCHANGE];
+    typedef Halves<SPAN::T> H;
+    const Found g = find(f, a.n * a.top_k, a.experts, a.crd, blockIdx.y);
+    if (g.expert < 0) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = blockIdx.x * 16;
+    for (int p0 = 0; p0 < g.count; p0 += 4) {
+        const unsigned short *list = f.list + p0;
+        const int count = g.count - p0;
+        int lane = threadIdx.x & 63, cols = a.inter;
+        asm volatile("" : "+v"(lane), "+s"(cols));
+        SPAN span;
+        span.set(0, w2, g.expert, row0, a.dim, lane, cols);
+        H x;
+        x.set(a.h, list[min(lane >> 2 & 3, count - 1)] * a.ldh + few_column<SPAN>(lane), a.rest);
+        float y[1];
+        few_product(span, x, cols, wave, KW, lane, Exchange(places + EXCHANGE * wave, lane), y);
+        put_few<1>(lds, wave, lane, y);
+        __syncthreads();
+        const int v = threadIdx.x >> 4, i = threadIdx.x & 15;
+        if (v < 4 && v < count && row0 + i < a.dim) a.P[(int64_t)list[v] * a.dim + row0 + i] = get_sum<KW, 1, 4>(lds, 0, v, i) * (1.0f / H::scale);
+        __syncthreads();
+    }
+}
+
+// ---- more tokens: tiles of 16 positions
+// A workgroup per expert that occurs and 4 * COPY_BLOCKS blocks of columns.
+constexpr int COPY_BLOCKS = 4;
+template <class SPAN>
+__global__ __launch_bounds__(THREADS) void k_moe_sort(Call a)
+{
+    __shared__ FindSpace<kMoePositions> f;
+    const Found g = find(f, a.n * a.top_k, a.experts, a.crd, blockIdx.y);
+    if (blockIdx.x == 0) {
+        if (threadIdx.x == 0) a.found[blockIdx.y] = g;
+        if (g.expert >= 0)
+            for (int i = threadIdx.x; i < g.count; i += THREADS) a.list[g.first + i] = f.list[i];
+    }
+    if (g.expert < 0) return;
+    const int lane = threadIdx.x & 63, blocks = copied_blocks(a.dim), b0 = (blockIdx.x * KW + (threadIdx.x >> 6)) * COPY_BLOCKS;
+    for (int t = 0; t < (g.count + 15) / 16; ++t) {
+        Plain16<SPAN::T> x;
+        x.set(a.X, f.list[min(16 * t + (lane & 15), g.count - 1)] / a.top_k * a.ldx);
+        for (int b = b0; b < min(b0 + COPY_BLOCKS, blocks); ++b) copy_block<SPAN>(x, a.dim, b, lane, a.copy + (int64_t)(g.tile + t) * blocks * 64);
+    }
+}
+
+// Where the two parts of column i of h stand in the copy of a tile, for vector m.
+template <bool SPREAD>
+__device__ __forceinline__ int64_t copied_at(int tile, int blocks, int i, int m)
+{
+    const int block = SPREAD ? 4 * (i >> 7) + (i >> 3 & 3) : i >> 5, quarter = SPREAD ? i >> 5 & 3 : i >> 3 & 3;
+    return (((int64_t)tile * blocks + block) * 2 * 64 + 16 * quarter + m) * 8 + (i & 7);
+}
+
+// NT tiles of 16 positions, 16 rows of W1 and of W3; rows past the last one write the zeros that pad the columns of the next step.
+template <class SPAN, int HT, bool SPREAD, int NT, class W>
+__device__ __forceinline__ void up_tiles(const Call &a, const W &w1, const W &w3, const Found &g, int t0, int row0, float *lds, v4u *places)
+{
+    int lane = threadIdx.x & 63, cols = a.dim;
+    asm volatile("" : "+v"(lane), "+s"(cols), "+s"(row0));
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), last = (g.count - 1) >> 4, blocks = copied_blocks(a.dim);
+    if (row0 < a.inter) {
+        SPAN span;
+        span.set(0, w1, g.expert, row0, a.inter, lane, cols);
+        span.set(1, w3, g.expert, row0, a.inter, lane, cols);
+        Copied<Plain16<SPAN::T>> x[NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t) x[t].set(a.X, list[min(16 * t + m, count - 1)] / a.top_k * a.ldx + 8 * quarter);
-        v4f acc[2][TILES], flat[2 * TILES];
-        tile_product<SPAN, TILES>(span, x, cols, wave, KW, lane, acc);
+        for (int t = 0; t < NT; ++t) x[t].set(a.copy, g.tile + min(t0 + t, last), blocks, lane);
+        v4f acc[2][NT], flat[2 * NT];
+        tile_product<SPAN, NT>(span, x, cols, wave, KW, Exchange(places + EXCHANGE * wave, lane), acc);
 #pragma unroll
         for (int t = 0; t < NT; ++t) { flat[t] = acc[0][t]; flat[NT + t] = acc[1][t]; }
-        put_sums<2 * TILES>(lds, wave, lane, flat);
+        put_sums<2 * NT>(lds, wave, lane, flat);
     }
     __syncthreads();
-    for (int o = threadIdx.x; o < TILES * V * 16; o += THREADS) {
-        const int t = o / (V * 16), v = o / 16 % V, i = o & 15;
-        if (V * t + v >= count || row0 + i >= a.inter) continue;
-        const float h = activate(a.act, get_sum<KW, 2 * TILES, V>(lds, t, v, i)) * get_sum<KW, 2 * TILES, V>(lds, TILES + t, v, i);
+    for (int o = threadIdx.x; o < NT * 256; o += THREADS) {
+        const int t = o >> 8, v = o >> 4 & 15, i = o & 15;
+        if (16 * (t0 + t) + v >= g.count) continue;
+        float h = 0;
+        if (row0 + i < a.inter) h = activate(a.act, get_sum<KW, 2 * NT, 16>(lds, t, v, i)) * get_sum<KW, 2 * NT, 16>(lds, NT + t, v, i);
         unsigned short p, q;
         Halves<HT>::split(h, p, q);
-        const int64_t at = list[V * t + v] * a.ldh + row0 + i;
+        const int64_t at = copied_at<SPREAD>(g.tile + t0 + t, copied_blocks(a.inter), row0 + i, v);
         a.h[at] = p;
-        a.h[at + a.rest] = q;
-    }
-}
-
-template <class SPAN, int HT, int MOST, class W>
-__global__ __launch_bounds__(THREADS, 3) void k_moe_up(UpArgs a, W w1, W w3)
-{
-    __shared__ FindSpace f;
-    __shared__ float lds[KW * (MOST ? MOST * 512 : 128)];
-    const Found g = find(f, a.n * a.top_k, a.experts, a.crd, blockIdx.y);
-    if (g.expert < 0) return;
-    const int row0 = blockIdx.x * 16;
-    for (int p0 = 0; p0 < g.count; p0 += MOST ? 16 * MOST : 4) {
-        const int c = g.count - p0;
-        if (MOST < 2 || c <= 16) up_rows<SPAN, HT, (MOST ? 1 : 0)>(a, w1, w3, g.expert, f.list + p0, c, row0, lds);
-        else up_rows<SPAN, HT, MOST>(a, w1, w3, g.expert, f.list + p0, c, row0, lds);
-        __syncthreads();
-    }
-}
-
-// 16 rows of W2 likewise, from both parts of h.
-template <class SPAN, int NT, class W>
-__device__ __forceinline__ void down_rows(const DownArgs &a, const W &w2, int expert, const unsigned short *list, int count, int row0, float *lds)
-{
-    constexpr int V = NT ? 16 : 4, TILES = NT ? NT : 1;
-    typedef Halves<SPAN::T> H;
-    int lane = threadIdx.x & 63, cols = a.inter;
-    // what would be the same for the next positions of this expert is not kept for them: it costs more registers than time
-    asm volatile("" : "+v"(lane), "+s"(cols), "+s"(row0));
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, m = lane & 15;
-    SPAN span;
-    span.set(0, w2, expert, min(row0 + m, a.dim - 1), quarter, cols);
-    H x[TILES];
-    if constexpr (NT == 0) {
-        x[0].set(a.h, list[min(m >> 2, count - 1)] * a.ldh + 32 * (m & 3) + 8 * quarter, a.rest);
-        float y[1];
-        few_product(span, x[0], cols, wave, KW, lane, y);
-        put_few<1>(lds, wave, lane, y);
-    } else {
-#pragma unroll
-        for (int t = 0; t < NT; ++t) x[t].set(a.h, list[min(16 * t + m, count - 1)] * a.ldh + 8 * quarter, a.rest);
-        v4f acc[1][TILES];
-        tile_product<SPAN, TILES>(span, x, cols, wave, KW, lane, acc);
-        put_sums<TILES>(lds, wave, lane, acc[0]);
+        a.h[at + 64 * 8] = q;
     }
     __syncthreads();
-    for (int o = threadIdx.x; o < TILES * V * 16; o += THREADS) {
-        const int t = o / (V * 16), v = o / 16 % V, i = o & 15;
-        if (V * t + v >= count || row0 + i >= a.dim) continue;
-        a.P[(int64_t)list[V * t + v] * a.dim + row0 + i] = get_sum<KW, TILES, V>(lds, t, v, i) * (1.0f / H::scale);
-    }
+}
+template <class SPAN, int HT, bool SPREAD, int MOST, class W>
+__global__ __launch_bounds__(THREADS, 3) void k_moe_up(Call a, W w1, W w3)
+{
+    __shared__ float lds[KW * MOST * 512];
+    __shared__ v4u places[KW * EXCHANGE];
+    const Found g = a.found[blockIdx.y];
+    if (g.expert < 0) return;
+    const int tiles = (g.count + 15) / 16;
+    int t = 0;
+    if constexpr (MOST > 1)
+        for (; t + 1 < tiles; t += MOST) up_tiles<SPAN, HT, SPREAD, MOST>(a, w1, w3, g, t, blockIdx.x * 16, lds, places);
+    for (; t < tiles; ++t) up_tiles<SPAN, HT, SPREAD, 1>(a, w1, w3, g, t, blockIdx.x * 16, lds, places);
 }
 
-template <class SPAN, int MOST, class W>
-__global__ __launch_bounds__(THREADS, 3) void k_moe_down(DownArgs a, W w2)
+template <class SPAN, int NT, class W>
+__device__ __forceinline__ void down_tiles(const Call &a, const W &w2, const Found &g, int t0, int row0, float *lds, v4u *places)
 {
-    __shared__ FindSpace f;
-    __shared__ float lds[KW * (MOST ? MOST * 256 : 64)];
-    const Found g = find(f, a.n * a.top_k, a.experts, a.crd, blockIdx.y);
-    if (g.expert < 0) return;
-    const int row0 = blockIdx.x * 16;
-    for (int p0 = 0; p0 < g.count; p0 += MOST ? 16 * MOST : 4) {
-        const int c = g.count - p0;
-        if (MOST < 2 || c <= 16) down_rows<SPAN, (MOST ? 1 : 0)>(a, w2, g.expert, f.list + p0, c, row0, lds);
-        else down_rows<SPAN, MOST>(a, w2, g.expert, f.list + p0, c, row0, lds);
-        __syncthreads();
+    typedef Halves<SPAN::T> H;
+    int lane = threadIdx.x & 63, cols = a.inter;
+    asm volatile("" : "+v"(lane), "+s"(cols), "+s"(row0));
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), last = (g.count - 1) >> 4, blocks = copied_blocks(a.inter);
+    SPAN span;
+    span.set(0, w2, g.expert, row0, a.dim, lane, cols);
+    Copied<H> x[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) x[t].set(a.h, g.tile + min(t0 + t, last), blocks, lane);
+    v4f acc[1][NT];
+    tile_product<SPAN, NT>(span, x, cols, wave, KW, Exchange(places + EXCHANGE * wave, lane), acc);
+    put_sums<NT>(lds, wave, lane, acc[0]);
+    __syncthreads();
+    for (int o = threadIdx.x; o < NT * 256; o += THREADS) {
+        const int t = o >> 8, v = 16 * (t0 + t) + (o >> 4 & 15), i = o & 15;
+        if (v < g.count && row0 + i < a.dim)
+            a.P[(int64_t)a.list[g.first + v] * a.dim + row0 + i] = get_sum<KW, NT, 16>(lds, t, o >> 4 & 15, i) * (1.0f / H::scale);
     }
+    __syncthreads();
+}
+template <class SPAN, int MOST, class W>
+__global__ __launch_bounds__(THREADS, 3) void k_moe_down(Call a, W w2)
+{
+    __shared__ float lds[KW * MOST * 256];
+    __shared__ v4u places[KW * EXCHANGE];
+    const Found g = a.found[blockIdx.y];
+    if (g.expert < 0) return;
+    const int tiles = (g.count + 15) / 16;
+    int t = 0;
+    if constexpr (MOST > 1)
+        for (; t + 1 < tiles; t += MOST) down_tiles<SPAN, MOST>(a, w2, g, t, blockIdx.x * 16, lds, places);
+    for (; t < tiles; ++t) down_tiles<SPAN, 1>(a, w2, g, t, blockIdx.x * 16, lds, places);
 }
 
 // A lane per element of Y.
@@ -205,44 +293,52 @@ __global__ __launch_bounds__(256) void k_moe_join(int dim, int experts, int top_
     store_as<YT>(Y, t * ldy + i, y);
 }
 
-struct Space {
-    unsigned short *h;
-    float *P;
-    int64_t ldh, rest;
-    size_t bytes;
-};
-Space carve_moe(void *base, int64_t positions, int64_t dim, int64_t inter)
+// Tokens of one set of launches, and their workspace.  Tiles: at most one that is not full per expert that occurs.
+int tokens_at_once(int64_t n, int top_k) { return (int)(n < kMoePositions / top_k ? n : kMoePositions / top_k); }
+size_t carve_moe(const MoeCall &c, Call *a)
 {
-    Space w;
-    w.ldh = (inter + 7) / 8 * 8;
-    const size_t a = align256((size_t)positions * w.ldh * 2), b = align256((size_t)positions * dim * 4);
-    char *p = static_cast<char *>(base);
-    w.h = reinterpret_cast<unsigned short *>(p);
-    w.rest = (int64_t)(a / 2);
-    w.P = reinterpret_cast<float *>(p + 2 * a);
-    w.bytes = 2 * a + b;
-    return w;
+    const int64_t n = tokens_at_once(c.n, c.top_k), positions = n * c.top_k, slots = positions < c.experts ? positions : c.experts;
+    char *p = static_cast<char *>(c.workspace);
+    size_t at = 0;
+    const auto take = [&](size_t bytes) { char *q = p + at; at += align256(bytes); return q; };
+    a->P = reinterpret_cast<float *>(take(positions * c.dim * 4));
+    if (c.n <= FEW) {
+        a->ldh = (c.inter + 7) / 8 * 8;
+        a->rest = (int64_t)(align256(positions * a->ldh * 2) / 2);
+        a->h = reinterpret_cast<unsigned short *>(take(4 * a->rest));
+    } else {
+        const int64_t tiles = positions / 16 + slots;
+        a->h = reinterpret_cast<unsigned short *>(take(tiles * copied_blocks(c.inter) * 2048));
+        a->copy = reinterpret_cast<v4u *>(take(tiles * copied_blocks(c.dim) * 1024));
+        a->found = reinterpret_cast<Found *>(take(slots * sizeof(Found)));
+        a->list = reinterpret_cast<int *>(take(positions * 4));
+    }
+    return at;
 }
 
-// tokens of one pair of launches
-int tokens_at_once(int64_t n, int top_k) { return (int)(n < kMoePositions / top_k ? n : kMoePositions / top_k); }
-
-// UP, DOWN: the spans of the two steps.  MOST: tiles of positions at once, 0: four positions.
-template <class UP, class DOWN, int YT, int MOST, class W>
-hipError_t launch_most(const MoeCall &c, const W &w1, const W &w3, const W &w2, hipStream_t s)
+// The spans of the two steps, for up to four tokens (FEW_*) and for tiles, MOST of them at once.  (The parts of h are in bf16, or weights in 16 bits: no
+// span of the second step takes columns in the order of f16 codes.)
+template <class FEW_UP, class FEW_DOWN, class UP, class DOWN, int MOST, int YT, class W>
+hipError_t launch_layer(const MoeCall &c, const W &w1, const W &w3, const W &w2, hipStream_t s)
 {
+    static_assert(!(DOWN::CODES && DOWN::T == F16), "copied_at");
+    Call a = {0, c.experts, c.top_k, c.dim, c.inter, c.act, nullptr, nullptr, c.ldx, nullptr, 0, 0, nullptr, nullptr, nullptr, nullptr};
+    carve_moe(c, &a);
     const int at_once = tokens_at_once(c.n, c.top_k);
-    const Space w = carve_moe(c.workspace, (int64_t)at_once * c.top_k, c.dim, c.inter);
     for (int64_t t0 = 0; t0 < c.n; t0 += at_once) {
-        const int n = (int)(c.n - t0 < at_once ? c.n - t0 : at_once);
-        const int slots = n * c.top_k < c.experts ? n * c.top_k : c.experts;
-        const int *crd = c.crd + t0 * c.top_k;
-        const UpArgs u = {n, c.experts, c.top_k, c.dim, c.inter, c.act, crd, static_cast<const unsigned short *>(c.X) + t0 * c.ldx, c.ldx, w.h, w.ldh, w.rest};
-        const DownArgs d = {n, c.experts, c.top_k, c.dim, c.inter, crd, w.h, w.ldh, w.rest, w.P};
-        const dim3 up((c.inter + 15) / 16, slots), down((c.dim + 15) / 16, slots);
-        PSK_LAUNCH((k_moe_up<UP, DOWN::T, MOST, W>), up, dim3(THREADS), 0, s, u, w1, w3);
-        PSK_LAUNCH((k_moe_down<DOWN, MOST, W>), down, dim3(THREADS), 0, s, d, w2);
-        PSK_LAUNCH(k_moe_join<YT>, dim3((c.dim + 255) / 256, n), dim3(256), 0, s, c.dim, c.experts, c.top_k, crd, c.vals + t0 * c.top_k, w.P,
+        a.n = (int)(c.n - t0 < at_once ? c.n - t0 : at_once);
+        a.crd = c.crd + t0 * c.top_k;
+        a.X = static_cast<const unsigned short *>(c.X) + t0 * c.ldx;
+        const int slots = a.n * c.top_k < c.experts ? a.n * c.top_k : c.experts, down = (c.dim + 15) / 16;
+        if (c.n <= FEW) {
+            PSK_LAUNCH((k_moe_up_few<FEW_UP, FEW_DOWN::T, W>), dim3((c.inter + 15) / 16, slots), dim3(THREADS), 0, s, a, w1, w3);
+            PSK_LAUNCH((k_moe_down_few<FEW_DOWN, W>), dim3(down, slots), dim3(THREADS), 0, s, a, w2);
+        } else {
+            PSK_LAUNCH((k_moe_sort<UP>), dim3((copied_blocks(c.dim) + KW * COPY_BLOCKS - 1) / (KW * COPY_BLOCKS), slots), dim3(THREADS), 0, s, a);
+            PSK_LAUNCH((k_moe_up<UP, DOWN::T, DOWN::SPREAD, MOST, W>), dim3(copied_blocks(c.inter) * 2, slots), dim3(THREADS), 0, s, a, w1, w3);
+            PSK_LAUNCH((k_moe_down<DOWN, MOST, W>), dim3(down, slots), dim3(THREADS), 0, s, a, w2);
+        }
+        PSK_LAUNCH(k_moe_join<YT>, dim3((c.dim + 255) / 256, a.n), dim3(256), 0, s, c.dim, c.experts, c.top_k, a.crd, c.vals + t0 * c.top_k, a.P,
                    static_cast<unsigned short *>(c.Y) + t0 * c.ldy, c.ldy);
     }
     return take_launch_status();

@@ -7,14 +7,20 @@ namespace {
 template <int T>
 hipError_t launch_16(const MoeCall &c, const Weights16 &w1, const Weights16 &w3, const Weights16 &w2, hipStream_t s)
 {
-    return c.n <= 4 ? launch_most<Span16<T, 2, 4>, Span16<T, 1, 4>, T, 0>(c, w1, w3, w2, s) : launch_most<Span16<T, 2, 2>, Span16<T, 1, 2>, T, 2>(c, w1, w3, w2, s);
+    return launch_layer<Span16<T, 2, 4>, Span16<T, 1, 4>, Span16<T, 2, 2>, Span16<T, 1, 2>, 2, T>(c, w1, w3, w2, s);
 }
 
 }  // namespace
 
-size_t moe_workspace_bytes(int64_t n, int64_t dim, int64_t inter, int top_k)
+size_t moe_workspace_bytes(int64_t n, int64_t dim, int64_t inter, int64_t experts, int top_k)
 {
-    return carve_moe(nullptr, (int64_t)tokens_at_once(n, top_k) * top_k, dim, inter).bytes;
+    // a call with fewer tokens may take the other way: enough for both
+    MoeCall c = {n, (int)dim, (int)inter, (int)experts, top_k, 0, nullptr, 0, nullptr, nullptr, nullptr, 0, nullptr};
+    Call a;
+    const size_t all = carve_moe(c, &a);
+    c.n = n < FEW ? n : FEW;
+    const size_t few = carve_moe(c, &a);
+    return (all > few ? all : few) + 256;
 }
 
 hipError_t launch_moe_16(const MoeCall &c, int type, const void *W1, const void *W3, int64_t ld1, int64_t stride1, const void *W2, int64_t ld2,

@@ -292,11 +292,10 @@ hipError_t launch_mttkrp_main(int64_t dim_k, int64_t dim_l, int32_t nslices, int
 // Types are psk_type.
 struct WeightsQ4;
 template <int XT>
-hipError_t launch_gemm_q4_of(const WeightsQ4 &A, int scale_type, int n, const void *X, int64_t ldx, void *Y, int64_t ldy, hipStream_t s);
+hipError_t launch_gemm_q4_of(const WeightsQ4 &A, int scale_type, int n, const void *X, int64_t ldx, void *Y, int64_t ldy, void *space, hipStream_t s);
 hipError_t launch_moe_route(int n, int dim, int experts, int top_k, int score, int normalise, float factor, int type, const void *X, int64_t ldx,
                             int wtype, const void *W, int64_t ldw, const float *bias, int *crd, float *vals, double *logits, hipStream_t s);
-// Positions of the gating matrix that a pair of launches takes (more tokens go in several pairs): each workgroup of the layer
-// keeps the list of its expert's in LDS.
+// Positions of the gating matrix that a set of launches takes (more tokens go in several): lists of them are kept in LDS.
 constexpr int kMoePositions = 4096;
 struct MoeCall {
     int64_t n;
@@ -309,7 +308,7 @@ struct MoeCall {
     int64_t ldy;
     void *workspace;
 };
-size_t moe_workspace_bytes(int64_t n, int64_t dim, int64_t inter, int top_k);
+size_t moe_workspace_bytes(int64_t n, int64_t dim, int64_t inter, int64_t experts, int top_k);
 hipError_t launch_moe_16(const MoeCall &c, int type, const void *W1, const void *W3, int64_t ld1, int64_t stride1, const void *W2, int64_t ld2,
                          int64_t stride2, hipStream_t s);
 template <int T>

@@ -6,6 +6,16 @@
 // The weights are the second operand, so a lane dequantises, loads the scale of and sums up the same row n.  Vectors past the
 // last one repeat it (their rows of D are not looked at), rows past the last one likewise; only columns need zeros.
 // Sums are held in 32 bits.
+//
+// What bounds these kernels, after memory itself, is how loads are taken apart:
+//  - a load of 16 bytes per lane costs a compute unit 65 cycles where neighbouring lanes read other rows, as the operands' layout would
+//    have them, and 17 to 35 where four and more neighbours read on in one row or all read one place (lines in the L1; 90
+//    cycles per kilobyte is what 7 TB/s leave);
+//  - 134 MB of rows of 4 KB by 16 rows x 64 bytes to a load take 29.9 us, by 8 rows x 128 bytes (whole lines) 25.3, and 21.9 where a
+//    wave reads on for 1 KB in each row before the next wave's part begins; in one piece 21.7.
+// So weights are loaded eight lanes to a row and change places through LDS (Exchange), a wave owns consecutive columns, the
+// scales of several groups are one load, and vectors come four blocks to a load (few of them) or from a copy in the order of the
+// operands (many).
 #pragma once
 #include "psk_dev.h"
 #include <type_traits>
@@ -66,11 +76,36 @@ __device__ __forceinline__ v4u load8(const unsigned short *p, int k, int left)
     return r;
 }
 
+// Two loads of a wave, rows 0 to 7 and 8 to 15 with 128 bytes each, into the order of the operands: for half h of the 128 bytes, row
+// lane % 16, bytes 64 h + 16 (lane / 16).  The place of a piece of 16 bytes within its row is chosen so that neither side's lanes meet on
+// the banks of LDS.
+__device__ __forceinline__ int load_row(int lane, int i) { return 8 * i + (lane >> 3); }
+__device__ __forceinline__ int load_piece(int lane) { return (lane & 7) ^ (lane >> 3); }
+struct Exchange {
+    v4u *put;
+    const v4u *get[2];
+    __device__ __forceinline__ Exchange(v4u *space, int lane) : put(space + lane)
+    {
+        for (int h = 0; h < 2; ++h) get[h] = space + 8 * (lane & 15) + ((4 * h + (lane >> 4)) ^ (lane & 7));
+    }
+    __device__ __forceinline__ void operator()(const v4u (&w)[2], v4u (&out)[2]) const
+    {
+        // LDS operations of one wave are carried out in their order; the compiler is kept from changing it
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        put[0] = w[0];
+        put[64] = w[1];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        out[0] = *get[0];
+        out[1] = *get[1];
+    }
+};
+constexpr int EXCHANGE = 128;                              // v4u of a wave
+
 // ---- vectors
 // Few vectors, up to four: row 4v + j of the first operand is block j (32 columns) of four blocks of vector v, so one load per lane
 // brings four blocks.  The instruction that multiplies it by block j of the weights leaves the product of the two in element j
 // of the lanes of quarter v (and products of blocks that do not belong together in the other elements).
-// Tiles: row m of an operand is vector m of the tile, four loads for four blocks.
+// Tiles: row m of an operand is vector m of the tile; they come from a copy of the vectors in the order of the operands (Copied).
 // A vector may have several parts whose products add up; P of them, the last one with a factor of its own if LO (see Halves).
 template <int T>
 struct Plain16 {                                           // 16 bits
@@ -154,6 +189,29 @@ struct Halves {
         b = __builtin_isfinite(w) ? narrow<T>(r) : (unsigned short)0;
     }
 };
+// The copy: for every tile and block of 32 columns, P kilobytes, one per part, the 16 bytes of lane l at 16 l.  Columns are padded with zeros
+// to a multiple of 256.  spread: the weights of a piece of 128 columns stay as they are loaded, lane quarter q with columns 32 q to 32 q + 31,
+// so block j of the piece is columns 32 q + 8 j; otherwise 32 j + 8 q.
+__host__ __device__ __forceinline__ int copied_blocks(int cols) { return (cols + 255) / 256 * 8; }
+__device__ __forceinline__ int copied_column(int block, int quarter, bool spread)
+{
+    return spread ? 128 * (block >> 2) + 32 * quarter + 8 * (block & 3) : 32 * block + 8 * quarter;
+}
+template <class X>
+struct Copied {
+    typedef X Parts;
+    struct Raw { v4u v[X::P]; };
+    const v4u *p;
+    __device__ __forceinline__ void set(const void *copy, int tile, int blocks, int lane)
+    {
+        p = static_cast<const v4u *>(copy) + (int64_t)tile * blocks * X::P * 64 + lane;
+    }
+    __device__ __forceinline__ void load(Raw &r, int block) const
+    {
+#pragma unroll
+        for (int q = 0; q < X::P; ++q) r.v[q] = p[(block * X::P + q) * 64];
+    }
+};
 // Sum of products of the parts with weights w.
 template <int T, class X>
 __device__ __forceinline__ v4f product(const v4u (&x)[X::P], v4u w, v4f c)
@@ -175,18 +233,20 @@ struct Weights16 {
     int64_t ld, stride;
     int rows, cols;
 };
-// B: blocks of 32 columns in a chunk: four for few vectors, two (a line of 128 bytes per row) for tiles.
+// B: blocks of 32 columns in a chunk: four for few vectors, two for tiles.
 template <int T_, int R_, int B_>
 struct Span16 {
     static constexpr int T = T_, R = R_, B = B_, CH = 32 * B, PIECES = 1;
-    const unsigned short *p[R];
+    static constexpr bool SPREAD = false, CODES = false;
+    const unsigned short *p[R][2];
     int left;                                              // columns from the lane's first one on
-    struct Regs { v4u w[R][B]; };
+    struct Regs { v4u w[R][B / 2][2]; };
     struct Few { v4f d[R][4]; };
-    __device__ __forceinline__ void set(int r, const Weights16 &W, int64_t m, int row, int quarter, int columns)
+    __device__ __forceinline__ void set(int r, const Weights16 &W, int64_t m, int row0, int rows, int lane, int columns)
     {
-        p[r] = W.base + m * W.stride + (int64_t)row * W.ld + 8 * quarter;
-        left = columns - 8 * quarter;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) p[r][i] = W.base + m * W.stride + (int64_t)min(row0 + load_row(lane, i), rows - 1) * W.ld + 8 * load_piece(lane);
+        left = columns - 8 * load_piece(lane);
     }
     template <bool TAIL>
     __device__ __forceinline__ void load(Regs &g, int c) const
@@ -194,8 +254,23 @@ struct Span16 {
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int j = 0; j < B; ++j)
-                g.w[r][j] = TAIL ? load8(p[r], c * CH + 32 * j, left) : __builtin_nontemporal_load(reinterpret_cast<const v4u *>(p[r] + c * CH + 32 * j));
+            for (int u = 0; u < B / 2; ++u)
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    g.w[r][u][i] = TAIL ? load8(p[r][i], c * CH + 64 * u, left)
+                                        : __builtin_nontemporal_load(reinterpret_cast<const v4u *>(p[r][i] + c * CH + 64 * u));
+    }
+    static __device__ __forceinline__ void exchange(const Regs &g, const Exchange &place, v4u (&all)[R][B])
+    {
+#pragma unroll
+        for (int u = 0; u < B / 2; ++u)
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                v4u o[2];
+                place(g.w[r][u], o);
+                all[r][2 * u] = o[0];
+                all[r][2 * u + 1] = o[1];
+            }
     }
     static __device__ __forceinline__ void clear(Few &f)
     {
@@ -206,35 +281,38 @@ struct Span16 {
     }
     static __device__ __forceinline__ float finish(const Few &f, int r) { return (f.d[r][0][0] + f.d[r][1][1]) + (f.d[r][2][2] + f.d[r][3][3]); }
     template <bool TAIL, class X>
-    __device__ __forceinline__ void few(const Regs &g, int, const typename X::Raw (&raw)[PIECES], Few &f) const
+    __device__ __forceinline__ void few(const Regs &g, int, const Exchange &place, const typename X::Raw (&raw)[PIECES], Few &f) const
     {
         static_assert(B == 4, "four blocks");
         v4u x[X::P];
         X::operands(raw[0], x);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int r = 0; r < R; ++r) f.d[r][j] = product<T, X>(x, g.w[r][j], f.d[r][j]);
+            for (int r = 0; r < R; ++r) {
+                v4u w[2];
+                place(g.w[r][u], w);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) f.d[r][2 * u + j] = product<T, X>(x, w[j], f.d[r][2 * u + j]);
+            }
     }
     template <bool TAIL, int NT, class X>
-    __device__ __forceinline__ void tiles(const Regs &g, int, const typename X::Raw (&raw)[NT][B], v4f (&acc)[R][NT]) const
+    __device__ __forceinline__ void tiles(const Regs &, int, int, const v4u (&all)[R][B], const typename Copied<X>::Raw (&raw)[NT][B], v4f (&acc)[R][NT]) const
     {
 #pragma unroll
         for (int j = 0; j < B; ++j)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                v4u x[X::P];
-                X::operands(raw[t][j], x);
+            for (int r = 0; r < R; ++r)
 #pragma unroll
-                for (int r = 0; r < R; ++r) acc[r][t] = product<T, X>(x, g.w[r][j], acc[r][t]);
-            }
+                for (int t = 0; t < NT; ++t) acc[r][t] = product<T, X>(raw[t][j].v, all[r][j], acc[r][t]);
     }
 };
 
 // ---- weights of 4 bits
-// A row of codes is two columns to a byte, the low half first.  A lane loads 16 bytes, so the four quarters of a wave hold 32
-// columns each; swapping words between the quarters (a 4 x 4 transposition, four instructions) leaves the words that one
-// matrix instruction takes, its 32 columns in order, in one register.
+// A row of codes is two columns to a byte, the low half first.  A lane loads 16 bytes, so after the exchange the four quarters of a wave
+// hold 32 columns each.  With groups of 128 columns and more the operands take them so (SPREAD); with smaller ones a matrix
+// instruction may not reach over the quarters, and swapping words between them (a 4 x 4 transposition, four instructions) leaves the
+// words of 32 columns in one register.
 struct WeightsQ4 {
     const unsigned char *codes, *zeros;                   // zeros NULL: 8
     const void *scales;
@@ -303,33 +381,37 @@ __device__ __forceinline__ v4u code_order(v4u x)           // eight elements in 
 // N scales or zero points that lie side by side, as one load.
 template <typename E, int N> struct Run { typedef E type __attribute__((ext_vector_type(N), aligned(sizeof(E)))); };
 
-// P: pieces of 128 columns in a chunk; two read whole lines of 128 bytes per row.  GB: blocks of 32 columns that share a scale: 1, 2 and
-// 4 for groups of just 32, 64 and 128 columns (then the scales of a chunk are one load), 8 for larger ones; 4 also for those if P is 1.
+// P: pieces of 128 columns in a chunk, two to a line of 128 bytes per row.  GB: blocks of 32 columns that share a scale: 1, 2 and 4 for
+// groups of just 32, 64 and 128 columns (then the scales of a chunk are one load), 4 P for groups of a chunk and more.
 // S: type of the scales.  T: type of the operands.  Z: some matrix has zero points; one that has none reads its codes in
 // their place and puts 8 for what it read, so that no load stands under a condition.
 template <int T_, int R_, int P, int GB, int S, bool Z>
 struct SpanQ4 {
+    static constexpr bool SPREAD = GB >= 4, CODES = true;
     static constexpr int T = T_, R = R_, B = 4 * P, CH = 32 * B, PIECES = P, NG = 4 * P > GB ? 4 * P / GB : 1, PER = GB < 4 ? GB : 4;     // PER: blocks of a piece that share one
     typedef typename std::conditional<S == F32, float, unsigned short>::type Scale;
     typedef typename Run<Scale, NG>::type Scales;
     typedef typename Run<unsigned char, NG>::type Zeros;
-    const unsigned char *q[R], *z[R];
+    const unsigned char *q[R][2], *z[R];
     const Scale *s[R];
     int cols, offset, shift[R];
     unsigned zmask[R], zelse[R];
-    struct Regs { v4u w[R][P]; Scales s[R]; Zeros z[Z ? R : 1]; };
+    struct Regs { v4u w[R][P / 2][2]; Scales s[R]; Zeros z[Z ? R : 1]; };
     struct Few { float y[R]; };
-    __device__ __forceinline__ void set(int r, const WeightsQ4 &W, int64_t m, int row, int quarter, int columns)
+    __device__ __forceinline__ void set(int r, const WeightsQ4 &W, int64_t m, int row0, int rows, int lane, int columns)
     {
-        q[r] = W.codes + m * W.stride_codes + (int64_t)row * W.ld_codes + 16 * quarter;
-        const int64_t at = m * W.stride_scales + (int64_t)row * W.ld_scales;
+        const unsigned char *codes = W.codes + m * W.stride_codes;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) q[r][i] = codes + (int64_t)min(row0 + load_row(lane, i), rows - 1) * W.ld_codes + 16 * load_piece(lane);
+        const int row = min(row0 + (lane & 15), rows - 1);
+        const int64_t at = m * W.stride_scales + row * W.ld_scales;
         s[r] = static_cast<const Scale *>(W.scales) + at;
-        z[r] = W.zeros ? W.zeros + at : q[r] - 16 * quarter;
+        z[r] = W.zeros ? W.zeros + at : codes + row * W.ld_codes;
         zmask[r] = W.zeros ? 255 : 0;
         zelse[r] = W.zeros ? 0 : 8;
         cols = columns;
         shift[r] = W.shift;
-        offset = 32 * quarter;
+        offset = 32 * load_piece(lane);
     }
     // Nothing is computed from what is loaded, so that it can be requested a chunk ahead.
     template <bool TAIL>
@@ -338,11 +420,13 @@ struct SpanQ4 {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
 #pragma unroll
-            for (int h = 0; h < P; ++h) {
-                if constexpr (TAIL) g.w[r][h] = v4u{0, 0, 0, 0};
-                if (!TAIL || c * CH + 128 * h + offset < cols)
-                    g.w[r][h] = __builtin_nontemporal_load(reinterpret_cast<const v4u *>(q[r] + c * (CH / 2) + 64 * h));
-            }
+            for (int u = 0; u < P / 2; ++u)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if constexpr (TAIL) g.w[r][u][i] = v4u{0, 0, 0, 0};
+                    if (!TAIL || c * CH + 256 * u + offset < cols)
+                        g.w[r][u][i] = __builtin_nontemporal_load(reinterpret_cast<const v4u *>(q[r][i] + c * (CH / 2) + 128 * u));
+                }
             if constexpr (TAIL) {
 #pragma unroll
                 for (int i = 0; i < NG; ++i) {
@@ -362,6 +446,19 @@ struct SpanQ4 {
         if constexpr (Z) return Zero<T>((int)((g.z[r][i] & zmask[r]) | zelse[r]));
         else return Zero<T>(8);
     }
+    static __device__ __forceinline__ void exchange(const Regs &g, const Exchange &place, v4u (&all)[R][P])
+    {
+#pragma unroll
+        for (int u = 0; u < P / 2; ++u)
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                v4u o[2];
+                place(g.w[r][u], o);
+                all[r][2 * u] = o[0];
+                all[r][2 * u + 1] = o[1];
+            }
+    }
+    static __device__ __forceinline__ v4u words(v4u w) { return SPREAD ? w : transpose_quarters(w); }
     static __device__ __forceinline__ float factor(Scale v)
     {
         float f;
@@ -377,8 +474,10 @@ struct SpanQ4 {
     static __device__ __forceinline__ float finish(const Few &f, int r) { return f.y[r]; }
     // A block past the last column counts nothing: its sum is zero, and so has the scale to be (it could be infinite).
     template <bool TAIL, class X>
-    __device__ __forceinline__ void few(const Regs &g, int c, const typename X::Raw (&raw)[PIECES], Few &f) const
+    __device__ __forceinline__ void few(const Regs &g, int c, const Exchange &place, const typename X::Raw (&raw)[PIECES], Few &f) const
     {
+        v4u all[R][P];
+        exchange(g, place, all);
 #pragma unroll
         for (int h = 0; h < P; ++h) {
             v4u x[X::P];
@@ -387,7 +486,7 @@ struct SpanQ4 {
             for (int q = 0; q < X::P; ++q) x[q] = code_order<T>(x[q]);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                const v4u w = transpose_quarters(g.w[r][h]);
+                const v4u w = words(all[r][h]);
 #pragma unroll
                 for (int i = 0; i < 4 / PER; ++i) {
                     const int at = 4 * h / GB + i;
@@ -404,15 +503,16 @@ struct SpanQ4 {
             }
         }
     }
+    // Piece h of the chunk, whose words are in `all`.
     template <bool TAIL, int NT, class X>
-    __device__ __forceinline__ void tiles(const Regs &g, int c, const typename X::Raw (&raw)[NT][4], v4f (&acc)[R][NT]) const
+    __device__ __forceinline__ void tiles(const Regs &g, int c, int h, const v4u (&all)[R][P], const typename Copied<X>::Raw (&raw)[NT][4], v4f (&acc)[R][NT]) const
     {
-        static_assert(P == 1, "one piece");
         v4u w[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) w[r] = transpose_quarters(g.w[r][0]);
+        for (int r = 0; r < R; ++r) w[r] = words(all[r][h]);
 #pragma unroll
         for (int i = 0; i < 4 / PER; ++i) {
+            const int at = 4 * h / GB + i;
             v4f sum[R][NT];
 #pragma unroll
             for (int r = 0; r < R; ++r)
@@ -423,20 +523,15 @@ struct SpanQ4 {
                 const int j = i * PER + b;
                 v4u wv[R];
 #pragma unroll
-                for (int r = 0; r < R; ++r) wv[r] = dequantise(w[r][j], zero(g, r, i));
+                for (int r = 0; r < R; ++r) wv[r] = dequantise(w[r][j], zero(g, r, at));
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    v4u x[X::P];
-                    X::operands(raw[t][j], x);
+                for (int t = 0; t < NT; ++t)
 #pragma unroll
-                    for (int q = 0; q < X::P; ++q) x[q] = code_order<T>(x[q]);
-#pragma unroll
-                    for (int r = 0; r < R; ++r) sum[r][t] = product<T, X>(x, wv[r], sum[r][t]);
-                }
+                    for (int r = 0; r < R; ++r) sum[r][t] = product<T, X>(raw[t][j].v, wv[r], sum[r][t]);
             }
 #pragma unroll
             for (int r = 0; r < R; ++r) {
-                const float f = !TAIL || c * CH + 32 * PER * i < cols ? factor(g.s[r][i]) : 0.0f;
+                const float f = !TAIL || c * CH + 128 * h + 32 * PER * i < cols ? factor(g.s[r][at]) : 0.0f;
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -446,77 +541,138 @@ struct SpanQ4 {
     }
 };
 
-// Chunks first, first + step, ... of the columns, weights and vectors requested a chunk ahead.  The last chunk, if it is
-// not whole, comes after the others and is the only one whose loads look at where the columns end.
-template <class SPAN, class LOAD, class APPLY>
-__device__ __forceinline__ void chunks(int cols, int first, int step, LOAD load, APPLY apply)
+// A wave's share of the columns: chunks from `first` to before `end`, all whole but the last one of the matrix.
+struct Share { int first, end, whole; };
+template <class SPAN>
+__device__ __forceinline__ Share share_of(int cols, int wave, int waves)
 {
-    const int whole = cols / SPAN::CH;
-    int c = first;
-    if (c >= whole) return;
-    load(0, c);
-    for (;;) {                                             // no load stands under a condition: waiting for one would wait for all
-        if (c + step >= whole) { apply(0, c); return; }
-        load(1, c + step);
-        apply(0, c);
-        c += step;
-        if (c + step >= whole) { apply(1, c); return; }
-        load(0, c + step);
-        apply(1, c);
-        c += step;
-    }
+    const int n = (cols + SPAN::CH - 1) / SPAN::CH;
+    Share s;
+    s.first = n * wave / waves;
+    s.end = n * (wave + 1) / waves;
+    s.whole = min(s.end, cols / SPAN::CH);
+    return s;
 }
+
+// The lane's first column of few vectors, counted from the chunk's.
+template <class SPAN>
+__device__ __forceinline__ int few_column(int lane) { return copied_column(lane & 3, lane >> 4, SPAN::SPREAD); }
+
+// Weights and vectors are requested a chunk ahead.  The matrix's last chunk, if it is not whole, is the only one whose loads look at where
+// the columns end.  (No load stands under a condition inside the loops: waiting for one would wait for all.)
 template <class SPAN, class X>
-__device__ __forceinline__ void few_product(const SPAN &s, const X &x, int cols, int first, int step, int lane, float (&y)[SPAN::R])
+__device__ __forceinline__ void few_product(const SPAN &s, const X &x, int cols, int wave, int waves, int lane, const Exchange &place, float (&y)[SPAN::R])
 {
     typename SPAN::Regs g[2];
     typename X::Raw raw[2][SPAN::PIECES];
     typename SPAN::Few f;
     SPAN::clear(f);
-    const int xleft = cols - 32 * (lane & 3) - 8 * (lane >> 4), whole = cols / SPAN::CH;
-    chunks<SPAN>(cols, first, step,
-        [&](int b, int c) {
-            s.template load<false>(g[b], c);
+    const Share sh = share_of<SPAN>(cols, wave, waves);
+    const int left = cols - few_column<SPAN>(lane);
+    const auto load = [&](int b, int c) {
+        s.template load<false>(g[b], c);
 #pragma unroll
-            for (int h = 0; h < SPAN::PIECES; ++h) x.template load<false>(raw[b][h], c * SPAN::CH + 128 * h, xleft);
-        },
-        [&](int b, int c) { s.template few<false, X>(g[b], c, raw[b], f); });
-    if (whole * SPAN::CH < cols && whole % step == first) {
-        s.template load<true>(g[0], whole);
+        for (int h = 0; h < SPAN::PIECES; ++h) x.template load<false>(raw[b][h], c * SPAN::CH + 128 * h, left);
+    };
+    const auto apply = [&](int b, int c) { s.template few<false, X>(g[b], c, place, raw[b], f); };
+    int c = sh.first;
+    if (c < sh.whole) {
+        load(0, c);
+        for (;;) {
+            if (c + 1 >= sh.whole) { apply(0, c++); break; }
+            load(1, c + 1);
+            apply(0, c++);
+            if (c + 1 >= sh.whole) { apply(1, c++); break; }
+            load(0, c + 1);
+            apply(1, c++);
+        }
+    }
+    if (c < sh.end) {
+        s.template load<true>(g[0], c);
 #pragma unroll
-        for (int h = 0; h < SPAN::PIECES; ++h) x.template load<true>(raw[0][h], whole * SPAN::CH + 128 * h, xleft);
-        s.template few<true, X>(g[0], whole, raw[0], f);
+        for (int h = 0; h < SPAN::PIECES; ++h) x.template load<true>(raw[0][h], c * SPAN::CH + 128 * h, left);
+        s.template few<true, X>(g[0], c, place, raw[0], f);
     }
 #pragma unroll
     for (int r = 0; r < SPAN::R; ++r) y[r] = SPAN::finish(f, r);
 }
+// The same for tiles.  Vectors are requested by pieces: those of a chunk's first piece while the one before it is multiplied, the others ahead
+// of the next chunk's weights, so that waiting for them does not wait for these.
 template <class SPAN, int NT, class X>
-__device__ __forceinline__ void tile_product(const SPAN &s, const X (&x)[NT], int cols, int first, int step, int lane, v4f (&acc)[SPAN::R][NT])
+__device__ __forceinline__ void tile_product(const SPAN &s, const Copied<X> (&x)[NT], int cols, int wave, int waves, const Exchange &place, v4f (&acc)[SPAN::R][NT])
 {
+    constexpr int PB = SPAN::B / SPAN::PIECES, N = SPAN::PIECES > 1 ? SPAN::PIECES : 2;      // blocks of a piece, sets of registers for pieces
     typename SPAN::Regs g[2];
-    typename X::Raw raw[2][NT][SPAN::B];
+    typename Copied<X>::Raw raw[N][NT][PB];
+    v4u all[SPAN::R][SPAN::PIECES > 1 ? SPAN::PIECES : SPAN::B];
 #pragma unroll
     for (int r = 0; r < SPAN::R; ++r)
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[r][t] = v4f{0, 0, 0, 0};
-    const int xleft = cols - 8 * (lane >> 4), whole = cols / SPAN::CH;
-    chunks<SPAN>(cols, first, step,
-        [&](int b, int c) {
-            s.template load<false>(g[b], c);
+    const Share sh = share_of<SPAN>(cols, wave, waves);
+    const auto vectors = [&](int set, int c, int h) {
 #pragma unroll
-            for (int j = 0; j < SPAN::B; ++j)
+        for (int j = 0; j < PB; ++j)
 #pragma unroll
-                for (int t = 0; t < NT; ++t) x[t].template load<false>(raw[b][t][j], c * SPAN::CH + 32 * j, xleft);
-        },
-        [&](int b, int c) { s.template tiles<false, NT, X>(g[b], c, raw[b], acc); });
-    if (whole * SPAN::CH < cols && whole % step == first) {
-        s.template load<true>(g[0], whole);
+            for (int t = 0; t < NT; ++t) x[t].load(raw[set][t][j], c * SPAN::B + h * PB + j);
+    };
+    const auto rest = [&](int c) {
 #pragma unroll
-        for (int j = 0; j < SPAN::B; ++j)
+        for (int h = 1; h < SPAN::PIECES; ++h) vectors(h, c, h);
+    };
+    const auto multiply_rest = [&](int b, int c) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t) x[t].template load<true>(raw[0][t][j], whole * SPAN::CH + 32 * j, xleft);
-        s.template tiles<true, NT, X>(g[0], whole, raw[0], acc);
+        for (int h = 1; h < SPAN::PIECES; ++h) s.template tiles<false, NT, X>(g[b], c, h, all, raw[h], acc);
+    };
+    const auto step = [&](int b, int c) {                  // chunk c, another one after it
+        const int set = SPAN::PIECES > 1 ? 0 : b, next = SPAN::PIECES > 1 ? 0 : 1 - b;
+        rest(c);
+        s.template load<false>(g[1 - b], c + 1);
+        if (SPAN::PIECES == 1) vectors(next, c + 1, 0);
+        SPAN::exchange(g[b], place, all);
+        s.template tiles<false, NT, X>(g[b], c, 0, all, raw[set], acc);
+        if (SPAN::PIECES > 1) vectors(next, c + 1, 0);
+        multiply_rest(b, c);
+    };
+    const auto last = [&](int b, int c) {
+        rest(c);
+        SPAN::exchange(g[b], place, all);
+        s.template tiles<false, NT, X>(g[b], c, 0, all, raw[SPAN::PIECES > 1 ? 0 : b], acc);
+        multiply_rest(b, c);
+    };
+    int c = sh.first;
+    if (c < sh.whole) {
+        s.template load<false>(g[0], c);
+        vectors(0, c, 0);
+        for (;;) {
+            if (c + 1 >= sh.whole) { last(0, c++); break; }
+            step(0, c++);
+            if (c + 1 >= sh.whole) { last(1, c++); break; }
+            step(1, c++);
+        }
     }
+    if (c < sh.end) {
+        s.template load<true>(g[0], c);
+        SPAN::exchange(g[0], place, all);
+#pragma unroll
+        for (int h = 0; h < SPAN::PIECES; ++h) {
+            vectors(0, c, h);
+            s.template tiles<true, NT, X>(g[0], c, h, all, raw[0], acc);
+        }
+    }
+}
+
+// One lane's part of the copy: block `block` of the row that x points at.
+template <class SPAN, class X>
+__device__ __forceinline__ void copy_block(const X &x, int cols, int block, int lane, v4u *tile)
+{
+    const int k = copied_column(block, lane >> 4, SPAN::SPREAD);
+    typename X::Raw raw;
+    x.template load<true>(raw, k, cols);
+    v4u v[X::P];
+    X::operands(raw, v);
+#pragma unroll
+    for (int q = 0; q < X::P; ++q) tile[(block * X::P + q) * 64 + lane] = SPAN::CODES ? code_order<SPAN::T>(v[q]) : v[q];
 }
 
 // Sums of the W waves of a workgroup, in the order of the waves.  Tiles: 16 vectors x 16 rows each; few vectors: 4 x 16.
