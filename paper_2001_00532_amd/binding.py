@@ -53,7 +53,7 @@ class psk_slab(ctypes.Structure):
 PSK_F32, PSK_F16, PSK_BF16 = 0, 1, 2
 PSK_SCORE_SOFTMAX, PSK_SCORE_SIGMOID = 0, 1
 PSK_ACT_SILU, PSK_ACT_GELU = 0, 1
-PSK_MAX_VECTORS, PSK_MOE_MAX_EXPERTS, PSK_MOE_MAX_TOP_K = 1 << 20, 1024, 64
+PSK_MAX_VECTORS, PSK_MOE_MAX_EXPERTS, PSK_MOE_MAX_TOP_K = 1 << 19, 1024, 64
 
 
 class psk_q4(ctypes.Structure):

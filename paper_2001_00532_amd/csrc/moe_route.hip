@@ -9,149 +9,202 @@
 namespace psk {
 namespace {
 
-constexpr int ROUTE_TOKENS = 8;      // tokens of a workgroup
-constexpr int ROUTE_WAVES = 4;
+typedef unsigned v2u __attribute__((ext_vector_type(2)));
 
+constexpr int THREADS = 256;
+
+// Eight elements from column k on as 64-bit numbers, zeros from column `cols` on.
 template <int T>
-__device__ __forceinline__ double element(const void *p, int64_t i)
+__device__ __forceinline__ void load_wide(const void *p, int64_t row, int k, int cols, double (&d)[8])
 {
-    if constexpr (T == F32) return (double)static_cast<const float *>(p)[i];
-    else return (double)widen<T>(static_cast<const unsigned short *>(p)[i]);
-}
-__device__ __forceinline__ double wave_sum64(double v)
-{
+    if constexpr (T == F32) {
+        const float *q = static_cast<const float *>(p) + row;
+        if (k + 8 <= cols) {
+            const v4f_e a = *reinterpret_cast<const v4f_e *>(q + k), b = *reinterpret_cast<const v4f_e *>(q + k + 4);
 #pragma unroll
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d, WAVE);
-    return v;
+            for (int i = 0; i < 4; ++i) { d[i] = a[i]; d[4 + i] = b[i]; }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) d[i] = k + i < cols ? q[k + i] : 0.0f;
+        }
+    } else {
+        const v4u v = load8(static_cast<const unsigned short *>(p) + row, k, cols);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] = widen<T>((unsigned short)(v[i / 2] >> 16 * (i & 1)));
+    }
 }
 
-// One expert, up to ROUTE_TOKENS tokens; the waves share the columns.
-template <int XT, int WT>
-__global__ __launch_bounds__(64 * ROUTE_WAVES) void k_route_logits(int n, int dim, int experts, const void *X, int64_t ldx, const void *W, int64_t ldw,
-                                                                    double *logits)
+// Sums over lanes; the exchanges are in registers (LDS takes a hundred cycles for each of twelve).
+template <int CTRL>
+__device__ __forceinline__ double dpp64(double v)
 {
-    __shared__ double part[ROUTE_WAVES][ROUTE_TOKENS];
-    const int e = blockIdx.x % experts, t0 = blockIdx.x / experts * ROUTE_TOKENS, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int nt = min(ROUTE_TOKENS, n - t0);
-    double acc[ROUTE_TOKENS] = {};
-    for (int j = threadIdx.x; j < dim; j += 64 * ROUTE_WAVES) {
-        const double w = element<WT>(W, e * ldw + j);
+    const v2u u = __builtin_bit_cast(v2u, v);
+    return __builtin_bit_cast(double, v2u{(unsigned)__builtin_amdgcn_update_dpp(0, (int)u[0], CTRL, 0xF, 0xF, true),
+                                          (unsigned)__builtin_amdgcn_update_dpp(0, (int)u[1], CTRL, 0xF, 0xF, true)});
+}
+// Lanes l and l ^ 32 (l ^ 16): a of the lower ones and b of the upper ones are put together.
+template <int D>
+__device__ __forceinline__ void halves64(double a, double b, double &x, double &y)
+{
+    const v2u u = __builtin_bit_cast(v2u, a), v = __builtin_bit_cast(v2u, b);
+    v2u p, q;
 #pragma unroll
-        for (int t = 0; t < ROUTE_TOKENS; ++t)
-            if (t < nt) acc[t] = fma(w, element<XT>(X, (t0 + t) * ldx + j), acc[t]);
+    for (int i = 0; i < 2; ++i) {
+        if constexpr (D == 32) {
+            auto r = __builtin_amdgcn_permlane32_swap(u[i], v[i], false, false);
+            p[i] = r[0];
+            q[i] = r[1];
+        } else {
+            auto r = __builtin_amdgcn_permlane16_swap(u[i], v[i], false, false);
+            p[i] = r[0];
+            q[i] = r[1];
+        }
+    }
+    x = __builtin_bit_cast(double, p);
+    y = __builtin_bit_cast(double, q);
+}
+template <class OP>
+__device__ __forceinline__ double row_all(double v, OP op)      // over 16 lanes
+{
+    v = op(v, dpp64<0xB1>(v));
+    v = op(v, dpp64<0x4E>(v));
+    v = op(v, dpp64<0x141>(v));
+    return op(v, dpp64<0x140>(v));
+}
+template <class OP>
+__device__ __forceinline__ double wave_all(double v, OP op)
+{
+    double x, y;
+    v = row_all(v, op);
+    halves64<16>(v, v, x, y);
+    v = op(x, y);
+    halves64<32>(v, v, x, y);
+    return op(x, y);
+}
+
+// EB experts by TB tokens; the threads share the columns, eight at a time.
+template <int XT, int WT, int EB, int TB>
+__global__ __launch_bounds__(THREADS) void k_route_logits(int n, int dim, int experts, const void *X, int64_t ldx, const void *W, int64_t ldw,
+                                                           double *logits)
+{
+    constexpr int N = EB * TB, M = N / 4;
+    static_assert(N % 4 == 0, "a quarter of the sums to each row of lanes");
+    __shared__ double part[THREADS / WAVE][N];
+    const int groups = (experts + EB - 1) / EB, e0 = blockIdx.x % groups * EB, t0 = blockIdx.x / groups * TB, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    double acc[N] = {};
+    for (int k = 8 * threadIdx.x; k < dim; k += 8 * THREADS) {
+        double w[EB][8];
+#pragma unroll
+        for (int e = 0; e < EB; ++e) load_wide<WT>(W, min(e0 + e, experts - 1) * ldw, k, dim, w[e]);
+#pragma unroll
+        for (int t = 0; t < TB; ++t) {
+            double x[8];
+            load_wide<XT>(X, min(t0 + t, n - 1) * ldx, k, dim, x);
+#pragma unroll
+            for (int e = 0; e < EB; ++e)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) acc[e * TB + t] = fma(w[e][i], x[i], acc[e * TB + t]);
+        }
+    }
+    // lanes 0-15 sum up numbers 0 .. M-1, 16-31 M .. 2M-1, ...
+    double two[N / 2], one[M];
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+        double x, y;
+        halves64<32>(acc[i], acc[i + N / 2], x, y);
+        two[i] = x + y;
     }
 #pragma unroll
-    for (int t = 0; t < ROUTE_TOKENS; ++t) {
-        const double v = wave_sum64(acc[t]);
-        if (lane == 0) part[wave][t] = v;
+    for (int i = 0; i < M; ++i) {
+        double x, y;
+        halves64<16>(two[i], two[i + M], x, y);
+        one[i] = row_all(x + y, [](double a, double b) { return a + b; });
+    }
+    if ((lane & 15) == 0) {
+#pragma unroll
+        for (int i = 0; i < M; ++i) part[wave][(lane >> 4) * M + i] = one[i];
     }
     __syncthreads();
-    if ((int)threadIdx.x < nt) {
+    for (int i = threadIdx.x; i < N; i += THREADS) {
+        const int e = e0 + i / TB, t = t0 + i % TB;
         double v = 0;
-        for (int w = 0; w < ROUTE_WAVES; ++w) v += part[w][threadIdx.x];
-        logits[(int64_t)(t0 + threadIdx.x) * experts + e] = v;
+        for (int w = 0; w < THREADS / WAVE; ++w) v += part[w][i];
+        if (e < experts && t < n) logits[(int64_t)t * experts + e] = v;
     }
 }
 
-// a before b in the order of choice: larger key, then lower index; a key that is no number comes after all others.
-__device__ __forceinline__ bool before(double ka, int ia, double kb, int ib)
-{
-    const bool na = ka != ka, nb = kb != kb;
-    if (na != nb) return nb;
-    if (!na && ka != kb) return ka > kb;
-    return ia < ib;
-}
-
-// A wave per token; lane l has experts l, l + 64, ..., PER of them.
-template <int SCORE, int PER>
-__global__ __launch_bounds__(64) void k_route_choose(int experts, int top_k, int normalise, float factor, const double *logits, const float *bias,
-                                                      int *crd, float *vals)
-{
-    constexpr int NONE = 0x7fffffff;
-    const int lane = threadIdx.x;
-    const int64_t t = blockIdx.x;
-    const double *row = logits + t * experts;
-    double key[PER], p[PER];
-    unsigned open = 0;                                       // experts of this lane that may be chosen
-    double top = -INFINITY, sum = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int e = lane + WAVE * i;
-        key[i] = p[i] = 0;
-        if (e < experts) {
-            p[i] = row[e];
-            if (!bias || !(bias[e] == -INFINITY)) open |= 1u << i;
-            top = p[i] != p[i] ? p[i] : (p[i] > top ? p[i] : top);
-        }
-    }
-    if constexpr (SCORE == PSK_SCORE_SOFTMAX) {
-#pragma unroll
-        for (int d = 32; d; d >>= 1) {
-            const double o = __shfl_xor(top, d, WAVE);
-            top = o > top || o != o ? o : top;
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-        const int e = lane + WAVE * i;
-        if (e >= experts) continue;
-        key[i] = p[i];
-        p[i] = SCORE == PSK_SCORE_SOFTMAX ? exp(p[i] - top) : 1.0 / (1.0 + exp(-p[i]));
-        sum += p[i];
-    }
-    if constexpr (SCORE == PSK_SCORE_SOFTMAX) {
-        sum = wave_sum64(sum);
-#pragma unroll
-        for (int i = 0; i < PER; ++i) p[i] /= sum;
-    }
-    if (bias) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i)
-            if (lane + WAVE * i < experts) key[i] = p[i] + (double)bias[lane + WAVE * i];
-    }
-    double gate = 0, total = 0;                              // lane s keeps entry s
-    int mine = -1;
-    for (int s = 0; s < top_k; ++s) {
-        double bk = 0, bp = 0;
-        int bi = NONE;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            const int e = lane + WAVE * i;
-            if ((open >> i & 1) && (bi == NONE || before(key[i], e, bk, bi))) { bk = key[i]; bp = p[i]; bi = e; }
-        }
-#pragma unroll
-        for (int d = 32; d; d >>= 1) {
-            const double ok = __shfl_xor(bk, d, WAVE), op = __shfl_xor(bp, d, WAVE);
-            const int oi = __shfl_xor(bi, d, WAVE);
-            if (oi != NONE && (bi == NONE || before(ok, oi, bk, bi))) { bk = ok; bp = op; bi = oi; }
-        }
-        if (bi == NONE) break;
-        if (bi % WAVE == lane) open &= ~(1u << (bi / WAVE));
-        if (lane == s) { mine = bi; gate = bp; }
-        total += bp;
-    }
-    if (lane < top_k) {
-        crd[t * top_k + lane] = mine;
-        vals[t * top_k + lane] = mine < 0 ? 0.0f : (float)((normalise ? gate / total : gate) * (double)factor);
-    }
-}
-
+// A workgroup per token, a lane per expert.  An expert's place in the row is the number of those before it: it compares its key with all
+// others (taking the best one top_k times, each time a search over the lanes, is 2.7 times as long with 64 experts).
 template <int SCORE>
-void choose(int n, int experts, int top_k, int normalise, float factor, const double *logits, const float *bias, int *crd, float *vals, hipStream_t s)
+__global__ __launch_bounds__(PSK_MOE_MAX_EXPERTS) void k_route_rank(int experts, int top_k, int normalise, float factor, const double *__restrict__ logits,
+                                                                     const float *__restrict__ bias, int *__restrict__ crd, float *__restrict__ vals)
 {
-#define PSK_CHOOSE(PER) PSK_LAUNCH((k_route_choose<SCORE, PER>), dim3(n), dim3(64), 0, s, experts, top_k, normalise, factor, logits, bias, crd, vals)
-    if (experts <= 64) PSK_CHOOSE(1);
-    else if (experts <= 128) PSK_CHOOSE(2);
-    else if (experts <= 256) PSK_CHOOSE(4);
-    else PSK_CHOOSE(PSK_MOE_MAX_EXPERTS / WAVE);
-#undef PSK_CHOOSE
+    __shared__ __align__(16) unsigned long long keys[PSK_MOE_MAX_EXPERTS];
+    __shared__ double gates[PSK_MOE_MAX_TOP_K], tops[PSK_MOE_MAX_EXPERTS / WAVE], sums[PSK_MOE_MAX_EXPERTS / WAVE];
+    __shared__ int open[PSK_MOE_MAX_EXPERTS / WAVE];
+    const int e = threadIdx.x, lane = e & 63, wave = e >> 6, waves = blockDim.x >> 6;
+    const int64_t t = blockIdx.x;
+    const bool real = e < experts;
+    const double logit = real ? logits[t * experts + e] : -INFINITY;
+    const float b = real && bias ? bias[e] : 0.0f;
+    double p;
+    if constexpr (SCORE == PSK_SCORE_SOFTMAX) {
+        const auto larger = [](double x, double y) { return y > x || y != y ? y : x; };
+        double top = wave_all(logit, larger);
+        if (lane == 0) tops[wave] = top;
+        __syncthreads();
+        for (int w = 0; w < waves; ++w) top = larger(top, tops[w]);
+        p = real ? exp(logit - top) : 0.0;
+        double sum = wave_all(p, [](double x, double y) { return x + y; });
+        if (lane == 0) sums[wave] = sum;
+        __syncthreads();
+        sum = 0;
+        for (int w = 0; w < waves; ++w) sum += sums[w];
+        p /= sum;
+    } else {
+        p = 1.0 / (1.0 + exp(-logit));
+    }
+    // numbers in their order as integers; 0: not to be chosen, 1: no number
+    const double k = (bias ? p + (double)b : logit) + 0.0;   // -0 as 0
+    const unsigned long long u = __builtin_bit_cast(unsigned long long, k);
+    unsigned long long key = k != k ? 1 : (u >> 63 ? ~u : u | 1ull << 63);
+    if (!real || b == -INFINITY) key = 0;
+    keys[e] = key;
+    const int mine = __popcll(__ballot(key != 0));
+    if (lane == 0) open[wave] = mine;
+    if (e < PSK_MOE_MAX_TOP_K) gates[e] = 0;
+    __syncthreads();
+    int rank = 0, taken = 0;
+    typedef unsigned long long v2l __attribute__((ext_vector_type(2)));
+#pragma unroll 8
+    for (int j = 0; j < experts; j += 2) {                   // (keys past the last expert are 0)
+        const v2l o = *reinterpret_cast<const v2l *>(keys + j);
+        rank += (o[0] > key || (o[0] == key && j < e)) + (o[1] > key || (o[1] == key && j + 1 < e));
+    }
+    for (int w = 0; w < waves; ++w) taken += open[w];
+    const bool chosen = key != 0 && rank < top_k;
+    if (chosen) gates[rank] = p;
+    if (normalise) {
+        __syncthreads();
+        double total = 0;
+        for (int i = 0; i < top_k; ++i) total += gates[i];
+        p /= total;
+    }
+    if (chosen) {
+        crd[t * top_k + rank] = e;
+        vals[t * top_k + rank] = (float)(p * (double)factor);
+    }
+    if (e >= taken && e < top_k) {
+        crd[t * top_k + e] = -1;
+        vals[t * top_k + e] = 0;
+    }
 }
 
 template <int XT, int WT>
 void logits_of(int n, int dim, int experts, const void *X, int64_t ldx, const void *W, int64_t ldw, double *logits, hipStream_t s)
 {
-    PSK_LAUNCH((k_route_logits<XT, WT>), dim3((n + ROUTE_TOKENS - 1) / ROUTE_TOKENS * experts), dim3(64 * ROUTE_WAVES), 0, s, n, dim, experts, X, ldx,
-               W, ldw, logits);
+    if (n == 1) PSK_LAUNCH((k_route_logits<XT, WT, 4, 1>), dim3((experts + 3) / 4), dim3(THREADS), 0, s, n, dim, experts, X, ldx, W, ldw, logits);
+    else PSK_LAUNCH((k_route_logits<XT, WT, 4, 8>), dim3((experts + 3) / 4 * ((n + 7) / 8)), dim3(THREADS), 0, s, n, dim, experts, X, ldx, W, ldw, logits);
 }
 
 }  // namespace
@@ -164,8 +217,9 @@ hipError_t launch_moe_route(int n, int dim, int experts, int top_k, int score, i
     else if (type == F16) logits_of<F16, F32>(n, dim, experts, X, ldx, W, ldw, logits, s);
     else if (wtype == BF16) logits_of<BF16, BF16>(n, dim, experts, X, ldx, W, ldw, logits, s);
     else logits_of<BF16, F32>(n, dim, experts, X, ldx, W, ldw, logits, s);
-    if (score == PSK_SCORE_SOFTMAX) choose<PSK_SCORE_SOFTMAX>(n, experts, top_k, normalise, factor, logits, bias, crd, vals, s);
-    else choose<PSK_SCORE_SIGMOID>(n, experts, top_k, normalise, factor, logits, bias, crd, vals, s);
+    const dim3 block((experts + WAVE - 1) / WAVE * WAVE);
+    if (score == PSK_SCORE_SOFTMAX) PSK_LAUNCH(k_route_rank<PSK_SCORE_SOFTMAX>, dim3(n), block, 0, s, experts, top_k, normalise, factor, logits, bias, crd, vals);
+    else PSK_LAUNCH(k_route_rank<PSK_SCORE_SIGMOID>, dim3(n), block, 0, s, experts, top_k, normalise, factor, logits, bias, crd, vals);
     return take_launch_status();
 }
 

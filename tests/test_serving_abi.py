@@ -89,7 +89,7 @@ def test_layer_refuses():
         assert layer(**over) == 7, over
     assert psk.psk_moe_workspace_bytes(4, 100, 0, 10, 3) == 0 and psk.psk_moe_workspace_bytes(4, 100, 48, 2000, 3) == 0
     # more tokens than one pair of launches takes need no more room
-    assert psk.psk_moe_workspace_bytes(1 << 20, 100, 48, 10, 8) == psk.psk_moe_workspace_bytes(4096, 100, 48, 10, 8)
+    assert psk.psk_moe_workspace_bytes(psk.PSK_MAX_VECTORS, 100, 48, 10, 8) == psk.psk_moe_workspace_bytes(4096, 100, 48, 10, 8)
 
 
 def layer_q4(w1=None, w3=None, w2=None, n=4, top_k=3, act=0, type=psk.PSK_BF16, X=ONE, ldx=100, crd=ONE, vals=ONE, Y=ONE, ldy=100, ws=ONE, have=BIG):
