@@ -80,6 +80,33 @@ __global__ __launch_bounds__(64 * KW) void k_gemm_q4(WeightsQ4 A, int n, const v
     }
 }
 
+// Up to 256 KW columns: the vectors kept (KeptQ4), workgroups that stay.  16-bit vectors are brought into the operands' order here; those of 32
+// bits come from the copy.
+template <int XT, int S, int GB, int KW>
+__global__ __launch_bounds__(64 * KW) void k_gemm_q4_kept(WeightsQ4 A, int n, const void *X, int64_t ldx, const v4u *copy, void *Y, int64_t ldy)
+{
+    constexpr int T = XT == F16 ? F16 : BF16;
+    typedef typename Vectors<XT>::type V;
+    typedef KeptQ4<T, 1, GB, S, KW, V> K;
+    __shared__ typename K::Space space;
+    const int tile = blockIdx.y;
+    const WeightsQ4 w[1] = {A};
+    K k(space, w, 0, A.rows, A.cols);
+    if constexpr (XT == F32) {
+        Copied<V> x;
+        x.set(copy, tile, copied_blocks(A.cols), k.lane);
+        keep_copied(k, x);
+    } else {
+        keep_rows<T>(k, static_cast<const unsigned short *>(X), ldx, n, tile);
+    }
+    k.run(blockIdx.x, gridDim.x, (A.rows + 15) / 16, [&](int set, const float *sums) {
+        for (int o = threadIdx.x; o < 256; o += 64 * KW) {
+            const int v = 16 * tile + (o >> 4), i = set * 16 + (o & 15);
+            if (v < n && i < A.rows) store_as<XT>(Y, v * ldy + i, get_sum<KW, 1, 16>(sums, 0, o >> 4, o & 15));
+        }
+    });
+}
+
 template <int XT, int S, int GB, bool Z, int P>
 void few_vectors(const WeightsQ4 &A, int n, const void *X, int64_t ldx, void *Y, int64_t ldy, hipStream_t s)
 {
@@ -92,13 +119,32 @@ void few_vectors_by_columns(const WeightsQ4 &A, int n, const void *X, int64_t ld
     if (A.cols >= 2048) few_vectors<XT, S, GB == 8 ? 4 * LONG : GB, Z, LONG>(A, n, X, ldx, Y, ldy, s);
     else few_vectors<XT, S, GB, Z, 2>(A, n, X, ldx, Y, ldy, s);
 }
+// Workgroups for KeptQ4: as many as are on the chip at once (1024 threads to a compute unit) for all tiles together, no more than sets of rows.
+inline int kept_groups(int sets, int tiles, int kw)
+{
+    const int n = 256 * (16 / kw) / tiles;
+    return n < 1 ? 1 : (n < sets ? n : sets);
+}
+template <int XT, int S, int GB, int KW>
+void kept_vectors(const WeightsQ4 &A, int n, const void *X, int64_t ldx, void *Y, int64_t ldy, const v4u *copy, hipStream_t s)
+{
+    const int rows = (A.rows + 15) / 16, tiles = (n + 15) / 16;
+    PSK_LAUNCH((k_gemm_q4_kept<XT, S, GB, KW>), dim3(kept_groups(rows, tiles, KW), tiles), dim3(64 * KW), 0, s, A, n, X, ldx, copy, Y, ldy);
+}
 template <int XT, int S, int GB>
 void more_vectors(const WeightsQ4 &A, int n, const void *X, int64_t ldx, void *Y, int64_t ldy, void *space, hipStream_t s)
 {
     const int rows = (A.rows + 15) / 16, tiles = (n + 15) / 16;
     v4u *copy = static_cast<v4u *>(space);
-    PSK_LAUNCH((k_gemm_q4_copy<XT, GB>), dim3(copied_blocks(A.cols) / 4, tiles), dim3(256), 0, s, n, A.cols, X, ldx, copy);
-    if (n <= 16) PSK_LAUNCH((k_gemm_q4<XT, S, GB, true, 1, 1, 4>), dim3(rows, 1), dim3(256), 0, s, A, n, copy, Y, ldy);
+    const bool kept = A.cols <= KEPT_COLUMNS;
+    // (kept vectors are in natural order, as for groups of 32 columns)
+    if (!kept) PSK_LAUNCH((k_gemm_q4_copy<XT, GB>), dim3(copied_blocks(A.cols) / 4, tiles), dim3(256), 0, s, n, A.cols, X, ldx, copy);
+    else if (XT == F32) PSK_LAUNCH((k_gemm_q4_copy<XT, 1>), dim3(copied_blocks(A.cols) / 4, tiles), dim3(256), 0, s, n, A.cols, X, ldx, copy);
+    if (kept) {
+        if (A.cols <= 1024) kept_vectors<XT, S, GB, 4>(A, n, X, ldx, Y, ldy, copy, s);
+        else if (A.cols <= 2048) kept_vectors<XT, S, GB, 8>(A, n, X, ldx, Y, ldy, copy, s);
+        else kept_vectors<XT, S, GB, 16>(A, n, X, ldx, Y, ldy, copy, s);
+    } else if (n <= 16) PSK_LAUNCH((k_gemm_q4<XT, S, GB, true, 1, 1, 4>), dim3(rows, 1), dim3(256), 0, s, A, n, copy, Y, ldy);
     else if constexpr (XT == F32) PSK_LAUNCH((k_gemm_q4<XT, S, GB, true, 2, 1, 4>), dim3((rows + 1) / 2, tiles), dim3(256), 0, s, A, n, copy, Y, ldy);
     else PSK_LAUNCH((k_gemm_q4<XT, S, GB, true, 2, 2, 4>), dim3((rows + 1) / 2, (tiles + 1) / 2), dim3(256), 0, s, A, n, copy, Y, ldy);
 }

@@ -318,7 +318,9 @@ size_t carve_moe(const MoeCall &c, Call *a)
 
 // The spans of the two steps, for up to four tokens (FEW_*) and for tiles, MOST of them at once.  (The parts of h are in bf16, or weights in 16 bits: no
 // span of the second step takes columns in the order of f16 codes.)
-template <class FEW_UP, class FEW_DOWN, class UP, class DOWN, int MOST, int YT, class W>
+// KEPT: another way for more than four tokens, where it fits.
+struct NotKept { static constexpr bool USED = false; };
+template <class FEW_UP, class FEW_DOWN, class UP, class DOWN, int MOST, int YT, class KEPT, class W>
 hipError_t launch_layer(const MoeCall &c, const W &w1, const W &w3, const W &w2, hipStream_t s)
 {
     static_assert(!(DOWN::CODES && DOWN::T == F16), "copied_at");
@@ -334,9 +336,21 @@ hipError_t launch_layer(const MoeCall &c, const W &w1, const W &w3, const W &w2,
             PSK_LAUNCH((k_moe_up_few<FEW_UP, FEW_DOWN::T, W>), dim3((c.inter + 15) / 16, slots), dim3(THREADS), 0, s, a, w1, w3);
             PSK_LAUNCH((k_moe_down_few<FEW_DOWN, W>), dim3(down, slots), dim3(THREADS), 0, s, a, w2);
         } else {
-            PSK_LAUNCH((k_moe_sort<UP>), dim3((copied_blocks(c.dim) + KW * COPY_BLOCKS - 1) / (KW * COPY_BLOCKS), slots), dim3(THREADS), 0, s, a);
-            PSK_LAUNCH((k_moe_up<UP, DOWN::T, DOWN::SPREAD, MOST, W>), dim3(copied_blocks(c.inter) * 2, slots), dim3(THREADS), 0, s, a, w1, w3);
-            PSK_LAUNCH((k_moe_down<DOWN, MOST, W>), dim3(down, slots), dim3(THREADS), 0, s, a, w2);
+            const dim3 sort((copied_blocks(c.dim) + KW * COPY_BLOCKS - 1) / (KW * COPY_BLOCKS), slots);
+            bool kept = false;
+            if constexpr (KEPT::USED) {
+                kept = KEPT::fits(c);
+                if (kept) {
+                    PSK_LAUNCH((k_moe_sort<typename KEPT::COPY>), sort, dim3(THREADS), 0, s, a);
+                    KEPT::up(a, slots, w1, w3, s);
+                    KEPT::down(a, slots, w2, s);
+                }
+            }
+            if (!kept) {
+                PSK_LAUNCH((k_moe_sort<UP>), sort, dim3(THREADS), 0, s, a);
+                PSK_LAUNCH((k_moe_up<UP, DOWN::T, DOWN::SPREAD, MOST, W>), dim3(copied_blocks(c.inter) * 2, slots), dim3(THREADS), 0, s, a, w1, w3);
+                PSK_LAUNCH((k_moe_down<DOWN, MOST, W>), dim3(down, slots), dim3(THREADS), 0, s, a, w2);
+            }
         }
         PSK_LAUNCH(k_moe_join<YT>, dim3((c.dim + 255) / 256, a.n), dim3(256), 0, s, c.dim, c.experts, c.top_k, a.crd, c.vals + t0 * c.top_k, a.P,
                    static_cast<unsigned short *>(c.Y) + t0 * c.ldy, c.ldy);

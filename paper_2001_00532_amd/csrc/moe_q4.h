@@ -6,11 +6,105 @@
 namespace psk {
 namespace {
 
+// ---- more than four tokens, up to KEPT_COLUMNS columns in both products: the vectors kept (KeptQ4)
+template <int T, int GB, int S, int KW>
+__global__ __launch_bounds__(64 * KW) void k_moe_q4_up(Call a, WeightsQ4 w1, WeightsQ4 w3)
+{
+    typedef KeptQ4<T, 2, GB, S, KW, Plain16<T>> K;
+    __shared__ typename K::Space space;
+    const Found g = a.found[blockIdx.y];
+    if (g.expert < 0) return;
+    const int sets = copied_blocks(a.inter) * 2, real = (a.inter + 15) / 16;      // sets past the last row: zeros that pad the next step's columns
+    const WeightsQ4 w[2] = {w1, w3};
+    for (int t = 0; 16 * t < g.count; ++t) {
+        K k(space, w, g.expert, a.inter, a.dim);
+        Copied<Plain16<T>> x;
+        x.set(a.copy, g.tile + t, copied_blocks(a.dim), k.lane);
+        keep_copied(k, x);
+        const auto store = [&](int set, int v, int i, float h) {
+            unsigned short p, q;
+            Halves<BF16>::split(h, p, q);
+            const int64_t at = copied_at<false>(g.tile + t, copied_blocks(a.inter), 16 * set + i, v);
+            a.h[at] = p;
+            a.h[at + 64 * 8] = q;
+        };
+        if ((int)blockIdx.x < real)
+            k.run(blockIdx.x, gridDim.x, real, [&](int set, const float *sums) {
+                for (int o = threadIdx.x; o < 256; o += 64 * KW) {
+                    const int v = o >> 4, i = o & 15;
+                    if (16 * t + v >= g.count) continue;
+                    const float h = activate(a.act, get_sum<KW, 2, 16>(sums, 0, v, i)) * get_sum<KW, 2, 16>(sums, 1, v, i);
+                    store(set, v, i, 16 * set + i < a.inter ? h : 0.0f);
+                }
+            });
+        for (int set = real + blockIdx.x; set < sets; set += gridDim.x)
+            for (int o = threadIdx.x; o < 256; o += 64 * KW)
+                if (16 * t + (o >> 4) < g.count) store(set, o >> 4, o & 15, 0.0f);
+    }
+}
+template <int GB, int S, int KW>
+__global__ __launch_bounds__(64 * KW) void k_moe_q4_down(Call a, WeightsQ4 w2)
+{
+    typedef KeptQ4<BF16, 1, GB, S, KW, Halves<BF16>> K;
+    __shared__ typename K::Space space;
+    const Found g = a.found[blockIdx.y];
+    if (g.expert < 0) return;
+    const WeightsQ4 w[1] = {w2};
+    for (int t = 0; 16 * t < g.count; ++t) {
+        K k(space, w, g.expert, a.dim, a.inter);
+        Copied<Halves<BF16>> x;
+        x.set(a.h, g.tile + t, copied_blocks(a.inter), k.lane);
+        keep_copied(k, x);
+        k.run(blockIdx.x, gridDim.x, (a.dim + 15) / 16, [&](int set, const float *sums) {
+            for (int o = threadIdx.x; o < 256; o += 64 * KW) {
+                const int v = 16 * t + (o >> 4), i = 16 * set + (o & 15);
+                if (v < g.count && i < a.dim) a.P[(int64_t)a.list[g.first + v] * a.dim + i] = get_sum<KW, 1, 16>(sums, 0, o >> 4, o & 15);
+            }
+        });
+    }
+}
+// Workgroups per expert: twice as many as are on the chip at once (a part of the experts may have no position), no more than sets.
+inline int kept_groups(int sets, int slots, int kw)
+{
+    const int n = 2 * 256 * (16 / kw) / slots;
+    return n < 1 ? 1 : (n < sets ? n : sets);
+}
+template <int T, int GB, int S, int KW>
+void launch_up(const Call &a, int slots, const WeightsQ4 &w1, const WeightsQ4 &w3, hipStream_t s)
+{
+    PSK_LAUNCH((k_moe_q4_up<T, GB, S, KW>), dim3(kept_groups((a.inter + 15) / 16, slots, KW), slots), dim3(64 * KW), 0, s, a, w1, w3);
+}
+template <int GB, int S, int KW>
+void launch_down(const Call &a, int slots, const WeightsQ4 &w2, hipStream_t s)
+{
+    PSK_LAUNCH((k_moe_q4_down<GB, S, KW>), dim3(kept_groups((a.dim + 15) / 16, slots, KW), slots), dim3(64 * KW), 0, s, a, w2);
+}
+template <int T, int S, int G1, int G2>
+struct KeptSteps {
+    static constexpr bool USED = true;
+    typedef SpanQ4<T, 1, 2, 1, S, false> COPY;                 // natural order
+    static bool fits(const MoeCall &c) { return c.dim <= KEPT_COLUMNS && c.inter <= KEPT_COLUMNS; }
+    static void up(const Call &a, int slots, const WeightsQ4 &w1, const WeightsQ4 &w3, hipStream_t s)
+    {
+        if (a.dim <= 1024) launch_up<T, G1, S, 4>(a, slots, w1, w3, s);
+        else if (a.dim <= 2048) launch_up<T, G1, S, 8>(a, slots, w1, w3, s);
+        else launch_up<T, G1, S, 16>(a, slots, w1, w3, s);
+    }
+    static void down(const Call &a, int slots, const WeightsQ4 &w2, hipStream_t s)
+    {
+        if (a.inter <= 1024) launch_down<G2, S, 4>(a, slots, w2, s);
+        else if (a.inter <= 2048) launch_down<G2, S, 8>(a, slots, w2, s);
+        else launch_down<G2, S, 16>(a, slots, w2, s);
+    }
+};
+
 // G: blocks that share a scale (SpanQ4), by the group
 template <int T, int S, int G1, int G2>
 hipError_t launch_q4(const MoeCall &c, const WeightsQ4 &w1, const WeightsQ4 &w3, const WeightsQ4 &w2, hipStream_t s)
 {
-    return launch_layer<SpanQ4<T, 2, 2, G1, S, true>, SpanQ4<BF16, 1, 2, G2, S, true>, SpanQ4<T, 2, 2, G1, S, true>, SpanQ4<BF16, 1, 2, G2, S, true>, 1, T>(c, w1, w3, w2, s);
+    typedef SpanQ4<T, 2, 2, G1, S, true> UP;
+    typedef SpanQ4<BF16, 1, 2, G2, S, true> DOWN;
+    return launch_layer<UP, DOWN, UP, DOWN, 1, T, KeptSteps<T, S, G1, G2>>(c, w1, w3, w2, s);
 }
 template <int T, int S, int G1>
 hipError_t launch_q4_down(const MoeCall &c, const WeightsQ4 &w1, const WeightsQ4 &w3, const WeightsQ4 &w2, hipStream_t s)

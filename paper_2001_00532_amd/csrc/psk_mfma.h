@@ -700,4 +700,193 @@ __device__ __forceinline__ float get_sum(const float *lds, int t, int m, int n)
     return v;
 }
 
+// ---- 4-bit weights and tiles of vectors, the vectors kept
+// A tile takes a kilobyte of vectors for each 256 bytes of weights.  So a wave keeps the vectors of its 256 columns in registers, and
+// the weights of one set of 16 R rows after the other pass by; the KW waves of a workgroup share up to 256 KW columns, their sums meet in LDS
+// for every set.  Scales and zero points of a set lie far apart, row by row, and would cost as much as the weights where each lane
+// loads its own: all threads bring them to LDS, a set ahead.
+constexpr int KEPT_CHUNK = 256, KEPT_COLUMNS = 16 * KEPT_CHUNK;
+template <int KW, int R, int GB, int S>
+struct KeptSpace {
+    typedef typename std::conditional<S == F32, float, unsigned short>::type Scale;
+    static constexpr int GROUPS = KW * 8 / GB, LD = GROUPS + (S == F32 ? 4 : 8), LDZ = GROUPS + 16;     // a row's neighbours on other banks
+    float sums[2][KW * R * 256];
+    v4u places[KW * EXCHANGE];
+    __align__(16) Scale s[2][R][16][LD];
+    __align__(16) unsigned char z[2][R][16][LDZ];
+};
+template <int T, int R, int GB, int S, int KW, class X>
+struct KeptQ4 {
+    typedef KeptSpace<KW, R, GB, S> Space;
+    typedef typename Space::Scale Scale;
+    static constexpr int THREADS = 64 * KW, NG = GB < 8 ? 8 / GB : 1, PER = GB < 4 ? GB : 4;
+    static constexpr int E = R * 16 * Space::GROUPS > THREADS ? R * 16 * Space::GROUPS / THREADS : 1;   // scales that a thread brings
+    Space &sp;
+    const WeightsQ4 (&w)[R];
+    int64_t m;
+    int rows, cols, c, lane, wave;
+    bool any, partial;                                     // whether the wave has columns, and fewer than a chunk
+    typename Copied<X>::Raw x[2][4];
+    v4u g[2][R][2];
+    Scale s[E];
+    unsigned char z[E];
+    Exchange place;
+    __device__ __forceinline__ KeptQ4(Space &space, const WeightsQ4 (&weights)[R], int64_t matrix, int n_rows, int n_cols)
+        : sp(space), w(weights), m(matrix), rows(n_rows), cols(n_cols), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)),
+          place(space.places + EXCHANGE * wave, lane)
+    {
+        c = wave;
+        any = c * KEPT_CHUNK < cols;
+        partial = (c + 1) * KEPT_CHUNK > cols;
+    }
+    // Weights and scales of the rows from row0 on.  A thread with none of the scales brings one that another thread brings too.
+    template <int B>
+    __device__ __forceinline__ void request(int row0)
+    {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                // past the last column, a piece of the row's beginning: its products are with zeros
+                const int k = c * KEPT_CHUNK + 32 * load_piece(lane);
+                const unsigned char *q = w[r].codes + m * w[r].stride_codes + (int64_t)min(row0 + load_row(lane, i), rows - 1) * w[r].ld_codes;
+                g[B][r][i] = __builtin_nontemporal_load(reinterpret_cast<const v4u *>(q + (k < cols ? k / 2 : 0)));
+            }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int i = threadIdx.x + e * THREADS, r = R == 1 ? 0 : i / (16 * Space::GROUPS) % R, row = i / Space::GROUPS % 16;
+            const int group = min(i % Space::GROUPS, (cols - 1) >> w[0].shift);
+            const WeightsQ4 &a = R == 1 || r == 0 ? w[0] : w[R - 1];
+            const int64_t at = m * a.stride_scales + (int64_t)min(row0 + row, rows - 1) * a.ld_scales + group;
+            s[e] = static_cast<const Scale *>(a.scales)[at];
+            z[e] = *(a.zeros ? a.zeros + at : a.codes + m * a.stride_codes);
+        }
+    }
+    template <int B>
+    __device__ __forceinline__ void put_scales()
+    {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const int i = threadIdx.x + e * THREADS, r = R == 1 ? 0 : i / (16 * Space::GROUPS) % R, row = i / Space::GROUPS % 16, group = i % Space::GROUPS;
+            const WeightsQ4 &a = R == 1 || r == 0 ? w[0] : w[R - 1];
+            sp.s[B][r][row][group] = s[e];
+            sp.z[B][r][row][group] = a.zeros ? z[e] : (unsigned char)8;
+        }
+    }
+    static __device__ __forceinline__ float factor(Scale v)
+    {
+        float f;
+        if constexpr (S == F32) f = v;
+        else f = widen<S>(v);
+        return T == BF16 ? f * 0x1p9f : f;
+    }
+    template <int B>
+    __device__ __forceinline__ void multiply()
+    {
+        v4f acc[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) acc[r] = v4f{0, 0, 0, 0};
+        if (any) {
+            v4u all[R][2];
+#pragma unroll
+            for (int r = 0; r < R; ++r) place(g[B][r], all[r]);
+            const int g0 = GB <= 8 ? c * (8 / (GB < 8 ? GB : 8)) : 0;
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                Scale fs[NG];
+                unsigned char zs[NG];
+#pragma unroll
+                for (int i = 0; i < NG; ++i) {
+                    const int at = GB == 8 ? (c * KEPT_CHUNK) >> w[0].shift : g0 + i;
+                    fs[i] = sp.s[B][r][lane & 15][at];
+                    zs[i] = sp.z[B][r][lane & 15][at];
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const v4u words = transpose_quarters(all[r][h]);
+#pragma unroll
+                    for (int i = 0; i < 4 / PER; ++i) {
+                        const int at = 4 * h / GB + i;
+                        const Zero<T> zero((int)zs[at]);
+                        v4f sum = v4f{0, 0, 0, 0};
+#pragma unroll
+                        for (int b = 0; b < PER; ++b) sum = product<T, X>(x[h][i * PER + b].v, dequantise(words[i * PER + b], zero), sum);
+                        // a block past the last column counts nothing: its sum is zero, and so has the scale to be
+                        const float f = c * KEPT_CHUNK + 128 * h + 32 * PER * i < cols ? factor(fs[at]) : 0.0f;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[r][e] = fmaf(sum[e], f, acc[r][e]);
+                    }
+                }
+            }
+        }
+        put_sums<R>(sp.sums[B], wave, lane, acc);
+    }
+    // Sets first, first + step, ... before `sets`; done(set, sums) takes over the sums of one.
+    template <class DONE>
+    __device__ __forceinline__ void run(int first, int step, int sets, DONE done)
+    {
+        int set = first;
+        request<0>(16 * set);
+        put_scales<0>();
+        __syncthreads();
+        for (;;) {
+            if (set + step >= sets) { last<0>(set, done); return; }
+            next<0>(set, step, done);
+            set += step;
+            if (set + step >= sets) { last<1>(set, done); return; }
+            next<1>(set, step, done);
+            set += step;
+        }
+    }
+    template <int B, class DONE>
+    __device__ __forceinline__ void next(int set, int step, DONE done)
+    {
+        request<1 - B>(16 * (set + step));
+        multiply<B>();
+        put_scales<1 - B>();
+        __syncthreads();
+        done(set, sp.sums[B]);
+    }
+    template <int B, class DONE>
+    __device__ __forceinline__ void last(int set, DONE done)
+    {
+        multiply<B>();
+        __syncthreads();
+        done(set, sp.sums[B]);
+        __syncthreads();                                   // (the next tile's first set)
+    }
+};
+// The vectors of the wave's columns: from a copy in natural order,
+template <class K, class X>
+__device__ __forceinline__ void keep_copied(K &k, const Copied<X> &x)
+{
+    if (k.any) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x.load(k.x[h][j], 8 * k.c + 4 * h + j);
+    }
+}
+// or 16-bit vectors 16 tile and on as they are, whole lines at a time, through LDS like the weights.
+template <int T, class K>
+__device__ __forceinline__ void keep_rows(K &k, const unsigned short *X, int64_t ldx, int n, int tile)
+{
+    if (!k.any) return;
+    v4u w[4][2], o[2];
+#pragma unroll
+    for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const unsigned short *p = X + min(16 * tile + load_row(k.lane, i), n - 1) * ldx + 8 * load_piece(k.lane);
+            const int at = KEPT_CHUNK * k.c + 64 * b;
+            w[b][i] = k.partial ? load8(p, at, k.cols - 8 * load_piece(k.lane)) : *reinterpret_cast<const v4u_u *>(p + at);
+        }
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        k.place(w[b], o);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) k.x[b >> 1][2 * (b & 1) + i].v[0] = code_order<T>(o[i]);
+    }
+}
+
 }  // namespace psk
