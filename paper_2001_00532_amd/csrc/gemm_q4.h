@@ -136,7 +136,7 @@ void more_vectors(const WeightsQ4 &A, int n, const void *X, int64_t ldx, void *Y
 {
     const int rows = (A.rows + 15) / 16, tiles = (n + 15) / 16;
     v4u *copy = static_cast<v4u *>(space);
-    const bool kept = A.cols <= KEPT_COLUMNS;
+    const bool kept = kept_fits(A);
     // (kept vectors are in natural order, as for groups of 32 columns)
     if (!kept) PSK_LAUNCH((k_gemm_q4_copy<XT, GB>), dim3(copied_blocks(A.cols) / 4, tiles), dim3(256), 0, s, n, A.cols, X, ldx, copy);
     else if (XT == F32) PSK_LAUNCH((k_gemm_q4_copy<XT, 1>), dim3(copied_blocks(A.cols) / 4, tiles), dim3(256), 0, s, n, A.cols, X, ldx, copy);

@@ -339,7 +339,7 @@ hipError_t launch_layer(const MoeCall &c, const W &w1, const W &w3, const W &w2,
             const dim3 sort((copied_blocks(c.dim) + KW * COPY_BLOCKS - 1) / (KW * COPY_BLOCKS), slots);
             bool kept = false;
             if constexpr (KEPT::USED) {
-                kept = KEPT::fits(c);
+                kept = KEPT::fits(w1, w3, w2);
                 if (kept) {
                     PSK_LAUNCH((k_moe_sort<typename KEPT::COPY>), sort, dim3(THREADS), 0, s, a);
                     KEPT::up(a, slots, w1, w3, s);

@@ -8,7 +8,7 @@ namespace {
 
 // ---- more than four tokens, up to KEPT_COLUMNS columns in both products: the vectors kept (KeptQ4)
 template <int T, int GB, int S, int KW>
-__global__ __launch_bounds__(64 * KW) void k_moe_q4_up(Call a, WeightsQ4 w1, WeightsQ4 w3)
+__global__ __launch_bounds__(64 * KW, 4) void k_moe_q4_up(Call a, WeightsQ4 w1, WeightsQ4 w3)
 {
     typedef KeptQ4<T, 2, GB, S, KW, Plain16<T>> K;
     __shared__ typename K::Space space;
@@ -83,7 +83,7 @@ template <int T, int S, int G1, int G2>
 struct KeptSteps {
     static constexpr bool USED = true;
     typedef SpanQ4<T, 1, 2, 1, S, false> COPY;                 // natural order
-    static bool fits(const MoeCall &c) { return c.dim <= KEPT_COLUMNS && c.inter <= KEPT_COLUMNS; }
+    static bool fits(const WeightsQ4 &w1, const WeightsQ4 &w3, const WeightsQ4 &w2) { return kept_fits(w1) && kept_fits(w3) && kept_fits(w2); }
     static void up(const Call &a, int slots, const WeightsQ4 &w1, const WeightsQ4 &w3, hipStream_t s)
     {
         if (a.dim <= 1024) launch_up<T, G1, S, 4>(a, slots, w1, w3, s);

@@ -706,6 +706,7 @@ __device__ __forceinline__ float get_sum(const float *lds, int t, int m, int n)
 // for every set.  Scales and zero points of a set lie far apart, row by row, and would cost as much as the weights where each lane
 // loads its own: all threads bring them to LDS, a set ahead.
 constexpr int KEPT_CHUNK = 256, KEPT_COLUMNS = 16 * KEPT_CHUNK;
+inline bool kept_fits(const WeightsQ4 &A) { return A.cols <= KEPT_COLUMNS && A.ld_codes < (1 << 26) && A.ld_scales < (1 << 24); }
 template <int KW, int R, int GB, int S>
 struct KeptSpace {
     typedef typename std::conditional<S == F32, float, unsigned short>::type Scale;
@@ -720,7 +721,7 @@ struct KeptQ4 {
     typedef KeptSpace<KW, R, GB, S> Space;
     typedef typename Space::Scale Scale;
     static constexpr int THREADS = 64 * KW, NG = GB < 8 ? 8 / GB : 1, PER = GB < 4 ? GB : 4;
-    static constexpr int E = R * 16 * Space::GROUPS > THREADS ? R * 16 * Space::GROUPS / THREADS : 1;   // scales that a thread brings
+    static constexpr int E = GB == 1 ? 2 : 1;              // scales of 16 rows that a thread brings: 2 / GB for each of them
     Space &sp;
     const WeightsQ4 (&w)[R];
     int64_t m;
@@ -728,50 +729,59 @@ struct KeptQ4 {
     bool any, partial;                                     // whether the wave has columns, and fewer than a chunk
     typename Copied<X>::Raw x[2][4];
     v4u g[2][R][2];
-    Scale s[E];
-    unsigned char z[E];
+    Scale s[R][E];
+    unsigned char z[R][E];
     Exchange place;
     __device__ __forceinline__ KeptQ4(Space &space, const WeightsQ4 (&weights)[R], int64_t matrix, int n_rows, int n_cols)
         : sp(space), w(weights), m(matrix), rows(n_rows), cols(n_cols), lane(threadIdx.x & 63), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)),
           place(space.places + EXCHANGE * wave, lane)
     {
+        asm volatile("" : "+v"(lane));                     // (nothing is kept for the next tile of vectors)
         c = wave;
         any = c * KEPT_CHUNK < cols;
         partial = (c + 1) * KEPT_CHUNK > cols;
     }
-    // Weights and scales of the rows from row0 on.  A thread with none of the scales brings one that another thread brings too.
+    // Weights and scales of the rows from row0 on.  Where a set begins is computed once per wave, a lane's offset from there has 32 bits
+    // (KeptQ4 is for such leading dimensions).  A thread with none of the scales brings one that another thread brings too.
     template <int B>
     __device__ __forceinline__ void request(int row0)
     {
+        const int last = rows - 1 - row0;
+        // the scales before the weights: they are waited for first, and loads arrive in their order
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+        for (int r = 0; r < R; ++r) {
+            const int64_t at = m * w[r].stride_scales + row0 * w[r].ld_scales;
+            const Scale *scales = static_cast<const Scale *>(w[r].scales) + at;
+            const unsigned char *zeros = w[r].zeros ? w[r].zeros + at : w[r].codes;            // (no load under a condition)
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                // past the last column, a piece of the row's beginning: its products are with zeros
-                const int k = c * KEPT_CHUNK + 32 * load_piece(lane);
-                const unsigned char *q = w[r].codes + m * w[r].stride_codes + (int64_t)min(row0 + load_row(lane, i), rows - 1) * w[r].ld_codes;
-                g[B][r][i] = __builtin_nontemporal_load(reinterpret_cast<const v4u *>(q + (k < cols ? k / 2 : 0)));
+            for (int e = 0; e < E; ++e) {
+                const int i = threadIdx.x + e * THREADS, row = min(i / Space::GROUPS % 16, last), group = min(i % Space::GROUPS, (cols - 1) >> w[0].shift);
+                const unsigned off = (unsigned)row * (unsigned)w[r].ld_scales + group;
+                s[r][e] = scales[off];
+                z[r][e] = zeros[w[r].zeros ? off : 0u];
             }
+        }
+        const unsigned k = c * KEPT_CHUNK + 32 * load_piece(lane);                // past the last column, the row's beginning: its products are with zeros
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int i = threadIdx.x + e * THREADS, r = R == 1 ? 0 : i / (16 * Space::GROUPS) % R, row = i / Space::GROUPS % 16;
-            const int group = min(i % Space::GROUPS, (cols - 1) >> w[0].shift);
-            const WeightsQ4 &a = R == 1 || r == 0 ? w[0] : w[R - 1];
-            const int64_t at = m * a.stride_scales + (int64_t)min(row0 + row, rows - 1) * a.ld_scales + group;
-            s[e] = static_cast<const Scale *>(a.scales)[at];
-            z[e] = *(a.zeros ? a.zeros + at : a.codes + m * a.stride_codes);
+        for (int r = 0; r < R; ++r) {
+            const unsigned char *base = w[r].codes + m * w[r].stride_codes + row0 * w[r].ld_codes;
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                g[B][r][i] = __builtin_nontemporal_load(reinterpret_cast<const v4u *>(
+                    base + ((unsigned)min(load_row(lane, i), last) * (unsigned)w[r].ld_codes + ((int)k < cols ? k / 2 : 0u))));
         }
     }
     template <int B>
     __device__ __forceinline__ void put_scales()
     {
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const int i = threadIdx.x + e * THREADS, r = R == 1 ? 0 : i / (16 * Space::GROUPS) % R, row = i / Space::GROUPS % 16, group = i % Space::GROUPS;
-            const WeightsQ4 &a = R == 1 || r == 0 ? w[0] : w[R - 1];
-            sp.s[B][r][row][group] = s[e];
-            sp.z[B][r][row][group] = a.zeros ? z[e] : (unsigned char)8;
-        }
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                const int i = threadIdx.x + e * THREADS, row = i / Space::GROUPS % 16, group = i % Space::GROUPS;
+                sp.s[B][r][row][group] = s[r][e];
+                sp.z[B][r][row][group] = w[r].zeros ? z[r][e] : (unsigned char)8;
+            }
     }
     static __device__ __forceinline__ float factor(Scale v)
     {
@@ -787,12 +797,12 @@ struct KeptQ4 {
 #pragma unroll
         for (int r = 0; r < R; ++r) acc[r] = v4f{0, 0, 0, 0};
         if (any) {
-            v4u all[R][2];
-#pragma unroll
-            for (int r = 0; r < R; ++r) place(g[B][r], all[r]);
             const int g0 = GB <= 8 ? c * (8 / (GB < 8 ? GB : 8)) : 0;
 #pragma unroll
             for (int r = 0; r < R; ++r) {
+                if (r) __builtin_amdgcn_sched_barrier(0);      // one after the other: together they take more registers than four waves may have
+                v4u all[2];
+                place(g[B][r], all);
                 Scale fs[NG];
                 unsigned char zs[NG];
 #pragma unroll
@@ -803,7 +813,7 @@ struct KeptQ4 {
                 }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const v4u words = transpose_quarters(all[r][h]);
+                    const v4u words = transpose_quarters(all[h]);
 #pragma unroll
                     for (int i = 0; i < 4 / PER; ++i) {
                         const int at = 4 * h / GB + i;
