@@ -76,6 +76,29 @@ __device__ __forceinline__ Found find(FindSpace<MOST> &f, int positions, int exp
     return r;
 }
 
+// The same for up to 64 positions, by every wave for itself and without waiting for the others: slots in the order of the first positions.
+template <int MOST>
+__device__ __forceinline__ Found find_few(FindSpace<MOST> &f, int positions, int experts, const int *__restrict__ crd, int j)
+{
+    if (positions > WAVE) return find(f, positions, experts, crd, j);
+    const int lane = threadIdx.x & 63, e = lane < positions ? crd[lane] : -1;
+    Found r = {-1, 0, 0, 0};
+    unsigned long long left = __ballot((unsigned)e < (unsigned)experts);
+    for (; left; --j) {
+        const int other = __builtin_amdgcn_readlane(e, __ffsll(left) - 1);
+        const unsigned long long same = __ballot(e == other);
+        if (j == 0) {
+            r.expert = other;
+            r.count = __popcll(same);
+            if (e == other) f.list[__popcll(same & ((1ull << lane) - 1))] = (unsigned short)lane;         // (all waves write the same)
+            break;
+        }
+        left &= ~same;
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    return r;
+}
+
 __device__ __forceinline__ float activate(int act, float v)
 {
     if (act == PSK_ACT_SILU) return v / (1.0f + expf(-v));
@@ -99,12 +122,12 @@ struct Call {
 // ---- up to four tokens
 constexpr int FEW = 4;
 template <class SPAN, int HT, class W>
-__global__ __launch_bounds__(THREADS, 3) void k_moe_up_few(Call a, W w1, W w3)
+__global__ __launch_bounds__(THREADS, 2) void k_moe_up_few(Call a, W w1, W w3)
 {
     __shared__ FindSpace<FEW * PSK_MOE_MAX_TOP_K> f;
     __shared__ float lds[KW * 128];
     __shared__ v4u places[KW * EXCHANGE];
-    const Found g = find(f, a.n * a.top_k, a.experts, a.crd, blockIdx.y);
+    const Found g = find_few(f, a.n * a.top_k, a.experts, a.crd, blockIdx.y);
     if (g.expert < 0) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = blockIdx.x * 16;
     for (int p0 = 0; p0 < g.count; p0 += 4) {                // more than four: an expert that occurs twice in a row
@@ -141,7 +164,7 @@ __global__ __launch_bounds__(THREADS, 3) void k_moe_down_few(Call a, W w2)
     __shared__ float lds[KW * 64];
     __shared__ v4u places[KW * EXCHANGE];
     typedef Halves<SPAN::T> H;
-    const Found g = find(f, a.n * a.top_k, a.experts, a.crd, blockIdx.y);
+    const Found g = find_few(f, a.n * a.top_k, a.experts, a.crd, blockIdx.y);
     if (g.expert < 0) return;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = blockIdx.x * 16;
     for (int p0 = 0; p0 < g.count; p0 += 4) {
@@ -241,41 +264,47 @@ __global__ __launch_bounds__(THREADS, 3) void k_moe_up(Call a, W w1, W w3)
     for (; t < tiles; ++t) up_tiles<SPAN, HT, SPREAD, 1>(a, w1, w3, g, t, blockIdx.x * 16, lds, places);
 }
 
+// 16 R rows of W2: h in both parts is twice what 16 rows of 16-bit weights are.
 template <class SPAN, int NT, class W>
 __device__ __forceinline__ void down_tiles(const Call &a, const W &w2, const Found &g, int t0, int row0, float *lds, v4u *places)
 {
     typedef Halves<SPAN::T> H;
+    constexpr int R = SPAN::R;
     int lane = threadIdx.x & 63, cols = a.inter;
     asm volatile("" : "+v"(lane), "+s"(cols), "+s"(row0));
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), last = (g.count - 1) >> 4, blocks = copied_blocks(a.inter);
     SPAN span;
-    span.set(0, w2, g.expert, row0, a.dim, lane, cols);
+#pragma unroll
+    for (int r = 0; r < R; ++r) span.set(r, w2, g.expert, row0 + 16 * r, a.dim, lane, cols);
     Copied<H> x[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t) x[t].set(a.h, g.tile + min(t0 + t, last), blocks, lane);
-    v4f acc[1][NT];
+    v4f acc[R][NT], flat[R * NT];
     tile_product<SPAN, NT>(span, x, cols, wave, KW, Exchange(places + EXCHANGE * wave, lane), acc);
-    put_sums<NT>(lds, wave, lane, acc[0]);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int t = 0; t < NT; ++t) flat[r * NT + t] = acc[r][t];
+    put_sums<R * NT>(lds, wave, lane, flat);
     __syncthreads();
-    for (int o = threadIdx.x; o < NT * 256; o += THREADS) {
-        const int t = o >> 8, v = 16 * (t0 + t) + (o >> 4 & 15), i = o & 15;
-        if (v < g.count && row0 + i < a.dim)
-            a.P[(int64_t)a.list[g.first + v] * a.dim + row0 + i] = get_sum<KW, NT, 16>(lds, t, o >> 4 & 15, i) * (1.0f / H::scale);
+    for (int o = threadIdx.x; o < R * NT * 256; o += THREADS) {
+        const int k = o >> 8, v = 16 * (t0 + k % NT) + (o >> 4 & 15), i = row0 + 16 * (k / NT) + (o & 15);
+        if (v < g.count && i < a.dim) a.P[(int64_t)a.list[g.first + v] * a.dim + i] = get_sum<KW, R * NT, 16>(lds, k, o >> 4 & 15, o & 15) * (1.0f / H::scale);
     }
     __syncthreads();
 }
 template <class SPAN, int MOST, class W>
 __global__ __launch_bounds__(THREADS, 3) void k_moe_down(Call a, W w2)
 {
-    __shared__ float lds[KW * MOST * 256];
+    __shared__ float lds[KW * SPAN::R * MOST * 256];
     __shared__ v4u places[KW * EXCHANGE];
     const Found g = a.found[blockIdx.y];
     if (g.expert < 0) return;
-    const int tiles = (g.count + 15) / 16;
+    const int tiles = (g.count + 15) / 16, row0 = blockIdx.x * (16 * SPAN::R);
     int t = 0;
     if constexpr (MOST > 1)
-        for (; t + 1 < tiles; t += MOST) down_tiles<SPAN, MOST>(a, w2, g, t, blockIdx.x * 16, lds, places);
-    for (; t < tiles; ++t) down_tiles<SPAN, 1>(a, w2, g, t, blockIdx.x * 16, lds, places);
+        for (; t + 1 < tiles; t += MOST) down_tiles<SPAN, MOST>(a, w2, g, t, row0, lds, places);
+    for (; t < tiles; ++t) down_tiles<SPAN, 1>(a, w2, g, t, row0, lds, places);
 }
 
 // A lane per element of Y.
@@ -349,7 +378,7 @@ hipError_t launch_layer(const MoeCall &c, const W &w1, const W &w3, const W &w2,
             if (!kept) {
                 PSK_LAUNCH((k_moe_sort<UP>), sort, dim3(THREADS), 0, s, a);
                 PSK_LAUNCH((k_moe_up<UP, DOWN::T, DOWN::SPREAD, MOST, W>), dim3(copied_blocks(c.inter) * 2, slots), dim3(THREADS), 0, s, a, w1, w3);
-                PSK_LAUNCH((k_moe_down<DOWN, MOST, W>), dim3(down, slots), dim3(THREADS), 0, s, a, w2);
+                PSK_LAUNCH((k_moe_down<DOWN, MOST, W>), dim3((down + DOWN::R - 1) / DOWN::R, slots), dim3(THREADS), 0, s, a, w2);
             }
         }
         PSK_LAUNCH(k_moe_join<YT>, dim3((c.dim + 255) / 256, a.n), dim3(256), 0, s, c.dim, c.experts, c.top_k, a.crd, c.vals + t0 * c.top_k, a.P,
