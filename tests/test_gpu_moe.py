@@ -187,6 +187,27 @@ def test_layer_q4(dtype, groups, scale32, n, dim, inter, experts, top_k, kind):
     R.check(y, ref, bound, "q4 %s %s" % (dtype, kind))
 
 
+LONG = [(5, 1024, 1025, 3, 2, "random"), (20, 1100, 2049, 2, 1, "random"), (6, 2300, 40, 3, 2, "holes"), (18, 72, 4096, 2, 2, "one"),
+        (5, 4097, 50, 2, 1, "random"), (7, 40, 4200, 2, 2, "twice"), (4, 2100, 1050, 3, 2, "random"), (37, 700, 530, 2, 1, "random")]
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,dim,inter,experts,top_k,kind", LONG)
+def test_long_columns(dtype, n, dim, inter, experts, top_k, kind):
+    """Columns on both sides of the lengths at which another kernel or another number of waves takes over."""
+    test_layer(dtype, n, dim, inter, experts, top_k, kind)
+    test_layer_q4(dtype, (128, 64) if dtype == "f16" else (32, 256), dtype == "bf16", n, dim, inter, experts, top_k, kind)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,top_k,experts,kind", [(4, 3, 3, "twice"), (4, 17, 20, "random"), (4, 64, 3, "twice"), (4, 16, 16, "holes"), (4, 2, 1024, "random"),
+                                                  (5, 3, 3, "twice"), (5, 64, 70, "random")])
+def test_few_tokens_with_many_entries(dtype, n, top_k, experts, kind):
+    """An expert more than four times among four tokens' entries, more than 64 entries, and five tokens beside four."""
+    test_layer(dtype, n, 40, 24, experts, top_k, kind)
+    test_layer_q4(dtype, (32, 32), False, n, 40, 24, experts, top_k, kind)
+
+
 def test_matrices_with_groups_and_zero_points_of_their_own():
     """The last matrix has a group of its own, and each of the three zero points or none."""
     rng = np.random.default_rng(16)

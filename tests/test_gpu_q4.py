@@ -45,6 +45,16 @@ def test_products(dtype, rows, cols, n, group, zeros, scale32):
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("rows,cols,n,group,zeros,scale32", [
+    (37, 255, 5, 32, True, False), (65, 1024, 16, 64, False, False), (16, 1025, 17, 32, True, True), (130, 2047, 5, 128, True, False),
+    (33, 2048, 33, 512, True, False), (17, 2049, 48, 32, False, False), (5000, 1056, 6, 256, True, False), (47, 4096, 16, 4096, True, True),
+    (31, 4095, 21, 64, True, False), (40, 4097, 5, 32, True, False), (40, 4097, 40, 128, False, True), (9000, 100, 17, 128, True, False)])
+def test_where_the_way_for_more_vectors_changes(dtype, rows, cols, n, group, zeros, scale32):
+    """Columns on both sides of every length at which another kernel or another number of waves takes over, few and many sets of rows."""
+    test_products(dtype, rows, cols, n, group, zeros, scale32)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
 def test_strides_and_what_lies_behind_the_rows(dtype):
     """Rows of X that start at odd elements between NaN, rows of codes and scales farther apart than they need, Y in a wider buffer."""
     t, rows, cols, n, group = TYPES[dtype], 37, 205, 7, 64
@@ -118,9 +128,10 @@ def test_empty_products():
     assert bool((y == 0).all())
 
 
-def test_codes_beyond_four_gigabytes():
+@pytest.mark.parametrize("rows,cols,n", [((1 << 20) + 37, 8192 + 64, 3), ((1 << 20) + 37, 8192 + 64, 20), ((1 << 21) + (1 << 17) + 37, 4096, 5)])
+def test_codes_beyond_four_gigabytes(rows, cols, n):
     """A vocabulary's worth of rows whose offsets pass 32 bits; the first and last rows and some in between are checked."""
-    rows, cols, group, n = (1 << 20) + 37, 8192 + 64, 128, 3
+    group = 128
     g = torch.Generator(device="cuda")
     g.manual_seed(3)
     codes = torch.randint(0, 256, (rows, (cols + 31) // 32 * 16), generator=g, device="cuda", dtype=torch.uint8)
@@ -174,5 +185,5 @@ def test_results_do_not_change_from_run_to_run():
     first = product(w, x, 3000, 64).clone()
     for _ in range(5):
         assert torch.equal(first, product(w, x, 3000, 64))
-    # a vector's result does not depend on the ones beside it
-    assert torch.equal(first[4:5], product(w, x[4:5], 3000, 64))
+    # a vector's result does not depend on the ones beside it, as long as the same kernel takes it
+    assert torch.equal(first[4:9], product(w, x[4:9], 3000, 64))
