@@ -33,15 +33,15 @@ struct Found {
 template <int MOST>
 struct FindSpace {
     int seen[PSK_MOE_MAX_EXPERTS];
-    int count;
+    int counts[KW];
     unsigned short list[MOST];
 };
-// The j-th expert that occurs (in the order of the experts) and its positions in `list`.  expert -1: fewer occur.
+// The j-th expert that occurs (in the order of the experts) and its positions in `list`, ascending: all workgroups that ask for an expert
+// have to see the same order.  expert -1: fewer occur.
 template <int MOST>
 __device__ __forceinline__ Found find(FindSpace<MOST> &f, int positions, int experts, const int *__restrict__ crd, int j)
 {
     for (int e = threadIdx.x; e < experts; e += THREADS) f.seen[e] = 0;
-    if (threadIdx.x == 0) f.count = 0;
     __syncthreads();
     for (int p = threadIdx.x; p < positions; p += THREADS) {
         const int e = crd[p];
@@ -67,12 +67,29 @@ __device__ __forceinline__ Found find(FindSpace<MOST> &f, int positions, int exp
         r.first += sum & 0xffff;
         r.tile += sum >> 16;
     }
-    if (r.expert >= 0) {
-        for (int p = threadIdx.x; p < positions; p += THREADS)
-            if (crd[p] == r.expert) f.list[atomicAdd(&f.count, 1)] = (unsigned short)p;
+    // every wave looks through a run of positions, first for how many there are in it
+    const int wave = threadIdx.x >> 6, run = (positions + THREADS - 1) / THREADS * WAVE, end = min((wave + 1) * run, positions);
+    int mine = 0;
+    for (int p0 = wave * run; p0 < end; p0 += WAVE) {
+        const int p = p0 + lane;
+        mine += __popcll(__ballot(p < end && r.expert >= 0 && crd[min(p, end - 1)] == r.expert));
     }
+    if (lane == 0) f.counts[wave] = mine;
     __syncthreads();
-    r.count = f.count;
+    int at = 0;
+    for (int w = 0; w < KW; ++w) {
+        if (w < wave) at += f.counts[w];
+        r.count += f.counts[w];
+    }
+    if (mine)
+        for (int p0 = wave * run; p0 < end; p0 += WAVE) {
+            const int p = p0 + lane;
+            const bool here = p < end && crd[min(p, end - 1)] == r.expert;
+            const unsigned long long b = __ballot(here);
+            if (here) f.list[at + __popcll(b & ((1ull << lane) - 1))] = (unsigned short)p;
+            at += __popcll(b);
+        }
+    __syncthreads();
     return r;
 }
 

@@ -192,6 +192,31 @@ LONG = [(5, 1024, 1025, 3, 2, "random"), (20, 1100, 2049, 2, 1, "random"), (6, 2
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,dim,inter,experts,top_k", [(24, 1500, 200, 8, 4), (65, 2100, 40, 3, 2), (600, 1030, 24, 5, 3), (300, 520, 16, 64, 8)])
+def test_many_positions_and_columns(dtype, n, dim, inter, experts, top_k):
+    """More positions than a wave looks at, with columns for several workgroups: all see an expert's positions in one order."""
+    rng = np.random.default_rng(n)
+    t = TYPES[dtype]
+    x = torch.from_numpy(rng.standard_normal((n, dim))).to(t)
+    crd, vals = gating(rng, n, experts, top_k)
+    w = [padded(rng, s, 1 / math.sqrt(s[2]), t) for s in ((experts, inter, dim), (experts, inter, dim), (experts, dim, inter))]
+    d = [doubles(m) for m in w]
+    ref, bound = R.layer(x, crd, vals, *d, 0, t, PARTS[dtype])
+    first = run16(x, crd, vals, *w)
+    R.check(first, ref, bound, "16 bits")
+    w = [R.q4_weights(rng, r, c, 64, True, t, experts, scale=0.4 / math.sqrt(c)) for r, c in ((inter, dim), (inter, dim), (dim, inter))]
+    ref, bound = R.layer(x, crd, vals, *(q4_doubles(m, c, 64) for m, c in zip(w, (dim, dim, inter))), 0, t, 2.0 ** -16)
+    A = [q4_of(m, c, 64) for m, c in zip(w, (dim, dim, inter))]
+    y = torch.empty(n, dim, dtype=t, device="cuda")
+    psk.psk_moe_experts_q4(x.cuda(), crd.cuda(), vals.cuda(), *A, y)
+    R.check(y, ref, bound, "4 bits")
+    for _ in range(3):
+        again = torch.empty_like(y)
+        psk.psk_moe_experts_q4(x.cuda(), crd.cuda(), vals.cuda(), *A, again)
+        assert torch.equal(again, y)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("n,dim,inter,experts,top_k,kind", LONG)
 def test_long_columns(dtype, n, dim, inter, experts, top_k, kind):
     """Columns on both sides of the lengths at which another kernel or another number of waves takes over."""
