@@ -74,7 +74,7 @@ typedef enum {
     PSK_ERR_WORKSPACE = 4,   /* workspace NULL, misaligned or smaller than psk_workspace_bytes */
     PSK_ERR_UNSUPPORTED = 5, /* unknown op / variant / phases */
     PSK_ERR_HIP = 6,         /* the HIP runtime reported an error at launch */
-    PSK_ERR_ALIGNMENT = 7    /* BCSR: vals (and x for SpMV) not 16-byte aligned; fp64 SpMV: an operand not 8-byte aligned */
+    PSK_ERR_ALIGNMENT = 7    /* BCSR: vals (and x for SpMV) not 16-byte aligned; fp64 SpMV: an operand not 8-byte aligned; 4-bit codes: not 16-byte */
 } psk_status;
 
 typedef enum {
@@ -576,9 +576,10 @@ int psk_moe_route(int64_t n, int64_t dim, int64_t experts, int32_t top_k, int sc
  * The layer: Y(t,:) = sum_s vals[t,s] * W2_e (act(W1_e X(t,:)) * (W3_e X(t,:))), e = crd[t,s], for n tokens of `type` (PSK_F16 or
  * PSK_BF16).  An entry outside [0, experts) stands for none; a token without entries gets zeros.  An expert may occur
  * twice in a row.  W1, W3: inter x dim, W2: dim x inter for each expert.
- * Made for a few tokens: the matrices of the experts that occur are read once for up to 64 entries of an expert.
- * psk_moe_experts: weights of `type`, matrix e of W1 and W3 at stride1*e elements, rows ld1 apart (W2: stride2, ld2); bases 16-byte aligned,
- * strides and leading dimensions multiples of 8.
+ * Made for a few tokens: the matrices of the experts that occur are read once for up to 32 entries of an expert (4-bit weights: 16; up to
+ * four tokens: 4).
+ * psk_moe_experts: weights of `type`, matrix e of W1 and W3 at stride1*e elements, rows ld1 apart (W2: stride2, ld2).  No alignment beyond the
+ * element's is asked of them; rows that begin at multiples of 16 bytes are read fastest.
  * psk_moe_experts_q4: weights in 4 bits, count = experts in all three, W1 and W3 alike in rows, cols and group, all with one scale_type.
  * With PSK_F16 and 16-bit weights, values between the two products of 2^24 and more become infinite.
  * The workspace is for both.

@@ -114,8 +114,7 @@ int psk_moe_experts(int64_t n, int64_t dim, int64_t inter, int64_t experts, int3
     if (!workspace_ok(workspace, workspace_bytes, moe_workspace_bytes(n, dim, inter, experts, top_k))) return PSK_ERR_WORKSPACE;
     if (n == 0) return PSK_OK;
     if (!X || !crd || !vals || !W1 || !W3 || !W2 || !Y) return PSK_ERR_NULL;
-    if (misaligned(X, 2) || misaligned(Y, 2) || misaligned(crd, 4) || misaligned(vals, 4) || misaligned(W1, 16) || misaligned(W3, 16) || misaligned(W2, 16) ||
-        ld1 % 8 || ld2 % 8 || (experts > 1 && (stride1 % 8 || stride2 % 8)))
+    if (misaligned(X, 2) || misaligned(Y, 2) || misaligned(crd, 4) || misaligned(vals, 4) || misaligned(W1, 2) || misaligned(W3, 2) || misaligned(W2, 2))
         return PSK_ERR_ALIGNMENT;
     const MoeCall c = {n, (int)dim, (int)inter, (int)experts, top_k, act, X, ldx, crd, vals, Y, ldy, workspace};
     return hip_status(launch_moe_16(c, type, W1, W3, ld1, stride1, W2, ld2, stride2, static_cast<hipStream_t>(stream)));

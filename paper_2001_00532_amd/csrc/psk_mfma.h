@@ -272,7 +272,7 @@ struct Span16 {
 #pragma unroll
                 for (int i = 0; i < 2; ++i)
                     g.w[r][u][i] = TAIL ? load8(p[r][i], c * CH + 64 * u, left)
-                                        : __builtin_nontemporal_load(reinterpret_cast<const v4u *>(p[r][i] + c * CH + 64 * u));
+                                        : __builtin_nontemporal_load(reinterpret_cast<const v4u_u *>(p[r][i] + c * CH + 64 * u));
     }
     static __device__ __forceinline__ void exchange(const Regs &g, const Exchange &place, v4u (&all)[R][B])
     {

@@ -287,6 +287,27 @@ def test_values_between_the_products_beyond_the_range_of_f16():
     R.check(run16(x, crd, vals, w1, w1, w2), ref, bound, "large h")
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n,dim,inter", [(1, 1231, 311), (3, 77, 129), (9, 1231, 311), (50, 333, 45), (7, 9, 3)])
+def test_weights_at_any_element(dtype, n, dim, inter):
+    """Rows of weights that begin at odd elements, NaN around them; and weights without any padding, up to the end of their tensor."""
+    t, experts, top_k = TYPES[dtype], 5, 2
+    rng = np.random.default_rng(dim)
+    x = torch.from_numpy(rng.standard_normal((n, dim))).to(t)
+    crd, vals = gating(rng, n, experts, top_k)
+
+    def loose(shape):
+        e, r, c = shape
+        buf = torch.full((e, r + 1, c + 3), float("nan"), dtype=t)
+        buf[:, 1:, 3:] = torch.from_numpy(rng.standard_normal(shape) / math.sqrt(c)).to(t)
+        return buf.cuda()[:, 1:, 3:]
+    w = [loose(s) for s in ((experts, inter, dim), (experts, inter, dim), (experts, dim, inter))]
+    ref, bound = R.layer(x, crd, vals, *map(doubles, w), 0, t, PARTS[dtype])
+    got = run16(x, crd, vals, *w)
+    R.check(got, ref, bound, "odd strides")
+    assert torch.equal(got, run16(x, crd, vals, *(m.contiguous() for m in w)))
+
+
 def test_one_matrix_holds_both_halves():
     """W1 and W3 as the halves of one tensor, experts a stride apart."""
     rng = np.random.default_rng(14)

@@ -84,8 +84,7 @@ def test_layer_refuses():
     assert layer(ws=NULL) == 4 and layer(have=psk.psk_moe_workspace_bytes(4, 100, 48, 10, 3) - 1) == 4
     for over in (dict(act=2), dict(type=psk.PSK_F32), dict(type=3)):
         assert layer(**over) == 5, over
-    for over in (dict(X=ODD), dict(Y=ODD), dict(W1=ctypes.c_void_p(264)), dict(W3=ctypes.c_void_p(264)), dict(W2=ctypes.c_void_p(264)), dict(ld1=101), dict(ld2=50),
-                 dict(stride1=4), dict(crd=ctypes.c_void_p(258))):
+    for over in (dict(X=ODD), dict(Y=ODD), dict(W1=ODD), dict(W3=ODD), dict(W2=ODD), dict(crd=ctypes.c_void_p(258))):
         assert layer(**over) == 7, over
     assert psk.psk_moe_workspace_bytes(4, 100, 0, 10, 3) == 0 and psk.psk_moe_workspace_bytes(4, 100, 48, 2000, 3) == 0
     # more tokens than one pair of launches takes need no more room
