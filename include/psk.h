@@ -562,8 +562,8 @@ int psk_gemm_q4(const psk_q4 *A, int64_t n, int type, const void *X, int64_t ldx
  *   l(t,e) = sum_j X[t][j] W[e][j]                     p = softmax of l(t,:), or 1 / (1 + exp(-l))
  * The top_k experts with the largest l are taken, or with a bias (float[experts], NULL: none) those with the largest p + bias,
  * the larger ones first, equal ones by their index; one whose bias is -infinity is never taken.  Where fewer remain, the rest
- * of the row is crd = -1, vals = 0.  What is no number comes last.  gate = p, divided by the sum of the taken p with normalise,
- * times factor.  Logits and scores are computed in 64 bits, so the choice does not depend on the order of a sum.
+ * of the row is crd = -1, vals = 0.  What is no number comes last.  gate = p, divided by the sum of the taken p with normalise
+ * (unless that is zero), times factor.  Logits and scores are computed in 64 bits, so the choice does not depend on the order of a sum.
  * wtype is PSK_F32 or `type`.
  */
 enum { PSK_SCORE_SOFTMAX = 0, PSK_SCORE_SIGMOID = 1 };

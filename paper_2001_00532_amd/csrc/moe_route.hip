@@ -188,7 +188,7 @@ __global__ __launch_bounds__(PSK_MOE_MAX_EXPERTS) void k_route_rank(int experts,
         __syncthreads();
         double total = 0;
         for (int i = 0; i < top_k; ++i) total += gates[i];
-        p /= total;
+        if (total != 0) p /= total;                          // (scores that all underflowed stay zeros)
     }
     if (chosen) {
         crd[t * top_k + rank] = e;

@@ -89,6 +89,14 @@ def test_experts_that_are_never_taken_and_rows_that_are_no_numbers(score):
     compare_route(x, w, 3, score, None, False, 1.0, "far logits")
 
 
+def test_scores_that_underflow():
+    x, w = torch.full((2, 1), 1000.0), torch.tensor([[-1.0], [-2.0], [-3.0], [0.0]])
+    crd, vals = routed(x, w, 3, score=1, bias=torch.tensor([0.0, 0.0, 0.0, -math.inf]))
+    assert crd.tolist() == [[0, 1, 2]] * 2 and vals.tolist() == [[0.0, 0.0, 0.0]] * 2
+    crd, vals = routed(x, w, 3, score=0)
+    assert crd.tolist() == [[3, 0, 1]] * 2 and vals.tolist() == [[1.0, 0.0, 0.0]] * 2
+
+
 def test_route_strides():
     rng = np.random.default_rng(5)
     x, w = torch.from_numpy(rng.standard_normal((5, 90))).half(), torch.from_numpy(rng.standard_normal((12, 95))).half()
