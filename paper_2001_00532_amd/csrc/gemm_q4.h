@@ -2,8 +2,14 @@
 //
 //   Y[t][i] = sum_g s_ig sum_{j in g} (q_ij - z_ig) X[t][j]
 //
-// Bound by reading the codes once (half a byte per weight).  A workgroup owns 16 R rows; its waves share the columns, and their sums
-// meet in LDS.
+// The codes less their zero points are exact in the operands, and the scale multiplies a group's sum in 32 bits, so only sums and the result
+// are rounded.  Bound by reading the codes once (half a byte per weight) and, from five vectors on, by the instructions that
+// dequantise them.  A workgroup owns 16 R rows; its waves share the columns, and their sums meet in LDS.
+//
+// Three ways, by the rules in by_group, more_vectors and few_vectors_by_columns:
+//   up to four vectors            k_gemv_q4        32768 x 8192, one vector of bf16, groups of 64: 29.7 us = 4.8 TB/s of codes and scales
+//   more, up to 4096 columns      k_gemm_q4_kept   10240 x 4096, 16 vectors of bf16: 10.2 us; 8192 x 4096, 64 vectors of f16: 16.5 us
+//   more, longer rows             k_gemm_q4        4096 x 8192, 16 vectors of bf16: 9.6 us; 64 vectors of f16: 17.4 us
 #pragma once
 #include "psk_internal.h"
 #include "psk_mfma.h"
@@ -14,7 +20,10 @@ namespace {
 template <int XT> struct Vectors { typedef Plain16<XT> type; };
 template <> struct Vectors<F32> { typedef Parts32 type; };
 
-// Up to four vectors, 16 R rows.
+// Up to four vectors, 16 R rows.  A matrix instruction has room for 16 vectors: its rows 4 v + j hold columns of block j of vector v, so four
+// blocks of columns are one load of vectors, and of each block's product the lane keeps the element that is its vector's.
+// R = 1: two sets of rows per workgroup are slower (32768 x 8192 29 to 33 us, with one 28; 4096 x 4096 6.9 and 4.8), there are fewer waves to
+// ask for memory.
 template <int XT, int S, int GB, bool Z, int R, int P, int KW>
 __global__ __launch_bounds__(64 * KW) void k_gemv_q4(WeightsQ4 A, int n, const void *X, int64_t ldx, void *Y, int64_t ldy)
 {
@@ -38,7 +47,8 @@ __global__ __launch_bounds__(64 * KW) void k_gemv_q4(WeightsQ4 A, int n, const v
     }
 }
 
-// The copy of the vectors for k_gemm_q4: a wave per tile and four blocks.
+// The copy of the vectors for k_gemm_q4 (and of those of 32 bits for k_gemm_q4_kept), in the order of the operands: a lane's load is then 16 bytes of a
+// kilobyte in one piece, where the rows themselves would cost a compute unit twice the time.  A wave per tile and four blocks.
 template <int XT, int GB>
 __global__ __launch_bounds__(256) void k_gemm_q4_copy(int n, int cols, const void *X, int64_t ldx, v4u *copy)
 {
@@ -50,7 +60,7 @@ __global__ __launch_bounds__(256) void k_gemm_q4_copy(int n, int cols, const voi
     copy_block<SPAN>(x, cols, block, lane, copy + (int64_t)tile * blocks * V::P * 64);
 }
 
-// NT tiles of 16 vectors, 16 R rows.
+// NT tiles of 16 vectors, 16 R rows: for rows that are too long to keep the vectors.
 template <int XT, int S, int GB, bool Z, int R, int NT, int KW>
 __global__ __launch_bounds__(64 * KW) void k_gemm_q4(WeightsQ4 A, int n, const v4u *copy, void *Y, int64_t ldy)
 {
@@ -81,7 +91,11 @@ __global__ __launch_bounds__(64 * KW) void k_gemm_q4(WeightsQ4 A, int n, const v
 }
 
 // Up to 256 KW columns: the vectors kept (KeptQ4), workgroups that stay.  16-bit vectors are brought into the operands' order here; those of 32
-// bits come from the copy.
+// bits come from the copy.  Takes 9 vector instructions per eight codes of f16 and 19 of bf16, and these bound it: weights of two or three sets
+// of rows requested ahead instead of one take as long (10.3, 11.1 and 11.5 us for 10240 x 4096 times 16).
+// 10240 x 4096 times 16 vectors 10.2 us, by k_gemm_q4 with its copy 13.3; 8192 x 4096 times 64 16.5, by k_gemm_q4 23.
+// Beyond 4096 columns it would take more than the 16 waves of a workgroup.
+// Vectors of 32 bits hold three parts and 16 waves of them do not fit into the registers (200 bytes per lane go to scratch).
 template <int XT, int S, int GB, int KW>
 __global__ __launch_bounds__(64 * KW) void k_gemm_q4_kept(WeightsQ4 A, int n, const void *X, int64_t ldx, const v4u *copy, void *Y, int64_t ldy)
 {
@@ -112,6 +126,8 @@ void few_vectors(const WeightsQ4 &A, int n, const void *X, int64_t ldx, void *Y,
 {
     PSK_LAUNCH((k_gemv_q4<XT, S, GB, Z, 1, P, 4>), dim3((A.rows + 15) / 16), dim3(256), 0, s, A, n, X, ldx, Y, ldy);
 }
+// Four pieces of 128 columns in a chunk for long rows, two for short ones, of which no wave would else get one: 4096 x 4096 4.4 us (two: 5.3),
+// 1024 x 1024 2.9 (two: 2.7).  Vectors of 32 bits: two, four would not fit into the registers.
 template <int XT, int S, int GB, bool Z>
 void few_vectors_by_columns(const WeightsQ4 &A, int n, const void *X, int64_t ldx, void *Y, int64_t ldy, hipStream_t s)
 {
@@ -120,6 +136,7 @@ void few_vectors_by_columns(const WeightsQ4 &A, int n, const void *X, int64_t ld
     else few_vectors<XT, S, GB, Z, 2>(A, n, X, ldx, Y, ldy, s);
 }
 // Workgroups for KeptQ4: as many as are on the chip at once (1024 threads to a compute unit) for all tiles together, no more than sets of rows.
+// 8192 x 4096 times 64, 16 waves: 64 workgroups for each of four tiles 16.7 us, 128 19.5, 256 26; 10240 x 2048 times 16, 8 waves: 512 6.5 us, 320 7.1, 256 6.7.
 inline int kept_groups(int sets, int tiles, int kw)
 {
     const int n = 256 * (16 / kw) / tiles;
@@ -137,6 +154,8 @@ void more_vectors(const WeightsQ4 &A, int n, const void *X, int64_t ldx, void *Y
     const int rows = (A.rows + 15) / 16, tiles = (n + 15) / 16;
     v4u *copy = static_cast<v4u *>(space);
     const bool kept = kept_fits(A);
+    // Longer rows: one tile and set of rows per workgroup where there is one tile (10240 x 4096 times 16 13.3 us, two sets of rows 13.7 to 15.7) or there
+    // would be few workgroups (2048 x 8192 times 32 9.0 us, two and two 15.9; 2048 x 8192 times 64, 512 workgroups, in f32 27, two sets of rows 20).
     // (kept vectors are in natural order, as for groups of 32 columns)
     if (!kept) PSK_LAUNCH((k_gemm_q4_copy<XT, GB>), dim3(copied_blocks(A.cols) / 4, tiles), dim3(256), 0, s, n, A.cols, X, ldx, copy);
     else if (XT == F32) PSK_LAUNCH((k_gemm_q4_copy<XT, 1>), dim3(copied_blocks(A.cols) / 4, tiles), dim3(256), 0, s, n, A.cols, X, ldx, copy);
@@ -144,13 +163,14 @@ void more_vectors(const WeightsQ4 &A, int n, const void *X, int64_t ldx, void *Y
         if (A.cols <= 1024) kept_vectors<XT, S, GB, 4>(A, n, X, ldx, Y, ldy, copy, s);
         else if (A.cols <= 2048) kept_vectors<XT, S, GB, 8>(A, n, X, ldx, Y, ldy, copy, s);
         else kept_vectors<XT, S, GB, 16>(A, n, X, ldx, Y, ldy, copy, s);
-    } else if (n <= 16) PSK_LAUNCH((k_gemm_q4<XT, S, GB, true, 1, 1, 4>), dim3(rows, 1), dim3(256), 0, s, A, n, copy, Y, ldy);
+    } else if (tiles == 1 || (int64_t)rows * tiles <= 256) PSK_LAUNCH((k_gemm_q4<XT, S, GB, true, 1, 1, 4>), dim3(rows, tiles), dim3(256), 0, s, A, n, copy, Y, ldy);
     else if constexpr (XT == F32) PSK_LAUNCH((k_gemm_q4<XT, S, GB, true, 2, 1, 4>), dim3((rows + 1) / 2, tiles), dim3(256), 0, s, A, n, copy, Y, ldy);
     else PSK_LAUNCH((k_gemm_q4<XT, S, GB, true, 2, 2, 4>), dim3((rows + 1) / 2, (tiles + 1) / 2), dim3(256), 0, s, A, n, copy, Y, ldy);
 }
 template <int XT, int S>
 void by_group(const WeightsQ4 &A, int n, const void *X, int64_t ldx, void *Y, int64_t ldy, void *space, hipStream_t s)
 {
+    // four vectors: 10240 x 4096 8.6 us here, 10.1 with the vectors kept; 2048 x 1024 2.9 and 4.0
     if (n > 4) {
         if (A.shift == 5) more_vectors<XT, S, 1>(A, n, X, ldx, Y, ldy, space, s);
         else if (A.shift == 6) more_vectors<XT, S, 2>(A, n, X, ldx, Y, ldy, space, s);

@@ -7,6 +7,8 @@ namespace psk {
 namespace {
 
 // ---- more than four tokens, up to KEPT_COLUMNS columns in both products: the vectors kept (KeptQ4)
+// 48 tokens, 8 of 64 experts of 3 x 1000 x 2048 in f16: 36.9 us for the first step and 29.8 for the second; by k_moe_up and k_moe_down the whole
+// layer took 154 us, by the first form of these 90.  The matrices once would be 29 us: instructions that dequantise share the time with the loads.
 template <int T, int GB, int S, int KW>
 __global__ __launch_bounds__(64 * KW, 4) void k_moe_q4_up(Call a, WeightsQ4 w1, WeightsQ4 w3)
 {
