@@ -9,7 +9,7 @@ static_assert(PSK_F32 == F32 && PSK_F16 == F16 && PSK_BF16 == BF16, "types");
 
 namespace {
 
-constexpr int64_t kMaxEdge = int64_t(1) << 30;            // rows and columns: column numbers are rounded up in 32 bits
+constexpr int64_t kMaxEdge = int64_t(1) << 28;            // rows and columns: places in the copy of a tile of vectors are counted in 32 bits
 
 inline int hip_status(hipError_t e) { return e == hipSuccess ? PSK_OK : PSK_ERR_HIP; }
 inline bool type_ok(int t) { return t == PSK_F32 || t == PSK_F16 || t == PSK_BF16; }

@@ -132,7 +132,9 @@ template <int XT, int S, int GB, bool Z>
 void few_vectors_by_columns(const WeightsQ4 &A, int n, const void *X, int64_t ldx, void *Y, int64_t ldy, hipStream_t s)
 {
     constexpr int LONG = XT == F32 ? 2 : 4;
-    if (A.cols >= 2048) few_vectors<XT, S, GB == 8 ? 4 * LONG : GB, Z, LONG>(A, n, X, ldx, Y, ldy, s);
+    // (GB = 8 stands for groups of 256 columns and more, of which a long chunk may hold two)
+    if (A.cols >= 2048 && GB == 8 && A.shift > 8) few_vectors<XT, S, GB == 8 ? 4 * LONG : GB, Z, LONG>(A, n, X, ldx, Y, ldy, s);
+    else if (A.cols >= 2048) few_vectors<XT, S, GB, Z, LONG>(A, n, X, ldx, Y, ldy, s);
     else few_vectors<XT, S, GB, Z, 2>(A, n, X, ldx, Y, ldy, s);
 }
 // Workgroups for KeptQ4: as many as are on the chip at once (1024 threads to a compute unit) for all tiles together, no more than sets of rows.

@@ -55,6 +55,23 @@ def test_where_the_way_for_more_vectors_changes(dtype, rows, cols, n, group, zer
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("cols", [512, 2048, 2600, 4099])
+@pytest.mark.parametrize("group", [32, 64, 128, 256, 512, 1024, 1 << 30])
+def test_every_group_with_few_and_more_vectors(dtype, cols, group):
+    """Groups smaller and larger than what a wave takes at once, short and long rows."""
+    for n, zeros in ((1, True), (4, False), (7, True)):
+        test_products(dtype, 19, cols, n, group, zeros, False)
+
+
+def test_very_many_vectors():
+    rng = np.random.default_rng(10)
+    w = R.q4_weights(rng, 17, 40, 32, True, torch.float16)
+    x = torch.from_numpy(rng.standard_normal((200001, 40))).half()
+    ref, bound = R.gemm(R.dequantised(*w, 40, 32), x, torch.float16)
+    R.check(product(w, x.cuda(), 40, 32), ref, bound, "200001 vectors")
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
 def test_strides_and_what_lies_behind_the_rows(dtype):
     """Rows of X that start at odd elements between NaN, rows of codes and scales farther apart than they need, Y in a wider buffer."""
     t, rows, cols, n, group = TYPES[dtype], 37, 205, 7, 64

@@ -31,7 +31,7 @@ def test_gemm_q4_refuses():
     for over in (dict(codes=0), dict(scales=0)):
         assert gemm(q4(**over)) == 1, over
     assert gemm(X=NULL) == 1 and gemm(Y=NULL) == 1
-    for over in (dict(rows=-1), dict(cols=-1), dict(cols=2 ** 30 + 1), dict(rows=2 ** 31), dict(group=0), dict(group=16), dict(group=96), dict(group=-32),
+    for over in (dict(rows=-1), dict(cols=-1), dict(cols=2 ** 28 + 1), dict(rows=2 ** 31), dict(group=0), dict(group=16), dict(group=96), dict(group=-32),
                  dict(ld_codes=48), dict(ld_scales=3), dict(count=2), dict(count=0), dict(count=-1)):
         assert gemm(q4(**over)) == 2, over
     assert gemm(n=-1) == 2 and gemm(n=psk.PSK_MAX_VECTORS + 1) == 2 and gemm(ldx=99) == 2 and gemm(ldy=47) == 2
