@@ -295,6 +295,20 @@ def test_values_between_the_products_beyond_the_range_of_f16():
     R.check(run16(x, crd, vals, w1, w1, w2), ref, bound, "large h")
 
 
+@pytest.mark.parametrize("n", [3, 9])
+def test_small_values_between_the_products(n):
+    """h of about 10^-6 with large weights behind it."""
+    rng = np.random.default_rng(18)
+    dim, inter, t = 64, 200, torch.float16
+    x = torch.from_numpy(rng.standard_normal((n, dim)) * 1e-2).half()
+    w1 = torch.from_numpy(rng.standard_normal((1, inter, dim)) * 1e-2).half()
+    w2 = torch.from_numpy(rng.standard_normal((1, dim, inter)) * 1e3).half()
+    crd, vals = torch.zeros(n, 1, dtype=torch.int32), torch.ones(n, 1)
+    # the two parts of h are steps of 2^-24 after factors of 2^-8 and 2^11: 2^-24 2^8 2^-11 = 2^-27, half of it the error, which is in the bound
+    ref, bound = R.layer(x, crd, vals, doubles(w1), doubles(w1), doubles(w2), 0, t, PARTS["f16"])
+    R.check(run16(x, crd, vals, w1, w1, w2), ref, bound, "small h")
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("n,dim,inter", [(1, 1231, 311), (3, 77, 129), (9, 1231, 311), (50, 333, 45), (7, 9, 3)])
 def test_weights_at_any_element(dtype, n, dim, inter):
@@ -327,6 +341,28 @@ def test_one_matrix_holds_both_halves():
     a = run16(x, crd, vals, both[:, :inter], both[:, inter:], w2)
     b = run16(x, crd, vals, both[:, :inter].contiguous(), both[:, inter:].contiguous(), w2)
     assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("n", [2, 9])
+def test_two_calls_at_once(n):
+    """Two streams, a workspace each: what both give alone."""
+    rng = np.random.default_rng(17)
+    dim, inter, experts, t = 1100, 600, 6, torch.bfloat16
+    w = [torch.from_numpy(rng.standard_normal(s) * 0.05).to(t).cuda() for s in ((experts, inter, dim), (experts, inter, dim), (experts, dim, inter))]
+    calls = []
+    for _ in range(2):
+        x = torch.from_numpy(rng.standard_normal((n, dim))).to(t).cuda()
+        crd, vals = (v.cuda() for v in gating(rng, n, experts, 2))
+        calls.append((x, crd, vals, torch.empty_like(x), torch.empty_like(x), psk.psk_moe_workspace(n, dim, inter, experts, 2), torch.cuda.Stream()))
+    for x, crd, vals, alone, _, ws, _ in calls:
+        psk.psk_moe_experts(x, crd, vals, *w, alone, ws=ws)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for x, crd, vals, _, y, ws, stream in calls:
+            psk.psk_moe_experts(x, crd, vals, *w, y, ws=ws, stream=stream)
+    torch.cuda.synchronize()
+    for _, _, _, alone, y, _, _ in calls:
+        assert torch.equal(alone, y)
 
 
 # ------------------------------------------------------------------ together

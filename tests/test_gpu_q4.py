@@ -118,6 +118,16 @@ def test_special_values(dtype):
     assert not bool(torch.isfinite(got[:6, 5]).any())
 
 
+@pytest.mark.parametrize("n", [1, 6, 20])
+@pytest.mark.parametrize("cols", [300, 5000])
+def test_activations_below_the_smallest_normal_f16(n, cols):
+    rng = np.random.default_rng(11)
+    w = R.q4_weights(rng, 20, cols, 64, True, torch.float16, scale=50)
+    x = torch.from_numpy(rng.standard_normal((n, cols)) * 5e-6).half()
+    ref, bound = R.gemm(R.dequantised(*w, cols, 64), x, torch.float16)
+    R.check(product(w, x.cuda(), cols, 64), ref, bound, "denormal activations")
+
+
 def test_vectors_of_32_bits_keep_their_bits():
     """Values whose low bits matter: sums that cancel to the last bits of the activations."""
     rows, cols = 16, 256
