@@ -683,9 +683,9 @@ def _type(t, what):
 
 def _rows(t, rows, cols, dtype, what):
     """(address, leading dimension) of a matrix of rows x cols."""
-    if t.dim() != 2 or tuple(t.shape) != (rows, cols):
+    if t.shape != (rows, cols):
         raise ValueError("%s: expected a tensor of %d x %d, got %s" % (what, rows, cols, tuple(t.shape)))
-    return _ptr(t, dtype), (int(t.stride(0)) if rows > 1 else max(int(t.stride(0)), cols))
+    return _ptr(t, dtype), (t.stride(0) if rows > 1 else max(t.stride(0), cols))
 
 
 def _gating_ptrs(crd, vals, n, top_k, what):
@@ -697,9 +697,9 @@ def _gating_ptrs(crd, vals, n, top_k, what):
 
 def _one_device(what, *tensors):
     """A call runs on the current device: all of its tensors have to be there."""
-    here = torch.cuda.current_device()
+    here = torch._C._cuda_getDevice()
     for t in tensors:
-        if t is not None and t.is_cuda and t.get_device() != here:
+        if t is not None and t.get_device() != here and t.is_cuda:
             raise ValueError("%s: a tensor is on cuda:%d, the current device is cuda:%d" % (what, t.get_device(), here))
 
 
@@ -733,6 +733,9 @@ class Q4:
         d.ld_scales = max(int(scales.stride(-2)), groups) if codes.shape[-2] <= 1 else int(scales.stride(-2))
         if codes.dim() == 3 and codes.shape[0] > 1:
             d.stride_codes, d.stride_scales = int(codes.stride(0)), int(scales.stride(0))
+        if any(t is not None and t.device != codes.device for t in (scales, zeros)):
+            raise ValueError("codes, scales and zeros must be on one device")
+        self.rows, self.cols, self._ref = d.rows, d.cols, ctypes.byref(d)      # (a field of the struct costs a call ten times as much)
 
 
 def psk_gemm_q4_workspace_bytes(rows: int, cols: int, n: int, type: int) -> int:
@@ -749,13 +752,13 @@ def psk_gemm_q4_workspace(A: Q4, X, stream=None):
 
 def psk_gemm_q4(A: Q4, X, Y, ws=None, stream=None):
     """Y (n x rows) = X (n x cols) A^T for one matrix in 4 bits."""
-    n, type = X.shape[0], _type(X, "psk_gemm_q4")
-    x, ldx = _rows(X, n, A.desc.cols, X.dtype, "psk_gemm_q4: X")
-    y, ldy = _rows(Y, n, A.desc.rows, X.dtype, "psk_gemm_q4: Y")
-    _one_device("psk_gemm_q4", X, Y, A.codes, A.scales, A.zeros, ws)
+    n, dtype, type = X.shape[0], X.dtype, _type(X, "psk_gemm_q4")
+    x, ldx = _rows(X, n, A.cols, dtype, "psk_gemm_q4: X")
+    y, ldy = _rows(Y, n, A.rows, dtype, "psk_gemm_q4: Y")
+    _one_device("psk_gemm_q4", X, Y, A.codes, ws)
     if ws is None:
         ws = psk_gemm_q4_workspace(A, X, stream)
-    st = lib().psk_gemm_q4(ctypes.byref(A.desc), n, type, x, ldx, y, ldy, _ptr(ws), ws.numel(), _stream(stream))
+    st = lib().psk_gemm_q4(A._ref, n, type, x, ldx, y, ldy, _ptr(ws), ws.numel(), _stream(stream))
     if st:
         _check(st, "psk_gemm_q4")
     return Y
@@ -837,13 +840,13 @@ def psk_moe_experts_q4(X, crd, vals, W1: Q4, W3: Q4, W2: Q4, Y, act=PSK_ACT_SILU
     """The layer with weights in 4 bits."""
     n, dim = X.shape
     type, top_k = _type(X, "psk_moe_experts_q4"), crd.shape[1]
-    x, ldx = _rows(X, n, W1.desc.cols, X.dtype, "psk_moe_experts_q4: X")
-    y, ldy = _rows(Y, n, W2.desc.rows, X.dtype, "psk_moe_experts_q4: Y")
+    x, ldx = _rows(X, n, W1.cols, X.dtype, "psk_moe_experts_q4: X")
+    y, ldy = _rows(Y, n, W2.rows, X.dtype, "psk_moe_experts_q4: Y")
     c, v = _gating_ptrs(crd, vals, n, top_k, "psk_moe_experts_q4")
-    _one_device("psk_moe_experts_q4", X, crd, vals, Y, ws, *(t for w in (W1, W3, W2) for t in (w.codes, w.scales, w.zeros)))
+    _one_device("psk_moe_experts_q4", X, crd, vals, Y, W1.codes, W3.codes, W2.codes, ws)
     if ws is None:
         ws = psk_moe_workspace(n, dim, W1.desc.rows, W1.desc.count, top_k, X.device, stream)
-    st = lib().psk_moe_experts_q4(n, top_k, int(act), type, x, ldx, c, v, ctypes.byref(W1.desc), ctypes.byref(W3.desc), ctypes.byref(W2.desc), y,
+    st = lib().psk_moe_experts_q4(n, top_k, int(act), type, x, ldx, c, v, W1._ref, W3._ref, W2._ref, y,
                                   ldy, _ptr(ws), ws.numel(), _stream(stream))
     if st:
         _check(st, "psk_moe_experts_q4")
