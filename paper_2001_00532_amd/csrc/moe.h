@@ -141,8 +141,8 @@ struct Call {
 };
 
 // ---- up to four tokens
-// Four tokens by tiles instead: 6 of 64 experts of 3 x 1024 x 2048 in 16 bits 55.3 us, here 53.7; 4 of 32 of 3 x 2048 x 4096 in 4 bits 72, here 60.  One token
-// by tiles would be two launches more.
+// Four tokens by tiles instead: 6 of 64 experts of 3 x 1024 x 2048 in 16 bits 55.3 us, here 53.7; 4 of 32 of 3 x 2048 x 4096 in 4 bits 72, here 60.  Tiles
+// also take a launch more.
 // Registers for two waves of the first step (16-bit weights of two matrices two chunks deep; for three they spill: 17.0 us, 11.3).
 constexpr int FEW = 4;
 template <class SPAN, int HT, class W>
