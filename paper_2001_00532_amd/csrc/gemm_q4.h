@@ -8,7 +8,7 @@
 //
 // Three ways, by the rules in by_group, more_vectors and few_vectors_by_columns:
 //   up to four vectors            k_gemv_q4        32768 x 8192, one vector of bf16, groups of 64: 29.7 us = 4.8 TB/s of codes and scales
-//   more, up to 4096 columns      k_gemm_q4_kept   10240 x 4096, 16 vectors of bf16: 10.2 us; 8192 x 4096, 64 vectors of f16: 16.5 us
+//   more, up to 4096 (f32: 2048) columns  k_gemm_q4_kept   10240 x 4096, 16 vectors of bf16: 10.2 us; 8192 x 4096, 64 vectors of f16: 16.5 us
 //   more, longer rows             k_gemm_q4        4096 x 8192, 16 vectors of bf16: 9.6 us; 64 vectors of f16: 17.4 us
 #pragma once
 #include "psk_internal.h"
@@ -95,7 +95,8 @@ __global__ __launch_bounds__(64 * KW) void k_gemm_q4(WeightsQ4 A, int n, const v
 // of rows requested ahead instead of one take as long (10.3, 11.1 and 11.5 us for 10240 x 4096 times 16).
 // 10240 x 4096 times 16 vectors 10.2 us, by k_gemm_q4 with its copy 13.3; 8192 x 4096 times 64 16.5, by k_gemm_q4 23.
 // Beyond 4096 columns it would take more than the 16 waves of a workgroup.
-// Vectors of 32 bits hold three parts and 16 waves of them do not fit into the registers (200 bytes per lane go to scratch).
+// Vectors of 32 bits hold three parts, of which 16 waves do not fit into the registers, so they are kept up to 2048 columns only: 10240 x 4096 times 16
+// 19.9 us by k_gemm_q4, 23.2 kept; 8192 x 4096 times 64 42.7 and 59.6; 8192 x 2048 times 64 24.9 and 19.6, times 16 (10240 rows) 10.2 and 11.6.
 template <int XT, int S, int GB, int KW>
 __global__ __launch_bounds__(64 * KW) void k_gemm_q4_kept(WeightsQ4 A, int n, const void *X, int64_t ldx, const v4u *copy, void *Y, int64_t ldy)
 {
@@ -155,7 +156,7 @@ void more_vectors(const WeightsQ4 &A, int n, const void *X, int64_t ldx, void *Y
 {
     const int rows = (A.rows + 15) / 16, tiles = (n + 15) / 16;
     v4u *copy = static_cast<v4u *>(space);
-    const bool kept = kept_fits(A);
+    const bool kept = kept_fits(A) && (XT != F32 || A.cols <= 2048);
     // Longer rows: one tile and set of rows per workgroup where there is one tile (10240 x 4096 times 16 13.3 us, two sets of rows 13.7 to 15.7) or there
     // would be few workgroups (2048 x 8192 times 32 9.0 us, two and two 15.9; 2048 x 8192 times 64, 512 workgroups, in f32 27, two sets of rows 20).
     // (kept vectors are in natural order, as for groups of 32 columns)
@@ -163,8 +164,8 @@ void more_vectors(const WeightsQ4 &A, int n, const void *X, int64_t ldx, void *Y
     else if (XT == F32) PSK_LAUNCH((k_gemm_q4_copy<XT, 1>), dim3(copied_blocks(A.cols) / 4, tiles), dim3(256), 0, s, n, A.cols, X, ldx, copy);
     if (kept) {
         if (A.cols <= 1024) kept_vectors<XT, S, GB, 4>(A, n, X, ldx, Y, ldy, copy, s);
-        else if (A.cols <= 2048) kept_vectors<XT, S, GB, 8>(A, n, X, ldx, Y, ldy, copy, s);
-        else kept_vectors<XT, S, GB, 16>(A, n, X, ldx, Y, ldy, copy, s);
+        else if (XT == F32 || A.cols <= 2048) kept_vectors<XT, S, GB, 8>(A, n, X, ldx, Y, ldy, copy, s);
+        else if constexpr (XT != F32) kept_vectors<XT, S, GB, 16>(A, n, X, ldx, Y, ldy, copy, s);
     } else if (tiles == 1 || (int64_t)rows * tiles <= 256) PSK_LAUNCH((k_gemm_q4<XT, S, GB, true, 1, 1, 4>), dim3(rows, tiles), dim3(256), 0, s, A, n, copy, Y, ldy);
     else if constexpr (XT == F32) PSK_LAUNCH((k_gemm_q4<XT, S, GB, true, 2, 1, 4>), dim3((rows + 1) / 2, tiles), dim3(256), 0, s, A, n, copy, Y, ldy);
     else PSK_LAUNCH((k_gemm_q4<XT, S, GB, true, 2, 2, 4>), dim3((rows + 1) / 2, (tiles + 1) / 2), dim3(256), 0, s, A, n, copy, Y, ldy);
