@@ -70,8 +70,12 @@ int psk_gemm_q4(const psk_q4 *A, int64_t n, int type, const void *X, int64_t ldx
     if (n == 0 || A->rows == 0) return PSK_OK;
     if (!Y || (A->cols > 0 && !X)) return PSK_ERR_NULL;
     if (misaligned(X, bytes_of(type)) || misaligned(Y, bytes_of(type))) return PSK_ERR_ALIGNMENT;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (A->cols == 0)                                      // the kernels load the scale of the last column; here there is none, nor need there be any codes
+        return hip_status(type == PSK_F32 ? launch_fill_zero_2d(static_cast<float *>(Y), n, (int32_t)A->rows, ldy, s)
+                                          : launch_fill_zero_2d(static_cast<uint16_t *>(Y), n, (int32_t)A->rows, ldy, s));
     const auto launch = type == PSK_F32 ? launch_gemm_q4_of<F32> : (type == PSK_F16 ? launch_gemm_q4_of<F16> : launch_gemm_q4_of<BF16>);
-    return hip_status(launch(weights(*A), A->scale_type, (int)n, X, ldx, Y, ldy, workspace, static_cast<hipStream_t>(stream)));
+    return hip_status(launch(weights(*A), A->scale_type, (int)n, X, ldx, Y, ldy, workspace, s));
 }
 
 size_t psk_moe_route_workspace_bytes(int64_t n, int64_t experts)

@@ -1,4 +1,6 @@
 """Products with 4-bit weights against the plain form in 64 bits."""
+import ctypes
+
 import numpy as np
 import pytest
 
@@ -153,6 +155,26 @@ def test_empty_products():
     y = torch.full((3, 8), 5.0, device="cuda", dtype=torch.float16)
     psk.psk_gemm_q4(psk.Q4(codes, scales[:, :0], cols=0, group=32), x[:, :0], y)
     assert bool((y == 0).all())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 4, 5, 17, 70000])
+def test_products_without_columns(dtype, n):
+    """No columns: rows of zeros for any number of vectors, nothing behind them, and no codes, scales or vectors needed for it."""
+    t, rows = TYPES[dtype], 37
+    d = psk.psk_q4()
+    d.count, d.rows, d.cols, d.group, d.scale_type = 1, rows, 0, 64, psk.PSK_F32
+    types = {"f32": psk.PSK_F32, "f16": psk.PSK_F16, "bf16": psk.PSK_BF16}
+    y = torch.full((n + 1, rows + 3), 5.0, device="cuda", dtype=t)
+    ws = torch.empty(psk.psk_gemm_q4_workspace_bytes(rows, 0, n, types[dtype]), device="cuda", dtype=torch.uint8)
+    st = psk.lib().psk_gemm_q4(ctypes.byref(d), n, types[dtype], None, 0, y.data_ptr(), rows + 3, ws.data_ptr(), ws.numel(),
+                               torch.cuda.current_stream().cuda_stream)
+    assert st == 0
+    assert bool((y[:n, :rows] == 0).all()) and bool((y[:, rows:] == 5).all()) and bool((y[n] == 5).all())
+    codes, scales = torch.zeros(rows, 0, dtype=torch.uint8, device="cuda"), torch.zeros(rows, 0, device="cuda", dtype=t)
+    whole = torch.full((n, rows), 5.0, device="cuda", dtype=t)
+    psk.psk_gemm_q4(psk.Q4(codes, scales, cols=0, group=64), torch.zeros(n, 0, device="cuda", dtype=t), whole)
+    assert bool((whole == 0).all())
 
 
 @pytest.mark.parametrize("rows,cols,n", [((1 << 20) + 37, 8192 + 64, 3), ((1 << 20) + 37, 8192 + 64, 20), ((1 << 21) + (1 << 17) + 37, 4096, 5)])
