@@ -123,7 +123,8 @@ __device__ __forceinline__ Found find_few(FindSpace<MOST> &f, int positions, int
 __device__ __forceinline__ float activate(int act, float v)
 {
     if (act == PSK_ACT_SILU) return v / (1.0f + expf(-v));
-    return 0.5f * v * (1.0f + erff(v * 0.70710678118654752f));
+    // 1 + erf(x) = erfc(-x): the sum would cancel for negative v, 4% off at v = -5
+    return 0.5f * v * erfcf(v * -0.70710678118654752f);
 }
 
 struct Call {

@@ -309,6 +309,36 @@ def test_small_values_between_the_products(n):
     R.check(run16(x, crd, vals, w1, w1, w2), ref, bound, "small h")
 
 
+def selecting(rows, cols, column, value, dtype):
+    """One expert's matrix whose rows take `column` (of each row its own where a function) times `value`: 16 bits, and the same in 4."""
+    w = torch.zeros(1, rows, cols, dtype=dtype)
+    codes = torch.full((1, rows, (cols + 31) // 32 * 16), 0x88, dtype=torch.uint8)
+    for r in range(rows):
+        c = column(r) if callable(column) else column
+        w[0, r, c] = value
+        codes[0, r, c // 2] = 0x98 if c % 2 else 0x89       # 9 - 8 = 1 there
+    return w, psk.Q4(codes.cuda(), torch.full((1, rows, 1), value, dtype=dtype).cuda(), cols=cols, group=32)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n", [4, 23])
+def test_gelu_keeps_its_relative_error(dtype, n):
+    """Pre-activations from -5.5 to 5.5 without any error of their own (one product by 1), the value after them times 2^19 and 2^-6."""
+    t, dim = TYPES[dtype], 8
+    x = torch.zeros(n, dim, dtype=t)
+    x[:, 0], x[:, 1] = torch.linspace(-5.5, 5.5, n).to(t), 1024
+    (w1, q1), (w3, q3), (w2, q2) = selecting(dim, dim, 0, 1.0, t), selecting(dim, dim, 1, 512.0, t), selecting(dim, dim, lambda r: r, 2.0 ** -6, t)
+    crd, vals = torch.zeros(n, 1, dtype=torch.int32), torch.ones(n, 1)
+    ref, _ = R.layer(x, crd, vals, doubles(w1), doubles(w3), doubles(w2), 1, t, 0)
+    # of erfc(-v / sqrt 2): two roundings of its argument, times |d log erfc(z) / d log z| <= 2 z^2 + 1 = v^2 + 1; 16 steps for it and three products;
+    # two 16-bit parts of bf16: 2^-16; rounding of Y (gelu(0) = 0 is its smallest number away at most)
+    bound = ref.abs() * ((x[:, :1].double() ** 2 + 17) * R.STEP + 2.0 ** -16) + R.out_error(ref, t)
+    R.check(run16(x, crd, vals, w1, w3, w2, 1), ref, bound, "16 bits")
+    y = torch.empty(n, dim, dtype=t, device="cuda")
+    psk.psk_moe_experts_q4(x.cuda(), crd.cuda(), vals.cuda(), q1, q3, q2, y, act=psk.PSK_ACT_GELU)
+    R.check(y, ref, bound, "4 bits")
+
+
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
 @pytest.mark.parametrize("n,dim,inter", [(1, 1231, 311), (3, 77, 129), (9, 1231, 311), (50, 333, 45), (7, 9, 3)])
 def test_weights_at_any_element(dtype, n, dim, inter):
