@@ -43,7 +43,7 @@ __global__ __launch_bounds__(64 * KW) void k_gemv_q4(WeightsQ4 A, int n, const v
     __syncthreads();
     for (int o = threadIdx.x; o < 64 * R; o += 64 * KW) {
         const int r = o >> 6, v = o >> 4 & 3, i = o & 15;
-        if (v < n && row0 + 16 * r + i < A.rows) store_as<XT>(Y, v * ldy + row0 + 16 * r + i, get_sum<KW, R, 4>(lds, r, v, i));
+        if (v < n && row0 + 16 * r + i < A.rows) store_as<XT>(Y, v * ldy + row0 + 16 * r + i, get_sum<KW, R, 4>(lds, r, v, i) * SPAN::unit);
     }
 }
 
@@ -86,7 +86,7 @@ __global__ __launch_bounds__(64 * KW) void k_gemm_q4(WeightsQ4 A, int n, const v
     __syncthreads();
     for (int o = threadIdx.x; o < R * NT * 256; o += 64 * KW) {
         const int k = o >> 8, v = 16 * (t0 + k % NT) + (o >> 4 & 15), i = row0 + 16 * (k / NT) + (o & 15);
-        if (v < n && i < A.rows) store_as<XT>(Y, v * ldy + i, get_sum<KW, R * NT, 16>(lds, k, o >> 4 & 15, o & 15));
+        if (v < n && i < A.rows) store_as<XT>(Y, v * ldy + i, get_sum<KW, R * NT, 16>(lds, k, o >> 4 & 15, o & 15) * SPAN::unit);
     }
 }
 
@@ -117,7 +117,7 @@ __global__ __launch_bounds__(64 * KW) void k_gemm_q4_kept(WeightsQ4 A, int n, co
     k.run(blockIdx.x, gridDim.x, (A.rows + 15) / 16, [&](int set, const float *sums) {
         for (int o = threadIdx.x; o < 256; o += 64 * KW) {
             const int v = 16 * tile + (o >> 4), i = set * 16 + (o & 15);
-            if (v < n && i < A.rows) store_as<XT>(Y, v * ldy + i, get_sum<KW, 1, 16>(sums, 0, o >> 4, o & 15));
+            if (v < n && i < A.rows) store_as<XT>(Y, v * ldy + i, get_sum<KW, 1, 16>(sums, 0, o >> 4, o & 15) * K::unit);
         }
     });
 }

@@ -172,7 +172,7 @@ __global__ __launch_bounds__(THREADS, 2) void k_moe_up_few(Call a, W w1, W w3)
         __syncthreads();
         const int v = threadIdx.x >> 4, i = threadIdx.x & 15;
         if (v < 4 && v < count && row0 + i < a.inter) {
-            const float h = activate(a.act, get_sum<KW, 2, 4>(lds, 0, v, i)) * get_sum<KW, 2, 4>(lds, 1, v, i);
+            const float h = activate(a.act, get_sum<KW, 2, 4>(lds, 0, v, i) * SPAN::unit) * (get_sum<KW, 2, 4>(lds, 1, v, i) * SPAN::unit);
             unsigned short p, q;
             Halves<HT>::split(h, p, q);
             const int64_t at = list[v] * a.ldh + row0 + i;
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(THREADS, 3) void k_moe_down_few(Call a, W w2)
         put_few<1>(lds, wave, lane, y);
         __syncthreads();
         const int v = threadIdx.x >> 4, i = threadIdx.x & 15;
-        if (v < 4 && v < count && row0 + i < a.dim) a.P[(int64_t)list[v] * a.dim + row0 + i] = get_sum<KW, 1, 4>(lds, 0, v, i) * (1.0f / H::scale);
+        if (v < 4 && v < count && row0 + i < a.dim) a.P[(int64_t)list[v] * a.dim + row0 + i] = get_sum<KW, 1, 4>(lds, 0, v, i) * (SPAN::unit / H::scale);
         __syncthreads();
     }
 }
@@ -266,7 +266,7 @@ __device__ __forceinline__ void up_tiles(const Call &a, const W &w1, const W &w3
         const int t = o >> 8, v = o >> 4 & 15, i = o & 15;
         if (16 * (t0 + t) + v >= g.count) continue;
         float h = 0;
-        if (row0 + i < a.inter) h = activate(a.act, get_sum<KW, 2 * NT, 16>(lds, t, v, i)) * get_sum<KW, 2 * NT, 16>(lds, NT + t, v, i);
+        if (row0 + i < a.inter) h = activate(a.act, get_sum<KW, 2 * NT, 16>(lds, t, v, i) * SPAN::unit) * (get_sum<KW, 2 * NT, 16>(lds, NT + t, v, i) * SPAN::unit);
         unsigned short p, q;
         Halves<HT>::split(h, p, q);
         const int64_t at = copied_at<SPREAD>(g.tile + t0 + t, copied_blocks(a.inter), row0 + i, v);
@@ -315,7 +315,7 @@ __device__ __forceinline__ void down_tiles(const Call &a, const W &w2, const Fou
     __syncthreads();
     for (int o = threadIdx.x; o < R * NT * 256; o += THREADS) {
         const int k = o >> 8, v = 16 * (t0 + k % NT) + (o >> 4 & 15), i = row0 + 16 * (k / NT) + (o & 15);
-        if (v < g.count && i < a.dim) a.P[(int64_t)a.list[g.first + v] * a.dim + i] = get_sum<KW, R * NT, 16>(lds, k, o >> 4 & 15, o & 15) * (1.0f / H::scale);
+        if (v < g.count && i < a.dim) a.P[(int64_t)a.list[g.first + v] * a.dim + i] = get_sum<KW, R * NT, 16>(lds, k, o >> 4 & 15, o & 15) * (SPAN::unit / H::scale);
     }
     __syncthreads();
 }

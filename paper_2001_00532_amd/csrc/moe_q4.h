@@ -35,7 +35,7 @@ __global__ __launch_bounds__(64 * KW, 4) void k_moe_q4_up(Call a, WeightsQ4 w1, 
                 for (int o = threadIdx.x; o < 256; o += 64 * KW) {
                     const int v = o >> 4, i = o & 15;
                     if (16 * t + v >= g.count) continue;
-                    const float h = activate(a.act, get_sum<KW, 2, 16>(sums, 0, v, i)) * get_sum<KW, 2, 16>(sums, 1, v, i);
+                    const float h = activate(a.act, get_sum<KW, 2, 16>(sums, 0, v, i) * K::unit) * (get_sum<KW, 2, 16>(sums, 1, v, i) * K::unit);
                     store(set, v, i, 16 * set + i < a.inter ? h : 0.0f);
                 }
             });
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(64 * KW) void k_moe_q4_down(Call a, WeightsQ4 w2)
         k.run(blockIdx.x, gridDim.x, (a.dim + 15) / 16, [&](int set, const float *sums) {
             for (int o = threadIdx.x; o < 256; o += 64 * KW) {
                 const int v = 16 * t + (o >> 4), i = 16 * set + (o & 15);
-                if (v < g.count && i < a.dim) a.P[(int64_t)a.list[g.first + v] * a.dim + i] = get_sum<KW, 1, 16>(sums, 0, o >> 4, o & 15);
+                if (v < g.count && i < a.dim) a.P[(int64_t)a.list[g.first + v] * a.dim + i] = get_sum<KW, 1, 16>(sums, 0, o >> 4, o & 15) * K::unit;
             }
         });
     }

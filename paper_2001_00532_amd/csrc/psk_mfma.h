@@ -252,6 +252,7 @@ template <int T_, int R_, int B_>
 struct Span16 {
     static constexpr int T = T_, R = R_, B = B_, CH = 32 * B, PIECES = 1;
     static constexpr bool SPREAD = false, CODES = false;
+    static constexpr float unit = 1;
     const unsigned short *p[R][2];
     int left;                                              // columns from the lane's first one on
     struct Regs { v4u w[R][B / 2][2]; };
@@ -347,7 +348,9 @@ __device__ __forceinline__ v4u transpose_quarters(v4u w)
 // f16: a code in the low bits of 1024.0 or, from four bits up, of 64.0 adds its value; the subtraction leaves code - zero.
 // Columns come in the order 0 4 1 5 2 6 3 7.
 // bf16: a byte that holds a code is that code times 2^-9 in e4m3, so a conversion takes two of them to 32 bits; what is left
-// after the subtraction has 8 bits at most and is cut to bf16.  The factor 2^9 is in the scale.  Columns in order.
+// after the subtraction has 8 bits at most and is cut to bf16.  The finished sum is multiplied by 2^9 (unit): in the scale 2^9 would make
+// one of 2^119 infinite, in the codes a sum of a group of activations of 2^125.  Columns in order.
+template <int T> constexpr float code_unit = T == BF16 ? 0x1p9f : 1.0f;
 template <int T> struct Zero;
 template <> struct Zero<F16> {
     v2h lo, hi;
@@ -406,6 +409,7 @@ template <typename E, int N> struct Run { typedef E type __attribute__((ext_vect
 template <int T_, int R_, int P, int GB, int S, bool Z>
 struct SpanQ4 {
     static constexpr bool SPREAD = GB >= 4, CODES = true;
+    static constexpr float unit = code_unit<T_>;           // what the sums are to be multiplied by
     static constexpr int T = T_, R = R_, B = 4 * P, CH = 32 * B, PIECES = P, NG = 4 * P > GB ? 4 * P / GB : 1, PER = GB < 4 ? GB : 4;     // PER: blocks of a piece that share one
     typedef typename std::conditional<S == F32, float, unsigned short>::type Scale;
     typedef typename Run<Scale, NG>::type Scales;
@@ -479,10 +483,8 @@ struct SpanQ4 {
     static __device__ __forceinline__ v4u words(v4u w) { return SPREAD ? w : transpose_quarters(w); }
     static __device__ __forceinline__ float factor(Scale v)
     {
-        float f;
-        if constexpr (S == F32) f = v;
-        else f = widen<S>(v);
-        return T == BF16 ? f * 0x1p9f : f;
+        if constexpr (S == F32) return v;
+        else return widen<S>(v);
     }
     static __device__ __forceinline__ void clear(Few &f)
     {
@@ -739,6 +741,7 @@ struct KeptQ4 {
     typedef KeptSpace<KW, R, GB, S> Space;
     typedef typename Space::Scale Scale;
     static constexpr int THREADS = 64 * KW, NG = GB < 8 ? 8 / GB : 1, PER = GB < 4 ? GB : 4;
+    static constexpr float unit = code_unit<T>;
     static constexpr int E = GB == 1 ? 2 : 1;              // scales of 16 rows that a thread brings: 2 / GB for each of them
     Space &sp;
     const WeightsQ4 (&w)[R];
@@ -805,10 +808,8 @@ struct KeptQ4 {
     }
     static __device__ __forceinline__ float factor(Scale v)
     {
-        float f;
-        if constexpr (S == F32) f = v;
-        else f = widen<S>(v);
-        return T == BF16 ? f * 0x1p9f : f;
+        if constexpr (S == F32) return v;
+        else return widen<S>(v);
     }
     template <int B>
     __device__ __forceinline__ void multiply()

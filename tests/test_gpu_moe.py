@@ -309,15 +309,16 @@ def test_small_values_between_the_products(n):
     R.check(run16(x, crd, vals, w1, w1, w2), ref, bound, "small h")
 
 
-def selecting(rows, cols, column, value, dtype):
-    """One expert's matrix whose rows take `column` (of each row its own where a function) times `value`: 16 bits, and the same in 4."""
+def selecting(rows, cols, column, value, dtype, stype=None):
+    """One expert's matrix whose rows take `column` (of each row its own where a function) times `value`: 16 bits, and the same in 4
+    (scales of type `stype`)."""
     w = torch.zeros(1, rows, cols, dtype=dtype)
     codes = torch.full((1, rows, (cols + 31) // 32 * 16), 0x88, dtype=torch.uint8)
     for r in range(rows):
         c = column(r) if callable(column) else column
         w[0, r, c] = value
         codes[0, r, c // 2] = 0x98 if c % 2 else 0x89       # 9 - 8 = 1 there
-    return w, psk.Q4(codes.cuda(), torch.full((1, rows, 1), value, dtype=dtype).cuda(), cols=cols, group=32)
+    return w, psk.Q4(codes.cuda(), torch.full((1, rows, 1), value, dtype=stype or dtype).cuda(), cols=cols, group=32)
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
@@ -337,6 +338,23 @@ def test_gelu_keeps_its_relative_error(dtype, n):
     y = torch.empty(n, dim, dtype=t, device="cuda")
     psk.psk_moe_experts_q4(x.cuda(), crd.cuda(), vals.cuda(), q1, q3, q2, y, act=psk.PSK_ACT_GELU)
     R.check(y, ref, bound, "4 bits")
+
+
+@pytest.mark.parametrize("dtype,scale32", [("bf16", False), ("bf16", True), ("f16", True)])
+@pytest.mark.parametrize("n", [3, 23])
+def test_scales_of_the_layer_near_the_largest_number(dtype, scale32, n):
+    """2^-80 in W3, 2^120 in W2 and gates of 2^-40: ordinary numbers before and after."""
+    t, dim = TYPES[dtype], 8
+    st = torch.float32 if scale32 else t
+    x = torch.zeros(n, dim, dtype=t)
+    x[:, 0], x[:, 1] = torch.linspace(-3, 3, n).to(t), 1
+    q = [selecting(dim, dim, c, v, torch.float32, st)[1] for c, v in ((0, 1.0), (1, 2.0 ** -80), (lambda r: r, 2.0 ** 120))]
+    crd, vals = torch.zeros(n, 1, dtype=torch.int32), torch.full((n, 1), 2.0 ** -40)
+    ref = R.act(x[:, :1].double(), 0).expand(n, dim)
+    y = torch.empty(n, dim, dtype=t, device="cuda")
+    psk.psk_moe_experts_q4(x.cuda(), crd.cuda(), vals.cuda(), *q, y)
+    # every sum has one term: 16 steps for the activation and the products, two 16-bit parts between them, rounding of Y
+    R.check(y, ref, ref.abs() * (16 * R.STEP + 2.0 ** -16) + R.out_error(ref, t), "large scales")
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])

@@ -120,6 +120,21 @@ def test_special_values(dtype):
     assert not bool(torch.isfinite(got[:6, 5]).any())
 
 
+@pytest.mark.parametrize("dtype,scale32", [("bf16", False), ("bf16", True), ("f32", True)])
+@pytest.mark.parametrize("n,cols,group", [(1, 300, 32), (3, 2200, 256), (6, 300, 64), (20, 1500, 128), (5, 2600, 32), (20, 5000, 64)])
+def test_scales_near_the_largest_number(dtype, scale32, n, cols, group):
+    """Scales of 2^118 to 2^127 with activations of about 2^-100; a group of every row has weights that are all zero."""
+    t, rows = TYPES[dtype], 35
+    rng = np.random.default_rng(cols)
+    codes, scales, _ = R.q4_weights(rng, rows, cols, group, False, torch.float32 if scale32 else t)
+    scales[:] = 2.0 ** torch.from_numpy(rng.integers(118, 126, scales.shape)).double()
+    scales[:, 1] = torch.finfo(scales.dtype).max
+    codes[:, group // 2:group] = 0x88
+    x = (torch.from_numpy(rng.standard_normal((n, cols))) * 2.0 ** -100).to(t)
+    ref, bound = R.gemm(R.dequantised(codes, scales, None, cols, group), x, t)
+    R.check(product((codes, scales, None), x.cuda(), cols, group), ref, bound, "large scales")
+
+
 @pytest.mark.parametrize("n", [1, 6, 20])
 @pytest.mark.parametrize("cols", [300, 5000])
 def test_activations_below_the_smallest_normal_f16(n, cols):
