@@ -581,7 +581,7 @@ int psk_moe_route(int64_t n, int64_t dim, int64_t experts, int32_t top_k, int sc
  * psk_moe_experts: weights of `type`, matrix e of W1 and W3 at stride1*e elements, rows ld1 apart (W2: stride2, ld2).  No alignment beyond the
  * element's is asked of them; rows that begin at multiples of 16 bytes are read fastest.
  * psk_moe_experts_q4: weights in 4 bits, count = experts in all three, W1 and W3 alike in rows, cols and group, all with one scale_type.
- * With PSK_F16 and 16-bit weights, values between the two products of 2^24 and more become infinite.
+ * Values between the two products keep 32 bits.  W2 is finite: what an infinite weight of it is multiplied into becomes infinite or NaN.
  * The workspace is for both.
  */
 enum { PSK_ACT_SILU = 0, PSK_ACT_GELU = 1 };   /* v / (1 + exp(-v));  v (1 + erf(v / sqrt 2)) / 2 */

@@ -17,8 +17,8 @@
 // tokens, 4 of 32 experts of 3 x 1280 x 4096 in f16 5.1 + 105 + 61 + 4.7 (137); one token, 4 of 32 experts of 3 x 2048 x 4096 in 4 bits
 // 13.4 + 7.6 + 3.3 (7.4).
 //
-// h goes to memory as two 16-bit numbers (Halves): rounding to one of them would cost as much accuracy as rounding Y does, and the
-// second one costs a matrix instruction where the matrix cores wait for memory.
+// h keeps its 32 bits: it goes to memory as three parts of bf16 (Thirds), and f16 weights are cut into two parts for them.  The matrix instructions
+// that this takes have room where memory is waited for.  (4-bit weights and kept vectors: as it is, moe_q4.h.)
 #pragma once
 #include "psk_internal.h"
 #include "psk_mfma.h"
@@ -132,9 +132,9 @@ struct Call {
     const int *crd;
     const unsigned short *X;
     int64_t ldx;
-    // h: row p with both parts apart by `rest` (few), or the order of the operands (tiles)
+    // h: row p with its parts apart by `apart` (few), or the order of the operands (tiles)
     unsigned short *h;
-    int64_t ldh, rest;
+    int64_t ldh, apart;
     float *P;
     Found *found;                                            // tiles: per slot
     int *list;                                               // tiles: positions, expert after expert
@@ -146,7 +146,7 @@ struct Call {
 // also take a launch more.
 // Registers for two waves of the first step (16-bit weights of two matrices two chunks deep; for three they spill: 17.0 us, 11.3).
 constexpr int FEW = 4;
-template <class SPAN, int HT, class W>
+template <class SPAN, class W>
 __global__ __launch_bounds__(THREADS, 2) void k_moe_up_few(Call a, W w1, W w3)
 {
     __shared__ FindSpace<FEW * PSK_MOE_MAX_TOP_K> f;
@@ -173,41 +173,65 @@ __global__ __launch_bounds__(THREADS, 2) void k_moe_up_few(Call a, W w1, W w3)
         const int v = threadIdx.x >> 4, i = threadIdx.x & 15;
         if (v < 4 && v < count && row0 + i < a.inter) {
             const float h = activate(a.act, get_sum<KW, 2, 4>(lds, 0, v, i) * SPAN::unit) * (get_sum<KW, 2, 4>(lds, 1, v, i) * SPAN::unit);
-            unsigned short p, q;
-            Halves<HT>::split(h, p, q);
-            const int64_t at = list[v] * a.ldh + row0 + i;
-            a.h[at] = p;
-            a.h[at + a.rest] = q;
+            Thirds::store(a.h, list[v] * a.ldh + row0 + i, a.apart, h);
         }
         __syncthreads();
     }
 }
+// One position: its three parts take the places of three vectors.
 template <class SPAN, class W>
-__global__ __launch_bounds__(THREADS, 3) void k_moe_down_few(Call a, W w2)
+__device__ __forceinline__ void down_one(const Call &a, const W &w2, int expert, int p, int row0, float *lds, v4u *places)
+{
+    int lane = threadIdx.x & 63, cols = a.inter;
+    asm volatile("" : "+v"(lane), "+s"(cols));
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    SPAN span;
+    span.set(0, w2, expert, row0, a.dim, lane, cols);
+    Plain16<BF16> x;
+    x.set(a.h, p * a.ldh + min(lane >> 2 & 3, Thirds::P - 1) * a.apart + few_column<SPAN>(lane));
+    float y[1];
+    few_product(span, x, cols, wave, KW, lane, Exchange(places + EXCHANGE * wave, lane), y);
+    put_few<1>(lds, wave, lane, y);
+    __syncthreads();
+    const int i = threadIdx.x;
+    if (i < 16 && row0 + i < a.dim)
+        a.P[(int64_t)p * a.dim + row0 + i] = ((get_sum<KW, 1, 4>(lds, 0, 2, i) + get_sum<KW, 1, 4>(lds, 0, 1, i)) + get_sum<KW, 1, 4>(lds, 0, 0, i)) * SPAN::unit;
+    __syncthreads();
+}
+// SINGLE: one position after the other, for one token, of which no expert has two (but where one occurs twice in its row).  Otherwise up to four
+// share the weights, in a kernel with one wave less on a SIMD (one token, 4 of 32 experts of 3 x 2048 x 4096 in 4 bits: 8.5 us, SINGLE 7.4).
+template <class SPAN, bool SINGLE, class W>
+__global__ __launch_bounds__(THREADS, SINGLE ? 4 : 3) void k_moe_down_few(Call a, W w2)
 {
     __shared__ FindSpace<FEW * PSK_MOE_MAX_TOP_K> f;
     __shared__ float lds[KW * 64];
     __shared__ v4u places[KW * EXCHANGE];
-    typedef Halves<SPAN::T> H;
     const Found g = find_few(f, a.n * a.top_k, a.experts, a.crd, blockIdx.y);
     if (g.expert < 0) return;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), row0 = blockIdx.x * 16;
-    for (int p0 = 0; p0 < g.count; p0 += 4) {
-        const unsigned short *list = f.list + p0;
-        const int count = g.count - p0;
-        int lane = threadIdx.x & 63, cols = a.inter;
-        asm volatile("" : "+v"(lane), "+s"(cols));
-        SPAN span;
-        span.set(0, w2, g.expert, row0, a.dim, lane, cols);
-        H x;
-        x.set(a.h, list[min(lane >> 2 & 3, count - 1)] * a.ldh + few_column<SPAN>(lane), a.rest);
-        float y[1];
-        few_product(span, x, cols, wave, KW, lane, Exchange(places + EXCHANGE * wave, lane), y);
-        put_few<1>(lds, wave, lane, y);
-        __syncthreads();
-        const int v = threadIdx.x >> 4, i = threadIdx.x & 15;
-        if (v < 4 && v < count && row0 + i < a.dim) a.P[(int64_t)list[v] * a.dim + row0 + i] = get_sum<KW, 1, 4>(lds, 0, v, i) * (SPAN::unit / H::scale);
-        __syncthreads();
+    const int row0 = blockIdx.x * 16;
+    if (SINGLE || g.count == 1) {
+        for (int k = 0; k < g.count; ++k) down_one<SPAN>(a, w2, g.expert, f.list[k], row0, lds, places);
+        return;
+    }
+    if constexpr (!SINGLE) {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        for (int p0 = 0; p0 < g.count; p0 += 4) {
+            const unsigned short *list = f.list + p0;
+            const int count = g.count - p0;
+            int lane = threadIdx.x & 63, cols = a.inter;
+            asm volatile("" : "+v"(lane), "+s"(cols));
+            SPAN span;
+            span.set(0, w2, g.expert, row0, a.dim, lane, cols);
+            Thirds x;
+            x.set(a.h, list[min(lane >> 2 & 3, count - 1)] * a.ldh + few_column<SPAN>(lane), a.apart);
+            float y[1];
+            few_product(span, x, cols, wave, KW, lane, Exchange(places + EXCHANGE * wave, lane), y);
+            put_few<1>(lds, wave, lane, y);
+            __syncthreads();
+            const int v = threadIdx.x >> 4, i = threadIdx.x & 15;
+            if (v < 4 && v < count && row0 + i < a.dim) a.P[(int64_t)list[v] * a.dim + row0 + i] = get_sum<KW, 1, 4>(lds, 0, v, i) * SPAN::unit;
+            __syncthreads();
+        }
     }
 }
 
@@ -233,16 +257,17 @@ __global__ __launch_bounds__(THREADS) void k_moe_sort(Call a)
     }
 }
 
-// Where the two parts of column i of h stand in the copy of a tile, for vector m.
+// Where the first part of column i of h stands in the copy of a tile, for vector m; the others follow COPIED_APART elements on.
+constexpr int COPIED_APART = 64 * 8;
 template <bool SPREAD>
 __device__ __forceinline__ int64_t copied_at(int tile, int blocks, int i, int m)
 {
     const int block = SPREAD ? 4 * (i >> 7) + (i >> 3 & 3) : i >> 5, quarter = SPREAD ? i >> 5 & 3 : i >> 3 & 3;
-    return (((int64_t)tile * blocks + block) * 2 * 64 + 16 * quarter + m) * 8 + (i & 7);
+    return (((int64_t)tile * blocks + block) * Thirds::P * 64 + 16 * quarter + m) * 8 + (i & 7);
 }
 
 // NT tiles of 16 positions (two at once where there are two: 4 experts with 24 positions each 24.8 us, one after the other 36.9), 16 rows of W1 and of W3; rows past the last one write the zeros that pad the columns of the next step.
-template <class SPAN, int HT, bool SPREAD, int NT, class W>
+template <class SPAN, bool SPREAD, int NT, class W>
 __device__ __forceinline__ void up_tiles(const Call &a, const W &w1, const W &w3, const Found &g, int t0, int row0, float *lds, v4u *places)
 {
     int lane = threadIdx.x & 63, cols = a.dim;
@@ -267,15 +292,11 @@ __device__ __forceinline__ void up_tiles(const Call &a, const W &w1, const W &w3
         if (16 * (t0 + t) + v >= g.count) continue;
         float h = 0;
         if (row0 + i < a.inter) h = activate(a.act, get_sum<KW, 2 * NT, 16>(lds, t, v, i) * SPAN::unit) * (get_sum<KW, 2 * NT, 16>(lds, NT + t, v, i) * SPAN::unit);
-        unsigned short p, q;
-        Halves<HT>::split(h, p, q);
-        const int64_t at = copied_at<SPREAD>(g.tile + t0 + t, copied_blocks(a.inter), row0 + i, v);
-        a.h[at] = p;
-        a.h[at + 64 * 8] = q;
+        Thirds::store(a.h, copied_at<SPREAD>(g.tile + t0 + t, copied_blocks(a.inter), row0 + i, v), COPIED_APART, h);
     }
     __syncthreads();
 }
-template <class SPAN, int HT, bool SPREAD, int MOST, class W>
+template <class SPAN, bool SPREAD, int MOST, class W>
 __global__ __launch_bounds__(THREADS, 3) void k_moe_up(Call a, W w1, W w3)
 {
     __shared__ float lds[KW * MOST * 512];
@@ -285,16 +306,17 @@ __global__ __launch_bounds__(THREADS, 3) void k_moe_up(Call a, W w1, W w3)
     const int tiles = (g.count + 15) / 16;
     int t = 0;
     if constexpr (MOST > 1)
-        for (; t + 1 < tiles; t += MOST) up_tiles<SPAN, HT, SPREAD, MOST>(a, w1, w3, g, t, blockIdx.x * 16, lds, places);
-    for (; t < tiles; ++t) up_tiles<SPAN, HT, SPREAD, 1>(a, w1, w3, g, t, blockIdx.x * 16, lds, places);
+        for (; t + 1 < tiles; t += MOST) up_tiles<SPAN, SPREAD, MOST>(a, w1, w3, g, t, blockIdx.x * 16, lds, places);
+    for (; t < tiles; ++t) up_tiles<SPAN, SPREAD, 1>(a, w1, w3, g, t, blockIdx.x * 16, lds, places);
 }
 
-// 16 R rows of W2.  h in both parts is twice what 16 rows of 16-bit weights are, so two sets of rows share it (24 tokens, 32 experts 61 us, with one set 78);
-// 4-bit weights take one.
+// 16 R rows of W2.  h in its parts is three times what 16 rows of 16-bit weights are, so two sets of rows share it (the layer for 24 tokens, 4 of 32 experts
+// 179 us, with one set 199); 4-bit weights take one.
+// Registers for two waves: with three, two tiles spill (64 tokens, 4 of 16 experts of 3 x 1024 x 2048: 61 us, with three 71; 4 bits, 48 tokens, 4 of 16
+// experts of 3 x 5000 x 1024 79 and 136), though one tile is 5 us faster then (24 tokens 174).
 template <class SPAN, int NT, class W>
 __device__ __forceinline__ void down_tiles(const Call &a, const W &w2, const Found &g, int t0, int row0, float *lds, v4u *places)
 {
-    typedef Halves<SPAN::T> H;
     constexpr int R = SPAN::R;
     int lane = threadIdx.x & 63, cols = a.inter;
     asm volatile("" : "+v"(lane), "+s"(cols), "+s"(row0));
@@ -302,9 +324,14 @@ __device__ __forceinline__ void down_tiles(const Call &a, const W &w2, const Fou
     SPAN span;
 #pragma unroll
     for (int r = 0; r < R; ++r) span.set(r, w2, g.expert, row0 + 16 * r, a.dim, lane, cols);
-    Copied<H> x[NT];
+    Copied<Thirds> x[NT];
 #pragma unroll
-    for (int t = 0; t < NT; ++t) x[t].set(a.h, g.tile + min(t0 + t, last), blocks, lane);
+    for (int t = 0; t < NT; ++t) {
+        // vectors past the last one repeat it, so half the lines of a block are not asked for where there are up to eight (the layer for 24
+        // tokens, 4 of 32 experts: 197 us without this)
+        const int tile = min(t0 + t, last);
+        x[t].set(a.h, g.tile + tile, blocks, (lane & 48) + min(lane & 15, g.count - 1 - 16 * tile));
+    }
     v4f acc[R][NT], flat[R * NT];
     tile_product<SPAN, NT>(span, x, cols, wave, KW, Exchange(places + EXCHANGE * wave, lane), acc);
 #pragma unroll
@@ -315,12 +342,12 @@ __device__ __forceinline__ void down_tiles(const Call &a, const W &w2, const Fou
     __syncthreads();
     for (int o = threadIdx.x; o < R * NT * 256; o += THREADS) {
         const int k = o >> 8, v = 16 * (t0 + k % NT) + (o >> 4 & 15), i = row0 + 16 * (k / NT) + (o & 15);
-        if (v < g.count && i < a.dim) a.P[(int64_t)a.list[g.first + v] * a.dim + i] = get_sum<KW, R * NT, 16>(lds, k, o >> 4 & 15, o & 15) * (SPAN::unit / H::scale);
+        if (v < g.count && i < a.dim) a.P[(int64_t)a.list[g.first + v] * a.dim + i] = get_sum<KW, R * NT, 16>(lds, k, o >> 4 & 15, o & 15) * SPAN::unit;
     }
     __syncthreads();
 }
 template <class SPAN, int MOST, class W>
-__global__ __launch_bounds__(THREADS, 3) void k_moe_down(Call a, W w2)
+__global__ __launch_bounds__(THREADS, 2) void k_moe_down(Call a, W w2)
 {
     __shared__ float lds[KW * SPAN::R * MOST * 256];
     __shared__ v4u places[KW * EXCHANGE];
@@ -359,11 +386,11 @@ size_t carve_moe(const MoeCall &c, Call *a)
     a->P = reinterpret_cast<float *>(take(positions * c.dim * 4));
     if (c.n <= FEW) {
         a->ldh = (c.inter + 7) / 8 * 8;
-        a->rest = (int64_t)(align256(positions * a->ldh * 2) / 2);
-        a->h = reinterpret_cast<unsigned short *>(take(4 * a->rest));
+        a->apart = (int64_t)(align256(positions * a->ldh * 2) / 2);
+        a->h = reinterpret_cast<unsigned short *>(take(2 * Thirds::P * a->apart));
     } else {
         const int64_t tiles = positions / 16 + slots;
-        a->h = reinterpret_cast<unsigned short *>(take(tiles * copied_blocks(c.inter) * 2048));
+        a->h = reinterpret_cast<unsigned short *>(take(tiles * copied_blocks(c.inter) * Thirds::P * 1024));
         a->copy = reinterpret_cast<v4u *>(take(tiles * copied_blocks(c.dim) * 1024));
         a->found = reinterpret_cast<Found *>(take(slots * sizeof(Found)));
         a->list = reinterpret_cast<int *>(take(positions * 4));
@@ -371,14 +398,13 @@ size_t carve_moe(const MoeCall &c, Call *a)
     return at;
 }
 
-// The spans of the two steps, for up to four tokens (FEW_*) and for tiles, MOST of them at once.  (The parts of h are in bf16, or weights in 16 bits: no
-// span of the second step takes columns in the order of f16 codes.)
+// The spans of the two steps, for up to four tokens (FEW_*) and for tiles, MOST of them at once.
 // KEPT: another way for more than four tokens, where it fits.
 struct NotKept { static constexpr bool USED = false; };
 template <class FEW_UP, class FEW_DOWN, class UP, class DOWN, int MOST, int YT, class KEPT, class W>
 hipError_t launch_layer(const MoeCall &c, const W &w1, const W &w3, const W &w2, hipStream_t s)
 {
-    static_assert(!(DOWN::CODES && DOWN::T == F16), "copied_at");
+    static_assert(FEW_DOWN::T == BF16 && DOWN::T == BF16, "the parts of h are in bf16, and copied_at knows no order of f16 codes");
     Call a = {0, c.experts, c.top_k, c.dim, c.inter, c.act, nullptr, nullptr, c.ldx, nullptr, 0, 0, nullptr, nullptr, nullptr, nullptr};
     carve_moe(c, &a);
     const int at_once = tokens_at_once(c.n, c.top_k);
@@ -388,8 +414,9 @@ hipError_t launch_layer(const MoeCall &c, const W &w1, const W &w3, const W &w2,
         a.X = static_cast<const unsigned short *>(c.X) + t0 * c.ldx;
         const int slots = a.n * c.top_k < c.experts ? a.n * c.top_k : c.experts, down = (c.dim + 15) / 16;
         if (c.n <= FEW) {
-            PSK_LAUNCH((k_moe_up_few<FEW_UP, FEW_DOWN::T, W>), dim3((c.inter + 15) / 16, slots), dim3(THREADS), 0, s, a, w1, w3);
-            PSK_LAUNCH((k_moe_down_few<FEW_DOWN, W>), dim3(down, slots), dim3(THREADS), 0, s, a, w2);
+            PSK_LAUNCH((k_moe_up_few<FEW_UP, W>), dim3((c.inter + 15) / 16, slots), dim3(THREADS), 0, s, a, w1, w3);
+            if (c.n == 1) PSK_LAUNCH((k_moe_down_few<FEW_DOWN, true, W>), dim3(down, slots), dim3(THREADS), 0, s, a, w2);
+            else PSK_LAUNCH((k_moe_down_few<FEW_DOWN, false, W>), dim3(down, slots), dim3(THREADS), 0, s, a, w2);
         } else {
             const dim3 sort((copied_blocks(c.dim) + KW * COPY_BLOCKS - 1) / (KW * COPY_BLOCKS), slots);
             bool kept = false;
@@ -403,7 +430,7 @@ hipError_t launch_layer(const MoeCall &c, const W &w1, const W &w3, const W &w2,
             }
             if (!kept) {
                 PSK_LAUNCH((k_moe_sort<UP>), sort, dim3(THREADS), 0, s, a);
-                PSK_LAUNCH((k_moe_up<UP, DOWN::T, DOWN::SPREAD, MOST, W>), dim3(copied_blocks(c.inter) * 2, slots), dim3(THREADS), 0, s, a, w1, w3);
+                PSK_LAUNCH((k_moe_up<UP, DOWN::SPREAD, MOST, W>), dim3(copied_blocks(c.inter) * 2, slots), dim3(THREADS), 0, s, a, w1, w3);
                 PSK_LAUNCH((k_moe_down<DOWN, MOST, W>), dim3((down + DOWN::R - 1) / DOWN::R, slots), dim3(THREADS), 0, s, a, w2);
             }
         }

@@ -7,7 +7,7 @@ namespace {
 template <int T>
 hipError_t launch_16(const MoeCall &c, const Weights16 &w1, const Weights16 &w3, const Weights16 &w2, hipStream_t s)
 {
-    return launch_layer<Span16<T, 2, 4>, Span16<T, 1, 4>, Span16<T, 2, 2>, Span16<T, 2, 2>, 2, T, NotKept>(c, w1, w3, w2, s);
+    return launch_layer<Span16<T, T, 2, 4>, Span16<T, BF16, 1, 4>, Span16<T, T, 2, 2>, Span16<T, BF16, 2, 2>, 2, T, NotKept>(c, w1, w3, w2, s);
 }
 
 }  // namespace

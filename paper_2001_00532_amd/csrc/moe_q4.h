@@ -1,5 +1,5 @@
-// The layer of a mixture of experts with 4-bit weights: which instance of the kernels in moe.h a call takes.  The second product takes bf16
-// whatever the type of the tokens is: codes are exact in it and h needs no scaling.
+// The layer of a mixture of experts with 4-bit weights: which instance of the kernels in moe.h a call takes.  The second product takes the parts
+// of h in bf16 whatever the type of the tokens is: codes are exact in it.
 #pragma once
 #include "moe.h"
 
@@ -9,6 +9,8 @@ namespace {
 // ---- more than four tokens, up to KEPT_COLUMNS columns in both products: the vectors kept (KeptQ4)
 // 48 tokens, 8 of 64 experts of 3 x 1000 x 2048 in f16: 36.9 us for the first step and 29.8 for the second; by k_moe_up and k_moe_down the whole
 // layer took 154 us, by the first form of these 90.  The matrices once would be 29 us: instructions that dequantise share the time with the loads.
+// Between the two, h goes to memory in 32 bits and becomes two parts of f16 where it is kept (Scaled): 64 registers, three parts of bf16 are 96 (the layer for 48
+// tokens, 4 of 16 experts of 3 x 2048 x 4096: 101 us, with these 111; of 32 of 3 x 3500 x 1000 72 and 114).
 template <int T, int GB, int S, int KW>
 __global__ __launch_bounds__(64 * KW, 4) void k_moe_q4_up(Call a, WeightsQ4 w1, WeightsQ4 w3)
 {
@@ -24,11 +26,8 @@ __global__ __launch_bounds__(64 * KW, 4) void k_moe_q4_up(Call a, WeightsQ4 w1, 
         x.set(a.copy, g.tile + t, copied_blocks(a.dim), k.lane);
         keep_copied(k, x);
         const auto store = [&](int set, int v, int i, float h) {
-            unsigned short p, q;
-            Halves<BF16>::split(h, p, q);
-            const int64_t at = copied_at<false>(g.tile + t, copied_blocks(a.inter), 16 * set + i, v);
-            a.h[at] = p;
-            a.h[at + 64 * 8] = q;
+            const int c = 16 * set + i;
+            reinterpret_cast<float *>(a.h)[((((int64_t)(g.tile + t) * copied_blocks(a.inter) + (c >> 5)) * 2 + (c >> 2 & 1)) * 64 + 16 * (c >> 3 & 3) + v) * 4 + (c & 3)] = h;
         };
         if ((int)blockIdx.x < real)
             k.run(blockIdx.x, gridDim.x, real, [&](int set, const float *sums) {
@@ -44,19 +43,19 @@ __global__ __launch_bounds__(64 * KW, 4) void k_moe_q4_up(Call a, WeightsQ4 w1, 
                 if (16 * t + (o >> 4) < g.count) store(set, o >> 4, o & 15, 0.0f);
     }
 }
+// Eight waves get registers for two workgroups on a compute unit, which takes a few spilled ones (3 x 2048 x 4096: 101 us, with one workgroup 110); with a
+// scale per 32 columns too many would be.
 template <int GB, int S, int KW>
-__global__ __launch_bounds__(64 * KW) void k_moe_q4_down(Call a, WeightsQ4 w2)
+__global__ __launch_bounds__(64 * KW, KW > 4 && GB > 1 ? 4 : 1) void k_moe_q4_down(Call a, WeightsQ4 w2)
 {
-    typedef KeptQ4<BF16, 1, GB, S, KW, Halves<BF16>> K;
+    typedef KeptQ4<F16, 1, GB, S, KW, Scaled> K;
     __shared__ typename K::Space space;
     const Found g = a.found[blockIdx.y];
     if (g.expert < 0) return;
     const WeightsQ4 w[1] = {w2};
     for (int t = 0; 16 * t < g.count; ++t) {
         K k(space, w, g.expert, a.dim, a.inter);
-        Copied<Halves<BF16>> x;
-        x.set(a.h, g.tile + t, copied_blocks(a.inter), k.lane);
-        keep_copied(k, x);
+        keep_scaled(k, reinterpret_cast<const v4f *>(a.h) + (int64_t)(g.tile + t) * copied_blocks(a.inter) * 128, min(g.count - 16 * t, 16));
         k.run(blockIdx.x, gridDim.x, (a.dim + 15) / 16, [&](int set, const float *sums) {
             for (int o = threadIdx.x; o < 256; o += 64 * KW) {
                 const int v = 16 * t + (o >> 4), i = 16 * set + (o & 15);

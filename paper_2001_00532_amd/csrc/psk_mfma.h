@@ -113,11 +113,10 @@ constexpr int EXCHANGE = 128;                              // v4u of a wave
 // brings four blocks.  The instruction that multiplies it by block j of the weights leaves the product of the two in element j
 // of the lanes of quarter v (and products of blocks that do not belong together in the other elements).
 // Tiles: row m of an operand is vector m of the tile; they come from a copy of the vectors in the order of the operands (Copied).
-// A vector may have several parts whose products add up; P of them, the last one with a factor of its own if LO (see Halves).
+// A vector may have several parts whose products add up; P of them.
 template <int T>
 struct Plain16 {                                           // 16 bits
     static constexpr int P = 1;
-    static constexpr bool LO = false;
     struct Raw { v4u v; };
     const unsigned short *p;
     __device__ __forceinline__ void set(const void *X, int64_t at) { p = static_cast<const unsigned short *>(X) + at; }
@@ -127,9 +126,18 @@ struct Plain16 {                                           // 16 bits
 };
 // 32 bits as three parts of bf16: v = a + b + c with 8 significant bits in each, cut off and not rounded, so the sum is exact and a
 // value near the largest does not become infinite.  Infinity and NaN stand in the first part alone.
+__device__ __forceinline__ void cut(float value, unsigned (&part)[3])      // the upper halves are the parts
+{
+    const float v = __builtin_canonicalizef(value);        // a NaN keeps its first bit
+    const float a = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, v) & 0xffff0000u), d = v - a;
+    const float rest = __builtin_isfinite(v) ? d : 0.0f;
+    const float b = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, rest) & 0xffff0000u), c = rest - b;
+    part[0] = __builtin_bit_cast(unsigned, a);
+    part[1] = __builtin_bit_cast(unsigned, b);
+    part[2] = __builtin_bit_cast(unsigned, c);
+}
 struct Parts32 {
     static constexpr int P = 3;
-    static constexpr bool LO = false;
     struct Raw { v4f_e a, b; };
     const float *p;
     __device__ __forceinline__ void set(const void *X, int64_t at) { p = static_cast<const float *>(X) + at; }
@@ -163,44 +171,54 @@ struct Parts32 {
         for (int i = 0; i < 4; ++i) {
             unsigned part[2][P];
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                const float v = __builtin_canonicalizef(i < 2 ? r.a[2 * i + e] : r.b[2 * i - 4 + e]);      // a NaN keeps its first bit
-                const float a = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, v) & 0xffff0000u), d = v - a;
-                const float rest = __builtin_isfinite(v) ? d : 0.0f;
-                const float b = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, rest) & 0xffff0000u), c = rest - b;
-                part[e][0] = __builtin_bit_cast(unsigned, a);
-                part[e][1] = __builtin_bit_cast(unsigned, b);
-                part[e][2] = __builtin_bit_cast(unsigned, c);
-            }
+            for (int e = 0; e < 2; ++e) cut(i < 2 ? r.a[2 * i + e] : r.b[2 * i - 4 + e], part[e]);
 #pragma unroll
             for (int q = 0; q < P; ++q) x[q][i] = __builtin_amdgcn_perm(part[1][q], part[0][q], 0x07060302u);
         }
     }
 };
-// Two 16-bit numbers per value, the nearest one and the nearest one to what is left, in two arrays.  f16 has too small a range for
-// that: the value is scaled by 2^-8 (up to 2^24 it is finite) and what is left by 2^11, and the second sum is kept apart.
-template <int T>
-struct Halves {
-    static constexpr int P = 2;
-    static constexpr bool LO = T == F16;
-    static constexpr float scale = T == F16 ? 0x1p-8f : 1.0f, rest = T == F16 ? 0x1p11f : 1.0f;
-    struct Raw { v4u v[2]; };
+// The same three parts, cut where the value is written and read many times: each in an array of its own.
+struct Thirds {
+    static constexpr int P = 3;
+    struct Raw { v4u v[P]; };
     const unsigned short *p;
-    int64_t apart;                                         // from the first array to the second one
-    __device__ __forceinline__ void set(const unsigned short *h, int64_t at, int64_t to_rest) { p = h + at; apart = to_rest; }
+    int64_t apart;                                         // from one array to the next
+    __device__ __forceinline__ void set(const unsigned short *h, int64_t at, int64_t to_next) { p = h + at; apart = to_next; }
     template <bool TAIL>
     __device__ __forceinline__ void load(Raw &r, int k, int left) const
     {
-        r.v[0] = TAIL ? load8(p, k, left) : *reinterpret_cast<const v4u_u *>(p + k);
-        r.v[1] = TAIL ? load8(p + apart, k, left) : *reinterpret_cast<const v4u_u *>(p + apart + k);
+#pragma unroll
+        for (int q = 0; q < P; ++q) r.v[q] = TAIL ? load8(p + q * apart, k, left) : *reinterpret_cast<const v4u_u *>(p + q * apart + k);
     }
-    static __device__ __forceinline__ void operands(const Raw &r, v4u (&x)[P]) { x[0] = r.v[0]; x[1] = r.v[1]; }
-    static __device__ __forceinline__ void split(float h, unsigned short &a, unsigned short &b)
+    static __device__ __forceinline__ void operands(const Raw &r, v4u (&x)[P])
     {
-        const float v = h * scale;
-        a = narrow<T>(v);
-        const float w = widen<T>(a), r = (v - w) * rest;
-        b = __builtin_isfinite(w) ? narrow<T>(r) : (unsigned short)0;
+#pragma unroll
+        for (int q = 0; q < P; ++q) x[q] = r.v[q];
+    }
+    static __device__ __forceinline__ void store(unsigned short *h, int64_t at, int64_t to_next, float v)
+    {
+        unsigned part[P];
+        cut(v, part);
+#pragma unroll
+        for (int q = 0; q < P; ++q) h[at + q * to_next] = (unsigned short)(part[q] >> 16);
+    }
+};
+// 32 bits as two parts of f16, the nearest one and the nearest one to what is left, which is as close as 32 bits are: 2^-24 of the value.  f16 has
+// a small range, so a wave scales its columns of a vector by a power of two that takes the largest finite value to 2^14 .. 2^15 (keep_scaled); what lies
+// 2^17 and more below that is off by 2^-25 / 2^14 of it.
+struct Scaled {
+    static constexpr int P = 2;
+    static __device__ __forceinline__ void operands(const v4f (&v)[2], int up, v4u (&x)[P])      // in the order of the codes
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const v2f s = {__builtin_amdgcn_ldexpf(v[0][i], up), __builtin_amdgcn_ldexpf(v[1][i], up)};
+            const v2h hi = __builtin_convertvector(s, v2h);
+            // what is left is 8 at most; of an infinity it is no number, and then -16, which leaves the product with the first part as it is
+            const v2f rest = {fmaxf(s[0] - (float)hi[0], -16.0f), fmaxf(s[1] - (float)hi[1], -16.0f)};
+            x[0][i] = __builtin_bit_cast(unsigned, hi);
+            x[1][i] = __builtin_bit_cast(unsigned, __builtin_convertvector(rest, v2h));
+        }
     }
 };
 // The copy: for every tile and block of 32 columns, P kilobytes, one per part, the 16 bytes of lane l at 16 l.  Columns are padded with zeros
@@ -231,13 +249,7 @@ template <int T, class X>
 __device__ __forceinline__ v4f product(const v4u (&x)[X::P], v4u w, v4f c)
 {
 #pragma unroll
-    for (int q = 0; q < X::P; ++q)
-        if (!(X::LO && q == X::P - 1)) c = mfma16<T>(x[q], w, c);
-    if constexpr (X::LO) {
-        const v4f d = mfma16<T>(x[X::P - 1], w, v4f{0, 0, 0, 0});
-#pragma unroll
-        for (int e = 0; e < 4; ++e) c[e] = fmaf(d[e], 1.0f / X::rest, c[e]);
-    }
+    for (int q = 0; q < X::P; ++q) c = mfma16<T>(x[q], w, c);
     return c;
 }
 
@@ -247,10 +259,23 @@ struct Weights16 {
     int64_t ld, stride;
     int rows, cols;
 };
-// B: blocks of 32 columns in a chunk: four for few vectors, two for tiles.
-template <int T_, int R_, int B_>
+// f16 weights for vectors in parts of bf16: 11 significant bits are two parts, cut off like those of the vectors.
+__device__ __forceinline__ void cut_f16(v4u w, v4u &hi, v4u &lo)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float a = widen<F16>((unsigned short)w[i]), b = widen<F16>((unsigned short)(w[i] >> 16));
+        const float p = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, a) & 0xffff0000u), q = __builtin_bit_cast(float, __builtin_bit_cast(unsigned, b) & 0xffff0000u);
+        hi[i] = __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, b), __builtin_bit_cast(unsigned, a), 0x07060302u);
+        lo[i] = __builtin_amdgcn_perm(__builtin_bit_cast(unsigned, b - q), __builtin_bit_cast(unsigned, a - p), 0x07060302u);
+    }
+}
+// B: blocks of 32 columns in a chunk: four for few vectors, two for tiles.  XT: type of the vectors' operands.
+template <int T_, int XT, int R_, int B_>
 struct Span16 {
-    static constexpr int T = T_, R = R_, B = B_, CH = 32 * B, PIECES = 1;
+    static constexpr int T = XT, R = R_, B = B_, CH = 32 * B, PIECES = 1;
+    static constexpr bool CUT = XT != T_;
+    static_assert(!CUT || T_ == F16, "f16 weights");
     static constexpr bool SPREAD = false, CODES = false;
     static constexpr float unit = 1;
     const unsigned short *p[R][2];
@@ -308,7 +333,14 @@ struct Span16 {
                 v4u w[2];
                 place(g.w[r][u], w);
 #pragma unroll
-                for (int j = 0; j < 2; ++j) f.d[r][2 * u + j] = product<T, X>(x, w[j], f.d[r][2 * u + j]);
+                for (int j = 0; j < 2; ++j) {
+                    v4u p[2] = {w[j], w[j]};
+                    if constexpr (CUT) {
+                        cut_f16(w[j], p[0], p[1]);
+                        f.d[r][2 * u + j] = product<T, X>(x, p[1], f.d[r][2 * u + j]);
+                    }
+                    f.d[r][2 * u + j] = product<T, X>(x, p[0], f.d[r][2 * u + j]);
+                }
             }
     }
     template <bool TAIL, int NT, class X>
@@ -317,9 +349,15 @@ struct Span16 {
 #pragma unroll
         for (int j = 0; j < B; ++j)
 #pragma unroll
-            for (int r = 0; r < R; ++r)
+            for (int r = 0; r < R; ++r) {
+                v4u w[2] = {all[r][j], all[r][j]};
+                if constexpr (CUT) cut_f16(all[r][j], w[0], w[1]);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) acc[r][t] = product<T, X>(raw[t][j].v, all[r][j], acc[r][t]);
+                for (int t = 0; t < NT; ++t) {
+                    if constexpr (CUT) acc[r][t] = product<T, X>(raw[t][j].v, w[1], acc[r][t]);
+                    acc[r][t] = product<T, X>(raw[t][j].v, w[0], acc[r][t]);
+                }
+            }
     }
 };
 
@@ -741,7 +779,8 @@ struct KeptQ4 {
     typedef KeptSpace<KW, R, GB, S> Space;
     typedef typename Space::Scale Scale;
     static constexpr int THREADS = 64 * KW, NG = GB < 8 ? 8 / GB : 1, PER = GB < 4 ? GB : 4;
-    static constexpr float unit = code_unit<T>;
+    static constexpr bool SCALED = std::is_same<X, Scaled>::value;
+    static constexpr float unit = SCALED ? 0x1p9f : code_unit<T>;
     static constexpr int E = GB == 1 ? 2 : 1;              // scales of 16 rows that a thread brings: 2 / GB for each of them
     Space &sp;
     const WeightsQ4 (&w)[R];
@@ -749,6 +788,7 @@ struct KeptQ4 {
     int rows, cols, c, lane, wave;
     bool any, partial;                                     // whether the wave has columns, and fewer than a chunk
     typename Copied<X>::Raw x[2][4];
+    int lift[4];                                           // SCALED: powers of two of the lane's four vectors, less those of unit (as code_unit)
     v4u g[2][R][2];
     Scale s[R][E];
     unsigned char z[R][E];
@@ -845,7 +885,7 @@ struct KeptQ4 {
                         // a block past the last column counts nothing: its sum is zero, and so has the scale to be
                         const float f = c * KEPT_CHUNK + 128 * h + 32 * PER * i < cols ? factor(fs[at]) : 0.0f;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[r][e] = fmaf(sum[e], f, acc[r][e]);
+                        for (int e = 0; e < 4; ++e) acc[r][e] = fmaf(SCALED ? __builtin_amdgcn_ldexpf(sum[e], lift[e]) : sum[e], f, acc[r][e]);
                     }
                 }
             }
@@ -884,6 +924,32 @@ __device__ __forceinline__ void keep_copied(K &k, const Copied<X> &x)
 #pragma unroll
             for (int j = 0; j < 4; ++j) x.load(k.x[h][j], 8 * k.c + 4 * h + j);
     }
+}
+// or from one of 32 bits, where 16 bytes of a lane are two times 16 (vectors from `live` on repeat the one before),
+template <class K>
+__device__ __forceinline__ void keep_scaled(K &k, const v4f *copy, int live)
+{
+    if (!k.any) return;
+    v4f v[8][2];
+    float top = 0;
+#pragma unroll
+    for (int b = 0; b < 8; ++b)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) v[b][e] = copy[((8 * k.c + b) * 2 + e) * 64 + (k.lane & 48) + min(k.lane & 15, live - 1)];
+#pragma unroll
+    for (int b = 0; b < 8; ++b)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            top = fmaxf(top, __builtin_fabsf(v[b][e >> 2][e & 3]));
+        }
+    top = fmaxf(top, __shfl_xor(top, 16, WAVE));
+    top = fmaxf(top, __shfl_xor(top, 32, WAVE));
+    // (with an infinity no sum of its vector is finite, whatever the others are rounded to)
+    const int up = 15 - __builtin_amdgcn_frexp_expf(fminf(top, __FLT_MAX__));
+#pragma unroll
+    for (int b = 0; b < 8; ++b) Scaled::operands(v[b], up, k.x[b >> 2][b & 3].v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) k.lift[i] = -9 - __shfl(up, 4 * (k.lane >> 4) + i, WAVE);
 }
 // or 16-bit vectors 16 tile and on as they are, whole lines at a time, through LDS like the weights.
 template <int T, class K>

@@ -332,8 +332,8 @@ def test_gelu_keeps_its_relative_error(dtype, n):
     crd, vals = torch.zeros(n, 1, dtype=torch.int32), torch.ones(n, 1)
     ref, _ = R.layer(x, crd, vals, doubles(w1), doubles(w3), doubles(w2), 1, t, 0)
     # of erfc(-v / sqrt 2): two roundings of its argument, times |d log erfc(z) / d log z| <= 2 z^2 + 1 = v^2 + 1; 16 steps for it and three products;
-    # two 16-bit parts of bf16: 2^-16; rounding of Y (gelu(0) = 0 is its smallest number away at most)
-    bound = ref.abs() * ((x[:, :1].double() ** 2 + 17) * R.STEP + 2.0 ** -16) + R.out_error(ref, t)
+    # rounding of Y (gelu(0) = 0 is its smallest number away at most)
+    bound = ref.abs() * (x[:, :1].double() ** 2 + 17) * R.STEP + R.out_error(ref, t)
     R.check(run16(x, crd, vals, w1, w3, w2, 1), ref, bound, "16 bits")
     y = torch.empty(n, dim, dtype=t, device="cuda")
     psk.psk_moe_experts_q4(x.cuda(), crd.cuda(), vals.cuda(), q1, q3, q2, y, act=psk.PSK_ACT_GELU)
@@ -353,8 +353,84 @@ def test_scales_of_the_layer_near_the_largest_number(dtype, scale32, n):
     ref = R.act(x[:, :1].double(), 0).expand(n, dim)
     y = torch.empty(n, dim, dtype=t, device="cuda")
     psk.psk_moe_experts_q4(x.cuda(), crd.cuda(), vals.cuda(), *q, y)
-    # every sum has one term: 16 steps for the activation and the products, two 16-bit parts between them, rounding of Y
-    R.check(y, ref, ref.abs() * (16 * R.STEP + 2.0 ** -16) + R.out_error(ref, t), "large scales")
+    # every sum has one term: 16 steps for the activation and the products, rounding of Y
+    R.check(y, ref, ref.abs() * 16 * R.STEP + R.out_error(ref, t), "large scales")
+
+
+def both_layers(x, pairs, act=0):
+    """Y of one expert with 16-bit weights and with 4-bit ones, gate 1; pairs: (16 bits, 4 bits) of W1, W3, W2."""
+    n, dim = x.shape
+    crd, vals = torch.zeros(n, 1, dtype=torch.int32), torch.ones(n, 1)
+    y = torch.empty(n, dim, dtype=x.dtype, device="cuda")
+    psk.psk_moe_experts_q4(x.cuda(), crd.cuda(), vals.cuda(), *(q for _, q in pairs), y, act=act)
+    return ("16 bits", run16(x, crd, vals, *(w for w, _ in pairs), act)), ("4 bits", y)
+
+
+def ones(rows, cols, at, dtype):
+    """One expert's matrix of 1 and -1 at places (row, column, sign), 0 elsewhere: 16 bits, and the same in 4."""
+    w, codes = torch.zeros(1, rows, cols, dtype=dtype), torch.full((1, rows, (cols + 31) // 32 * 16), 0x88, dtype=torch.uint8)
+    for r, c, sign in at:
+        w[0, r, c] = sign
+        codes[0, r, c // 2] += sign * (16 if c % 2 else 1)
+    return w, psk.Q4(codes.cuda(), torch.ones(1, rows, 1, dtype=dtype).cuda(), cols=cols, group=8192)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n", [1, 3, 23])
+@pytest.mark.parametrize("x1,w3,w2", [(-10, -14, 15), (10, 15, -14)])
+def test_far_values_between_the_products_keep_their_relative_error(dtype, n, x1, w3, w2):
+    """h of about 2^-24 and of about 2^25, every sum of one term."""
+    t, dim = TYPES[dtype], 8
+    x = torch.zeros(n, dim, dtype=t)
+    x[:, 0], x[:, 1] = torch.linspace(0.7, 3, n).to(t), 2.0 ** x1
+    pairs = selecting(dim, dim, 0, 1.0, t), selecting(dim, dim, 1, 2.0 ** w3, t), selecting(dim, dim, lambda r: r, 2.0 ** w2, t)
+    ref = (R.act(x[:, :1].double(), 0) * 2.0 ** (x1 + w3 + w2)).expand(n, dim)
+    for what, y in both_layers(x, pairs):
+        # 16 steps of 32 bits for the activation and the products
+        R.check(y, ref, ref.abs() * 16 * R.STEP + R.out_error(ref, t), what)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("n", [1, 3, 23])
+@pytest.mark.parametrize("inter", [8, 1500, 3000, 4104])
+def test_values_between_the_products_keep_32_bits(dtype, n, inter):
+    """Differences of two h that agree in their first 11 to 13 bits: h[2i] = s (1 + d), h[2i+1] = s with s = silu(v), Y = s d.  Every way of the
+    second product, by its columns."""
+    t, dim = TYPES[dtype], 8
+    rng = np.random.default_rng(n)
+    x = torch.zeros(n, dim, dtype=t)
+    x[:, 0], x[:, 1], x[:, 2] = torch.linspace(0.7, 3, n).to(t), 1, torch.from_numpy(2.0 ** rng.uniform(-13, -11, n)).to(t)
+    pairs = (ones(inter, dim, [(r, 0, 1) for r in range(inter)], t), ones(inter, dim, [(r, 1, 1) for r in range(inter)] + [(r, 2, 1) for r in range(0, inter, 2)], t),
+             ones(dim, inter, [(r, 2 * (r * (inter // 2 - 1) // 7) + k, 1 - 2 * k) for r in range(dim) for k in (0, 1)], t))
+    s = R.act(x[:, :1].double(), 0)
+    ref = (s * x[:, 2:3].double()).expand(n, dim)
+    # s is the same number in both: its 16 steps count relative to Y.  1 + d in 32 bits and the product with it: half a step each, in both; the second
+    # product adds up six parts of at most s (1 + d) each: a step of the sizes so far, of 2 s, for each
+    bound = ref.abs() * 16 * R.STEP + s.abs() * (2 + 6 * 2) * 1.001 * R.STEP + R.out_error(ref, t)
+    for what, y in both_layers(x, pairs):
+        R.check(y, ref, bound, what)
+
+
+@pytest.mark.parametrize("n", [1, 3, 23])
+def test_infinite_values_between_the_products(n):
+    """h beyond 2^128 in every other token: Y is infinite there (all weights behind h are 1) and finite in the others."""
+    dim = 8
+    x = torch.zeros(n, dim, dtype=torch.bfloat16)
+    x[:, 0], x[:, 1] = torch.linspace(0.7, 3, n).to(torch.bfloat16), 2.0 ** -70
+    x[0::2, 1] = 2.0 ** 70
+    pairs = (selecting(dim, dim, 0, 1.0, torch.bfloat16), selecting(dim, dim, 1, 2.0 ** 60, torch.bfloat16),
+             ones(dim, dim, [(r, c, 1) for r in range(dim) for c in range(dim)], torch.bfloat16))
+    ref = (8 * R.act(x[:, :1].double(), 0) * x[:, 1:2].double() * 2.0 ** 60).expand(n, dim).clone()
+    ref[0::2] = math.inf
+    for what, y in both_layers(x, pairs):
+        R.check(y, ref, ref.abs() * 32 * R.STEP + R.out_error(ref, torch.bfloat16), what)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("top_k,experts", [(5, 3), (3, 1), (64, 2), (20, 30)])
+def test_one_token_with_an_expert_in_every_slot(dtype, top_k, experts):
+    test_layer(dtype, 1, 72, 40, experts, top_k, "twice")
+    test_layer_q4(dtype, (32, 64), False, 1, 72, 40, experts, top_k, "twice")
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
