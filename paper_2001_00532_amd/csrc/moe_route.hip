@@ -93,7 +93,7 @@ __global__ __launch_bounds__(THREADS) void k_route_logits(int n, int dim, int ex
     constexpr int N = EB * TB, M = N / 4;
     static_assert(N % 4 == 0, "a quarter of the sums to each row of lanes");
     __shared__ double part[THREADS / WAVE][N];
-    const int groups = (experts + EB - 1) / EB, e0 = blockIdx.x % groups * EB, t0 = blockIdx.x / groups * TB, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int e0 = blockIdx.x * EB, t0 = blockIdx.y * TB, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     double acc[N] = {};
     for (int k = 8 * threadIdx.x; k < dim; k += 8 * THREADS) {
         double w[EB][8];
@@ -207,7 +207,7 @@ template <int XT, int WT>
 void logits_of(int n, int dim, int experts, const void *X, int64_t ldx, const void *W, int64_t ldw, double *logits, hipStream_t s)
 {
     if (n == 1) PSK_LAUNCH((k_route_logits<XT, WT, 4, 1>), dim3((experts + 3) / 4), dim3(THREADS), 0, s, n, dim, experts, X, ldx, W, ldw, logits);
-    else PSK_LAUNCH((k_route_logits<XT, WT, 4, 8>), dim3((experts + 3) / 4 * ((n + 7) / 8)), dim3(THREADS), 0, s, n, dim, experts, X, ldx, W, ldw, logits);
+    else PSK_LAUNCH((k_route_logits<XT, WT, 4, 8>), dim3((experts + 3) / 4, (n + 7) / 8), dim3(THREADS), 0, s, n, dim, experts, X, ldx, W, ldw, logits);
 }
 
 }  // namespace

@@ -107,6 +107,21 @@ def test_route_strides():
     assert torch.equal(crd.cpu(), a) and torch.equal(vals.cpu(), b)
 
 
+@pytest.mark.parametrize("experts", [3, 1024])
+def test_as_many_tokens_as_a_call_may_have(experts):
+    n, dim, top_k = psk.PSK_MAX_VECTORS, 8, 2
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    x, w = torch.randn(n, dim, generator=g, device="cuda"), torch.randn(experts, dim, generator=g, device="cuda")
+    crd, vals = torch.full((n, top_k), 99, dtype=torch.int32, device="cuda"), torch.full((n, top_k), 99.0, device="cuda")
+    psk.psk_moe_route(x, w, crd, vals, normalise=False)
+    torch.cuda.synchronize()
+    for t in (0, 123457, n - 9):
+        ids, gates = R.route(x[t:t + 9].cpu(), w.cpu(), top_k, 0, None, False, 1.0)
+        assert torch.equal(crd[t:t + 9].cpu(), ids)
+        R.check(vals[t:t + 9], gates, gates.abs() * 2.0 ** -23 + 1e-40, "tokens from %d" % t)
+
+
 # ------------------------------------------------------------------ layer
 def gating(rng, n, experts, top_k, kind="random"):
     crd = np.full((n, top_k), -1, dtype=np.int32)
