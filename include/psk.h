@@ -524,7 +524,7 @@ int psk_calibrate_gather_lds(const float *table, int32_t table_elems, const uint
  */
 typedef enum { PSK_F32 = 0, PSK_F16 = 1, PSK_BF16 = 2 } psk_type;
 
-#define PSK_MAX_VECTORS (1 << 19)       /* largest n; a matrix has at most 2^28 rows and columns */
+#define PSK_MAX_VECTORS (1 << 19)       /* largest n; a matrix has at most 2^28 - 256 rows and columns */
 #define PSK_MOE_MAX_EXPERTS 1024
 #define PSK_MOE_MAX_TOP_K 64
 

@@ -9,7 +9,9 @@ static_assert(PSK_F32 == F32 && PSK_F16 == F16 && PSK_BF16 == BF16, "types");
 
 namespace {
 
-constexpr int64_t kMaxEdge = int64_t(1) << 28;            // rows and columns: places in the copy of a tile of vectors are counted in 32 bits
+// Rows and columns: a launch has fewer than 2^32 threads, 256 of them for 16 rows padded to 256; and places in the copy of a tile of vectors are
+// counted in 32 bits.
+constexpr int64_t kMaxEdge = (int64_t(1) << 28) - 256;
 
 inline int hip_status(hipError_t e) { return e == hipSuccess ? PSK_OK : PSK_ERR_HIP; }
 inline bool type_ok(int t) { return t == PSK_F32 || t == PSK_F16 || t == PSK_BF16; }

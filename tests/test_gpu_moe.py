@@ -469,6 +469,39 @@ def test_weights_at_any_element(dtype, n, dim, inter):
     assert torch.equal(got, run16(x, crd, vals, *(m.contiguous() for m in w)))
 
 
+@pytest.mark.parametrize("n", [1, 5])
+@pytest.mark.parametrize("dim,inter", [((1 << 28) - 256, 16), (16, (1 << 28) - 256)])
+def test_as_many_rows_and_columns_as_a_matrix_may_have(n, dim, inter):
+    """Weights that are zero but in the first and the last two columns, 16 bits and 4."""
+    t = torch.bfloat16
+    crd, vals = torch.zeros(n, 1, dtype=torch.int32, device="cuda"), torch.ones(n, 1, device="cuda")
+    x = torch.zeros(n, dim, dtype=t, device="cuda")
+    x[:, 0], x[:, -2], x[:, -1] = (torch.linspace(a, b, n) for a, b in ((0.5, 1), (-1, 2), (1, -0.5)))
+    # a = u = x[0] + x[-2] - x[-1], Y = h[0] + h[-2] - h[-1] with h alike in all columns
+    v = x[:, 0].double() + x[:, -2].double() - x[:, -1].double()
+    size = x[:, 0].double().abs() + x[:, -2].double().abs() + x[:, -1].double().abs()
+    h = R.act(v, 0) * v
+    # sums of three numbers (and zeros): 8 steps of their sizes in a and in u, |act'| <= 1.13; 16 steps for the activation and the products; Y is three h
+    bound = 3 * ((1.13 + 1) * 8 * R.STEP * size * (v.abs() + size) + 24 * R.STEP * h.abs()) + R.out_error(h, t)
+
+    def wide(rows, cols):
+        w = torch.zeros(1, rows, cols, dtype=t, device="cuda")
+        w[:, :, 0], w[:, :, -2], w[:, :, -1] = 1, 1, -1
+        return w
+
+    def four(rows, cols):
+        codes = torch.full((1, rows, cols // 32 * 16 + 16), 0x88, dtype=torch.uint8, device="cuda")
+        codes[:, :, 0] = 0x89
+        codes[:, :, cols // 2 - 1] = 0x79
+        return psk.Q4(codes, torch.ones(1, rows, 1, dtype=t, device="cuda"), cols=cols, group=1 << 30)
+    for make, call in ((wide, psk.psk_moe_experts), (four, psk.psk_moe_experts_q4)):
+        y = torch.full((n, dim), 77.0, dtype=t, device="cuda")
+        call(x, crd, vals, make(inter, dim), make(inter, dim), make(dim, inter), y)
+        torch.cuda.synchronize()
+        off = (y.double() - h[:, None]).abs() / bound[:, None]
+        assert float(off.max()) <= 1, float(off.max())
+
+
 def test_one_matrix_holds_both_halves():
     """W1 and W3 as the halves of one tensor, experts a stride apart."""
     rng = np.random.default_rng(14)

@@ -210,6 +210,23 @@ def test_codes_beyond_four_gigabytes(rows, cols, n):
         R.check(y[:, part], ref, bound, "rows from %d" % r)
 
 
+@pytest.mark.parametrize("n", [1, 5])
+def test_as_many_rows_as_a_matrix_may_have(n):
+    rows, cols, group = (1 << 28) - 256, 32, 32
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    codes = torch.randint(0, 256, (rows, 16), generator=g, device="cuda", dtype=torch.uint8)
+    scales = torch.rand(rows, 1, generator=g, device="cuda", dtype=torch.float16)
+    x = torch.randn(n, cols, generator=g, device="cuda").half()
+    y = torch.zeros(n, rows, device="cuda", dtype=torch.float16)
+    psk.psk_gemm_q4(psk.Q4(codes, scales, cols=cols, group=group), x, y)
+    torch.cuda.synchronize()
+    for r in (0, rows // 2 + 3, rows - 17):
+        part = slice(r, r + 17)
+        ref, bound = R.gemm(R.dequantised(codes[part].cpu(), scales[part].cpu(), None, cols, group), x.cpu(), torch.float16)
+        R.check(y[:, part], ref, bound, "rows from %d" % r)
+
+
 @pytest.mark.parametrize("n", [1, 20])
 def test_other_stream_and_graph(n):
     """On a stream that is not the current one, and captured: replays follow the activations, with eager work in between."""

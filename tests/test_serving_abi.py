@@ -109,6 +109,23 @@ def test_layer_q4_refuses():
     assert layer_q4(w1=q4(count=10, stride_codes=40)) == 7 and layer_q4(X=ODD) == 7
 
 
+def test_largest_sizes():
+    """One row or column more than a launch has threads for is refused, as many as it has are not (X = NULL is, after that)."""
+    most = 2 ** 28 - 256
+    big = dict(ld_codes=1 << 28, ld_scales=1 << 28, stride_codes=0, stride_scales=0)
+    for rows, cols in ((most, 100), (48, most)):
+        assert gemm(q4(rows=rows, cols=cols, **big), X=NULL, ldx=1 << 28, ldy=1 << 28, have=1 << 50) == 1
+        assert psk.psk_gemm_q4_workspace_bytes(rows, cols, 5, psk.PSK_BF16) > 0 and psk.psk_moe_workspace_bytes(5, rows, cols, 3, 2) > 0
+        assert layer(dim=rows, inter=cols, X=NULL, ldx=1 << 28, ldy=1 << 28, ld1=1 << 28, ld2=1 << 28, have=1 << 50) == 1
+    for rows, cols in ((most + 1, 100), (48, most + 1), (2 ** 28, 100), (48, 2 ** 28)):
+        assert gemm(q4(rows=rows, cols=cols, **big), X=NULL, ldx=1 << 28, ldy=1 << 28, have=1 << 50) == 2
+        assert psk.psk_gemm_q4_workspace_bytes(rows, cols, 5, psk.PSK_BF16) == 0 and psk.psk_moe_workspace_bytes(5, rows, cols, 3, 2) == 0
+        assert layer(dim=rows, inter=cols, X=NULL, ldx=1 << 28, ldy=1 << 28, ld1=1 << 28, ld2=1 << 28, have=1 << 50) == 2
+        w = dict(count=10, **big)
+        assert layer_q4(q4(rows=cols, cols=rows, **w), q4(rows=cols, cols=rows, **w), q4(rows=rows, cols=cols, **w), X=NULL, ldx=1 << 28, ldy=1 << 28) == 2
+    assert route(dim=most, X=NULL, ldx=1 << 28, ldw=1 << 28) == 1 and route(dim=most + 1, X=NULL, ldx=1 << 28, ldw=1 << 28) == 2
+
+
 def test_binding_refuses():
     """Shapes and types are checked before an address is asked for, host tensors when it is."""
     codes, scales = torch.zeros(8, 32, dtype=torch.uint8), torch.zeros(8, 2)
