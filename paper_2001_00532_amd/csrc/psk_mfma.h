@@ -125,7 +125,8 @@ struct Plain16 {                                           // 16 bits
     static __device__ __forceinline__ void operands(const Raw &r, v4u (&x)[P]) { x[0] = r.v; }
 };
 // 32 bits as three parts of bf16: v = a + b + c with 8 significant bits in each, cut off and not rounded, so the sum is exact and a
-// value near the largest does not become infinite.  Infinity and NaN stand in the first part alone.
+// value near the largest does not become infinite.  Exact from 2^-110 on: below, the last bits are less than 2^-133, the smallest number of bf16, and are
+// lost.  Infinity and NaN stand in the first part alone.
 __device__ __forceinline__ void cut(float value, unsigned (&part)[3])      // the upper halves are the parts
 {
     const float v = __builtin_canonicalizef(value);        // a NaN keeps its first bit

@@ -161,6 +161,28 @@ def test_vectors_of_32_bits_keep_their_bits():
     assert abs(got - float(ref)) <= 256 * 2.0 ** -14 * 2.0 ** -23 * 2 ** 9, (got, float(ref))
 
 
+@pytest.mark.parametrize("power", [0, -109])
+@pytest.mark.parametrize("rows,cols,n", [(20, 300, 1), (20, 2500, 4), (20, 512, 5), (20, 1000, 33), (20, 1536, 16), (20, 2040, 5), (20, 2560, 16), (20, 5000, 33),
+                                         (1500, 2560, 33)])
+@pytest.mark.parametrize("group", [32, 64, 128, 256])
+def test_every_way_keeps_the_bits_of_vectors_of_32_bits(rows, cols, n, group, power):
+    """Neighbouring numbers cancel to their last bits: rows of +1 -1 or -1 +1 by pairs of columns, each worth a step of 2^-23."""
+    rng = np.random.default_rng(cols + n)
+    signs = rng.integers(0, 2, (rows, cols // 2))
+    codes = torch.zeros(rows, (cols + 31) // 32 * 16, dtype=torch.uint8)
+    codes[:, :cols // 2] = torch.from_numpy(np.where(signs, 0x79, 0x97).astype(np.uint8))      # +1 -1, -1 +1
+    scales = torch.full((rows, (cols + group - 1) // group), 2.0 ** min(100, -power))
+    a = torch.from_numpy(rng.uniform(1, 2, (n, cols // 2)) * (1 - 2 * rng.integers(0, 2, (n, cols // 2)))).float()
+    x = torch.empty(n, cols)
+    x[:, 0::2], x[:, 1::2] = torch.nextafter(a, 2 * a), a
+    d = (x[:, 0::2] - x[:, 1::2]).double()
+    ref = d @ torch.from_numpy(2.0 * signs - 1).t()
+    got = product((codes, scales, None), (x * 2.0 ** power).cuda(), cols, group).cpu().double() * 2.0 ** -(power + min(100, -power))
+    # the sums of each part are multiples of its last bit, 2^-7, 2^-15 and 2^-23, and of 32 products below 2^6, 2^-2 and 2^-10; those of all three, of a
+    # group and of the row, multiples of 2^-23 below 2: everything is exact
+    assert torch.equal(got, ref), float((got - ref).abs().max() / ref.abs().max())
+
+
 def test_empty_products():
     x = torch.zeros(3, 64, device="cuda", dtype=torch.float16)
     codes, scales = torch.zeros(8, 32, dtype=torch.uint8, device="cuda"), torch.ones(8, 2, device="cuda", dtype=torch.float16)
