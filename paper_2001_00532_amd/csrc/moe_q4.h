@@ -7,10 +7,10 @@ namespace psk {
 namespace {
 
 // ---- more than four tokens, up to KEPT_COLUMNS columns in both products: the vectors kept (KeptQ4)
-// 48 tokens, 8 of 64 experts of 3 x 1000 x 2048 in f16: 36.9 us for the first step and 29.8 for the second; by k_moe_up and k_moe_down the whole
+// 48 tokens, 8 of 64 experts of 3 x 1000 x 2048 in f16: 37 us for the first step and 31 for the second; by k_moe_up and k_moe_down the whole
 // layer took 154 us, by the first form of these 90.  The matrices once would be 29 us: instructions that dequantise share the time with the loads.
 // Between the two, h goes to memory in 32 bits and becomes two parts of f16 where it is kept (Scaled): 64 registers, three parts of bf16 are 96 (the layer for 48
-// tokens, 4 of 16 experts of 3 x 2048 x 4096: 101 us, with these 111; of 32 of 3 x 3500 x 1000 72 and 114).
+// tokens, 4 of 16 experts of 3 x 2048 x 4096: 101 us, with these 111; of 32 of 3 x 3500 x 1000 72 and 114; all with twice the workgroups of kept_groups).
 template <int T, int GB, int S, int KW>
 __global__ __launch_bounds__(64 * KW, 4) void k_moe_q4_up(Call a, WeightsQ4 w1, WeightsQ4 w3)
 {
@@ -64,22 +64,23 @@ __global__ __launch_bounds__(64 * KW, KW > 4 && GB > 1 ? 4 : 1) void k_moe_q4_do
         });
     }
 }
-// Workgroups per expert, no more than sets: `rounds` times as many as are on the chip at once (1024 threads to a compute unit).  One for the first step
-// (64 experts of 1000 x 2048: 36.9 us, with two 38.1) and two for the second, which needs fewer registers (29.8 us, with one 32.2).
-inline int kept_groups(int sets, int slots, int kw, int rounds)
+// Workgroups per expert, no more than sets: as many as are on the chip at once (1024 threads to a compute unit).  With twice as many the first step takes 38.1 us
+// and not 36.9 (64 experts of 1000 x 2048); the second one brings h into two parts in each, the layers for 48 tokens, 4 of 32 experts of 3 x 3500 x 1000 and of
+// 3 x 1024 x 2048 with groups of 32: 67.5 and 57.9 us, with twice as many workgroups there 71.9 and 59.9, three times 79.4 and 63.8.
+inline int kept_groups(int sets, int slots, int kw)
 {
-    const int n = rounds * 256 * (16 / kw) / slots;
+    const int n = 256 * (16 / kw) / slots;
     return n < 1 ? 1 : (n < sets ? n : sets);
 }
 template <int T, int GB, int S, int KW>
 void launch_up(const Call &a, int slots, const WeightsQ4 &w1, const WeightsQ4 &w3, hipStream_t s)
 {
-    PSK_LAUNCH((k_moe_q4_up<T, GB, S, KW>), dim3(kept_groups((a.inter + 15) / 16, slots, KW, 1), slots), dim3(64 * KW), 0, s, a, w1, w3);
+    PSK_LAUNCH((k_moe_q4_up<T, GB, S, KW>), dim3(kept_groups((a.inter + 15) / 16, slots, KW), slots), dim3(64 * KW), 0, s, a, w1, w3);
 }
 template <int GB, int S, int KW>
 void launch_down(const Call &a, int slots, const WeightsQ4 &w2, hipStream_t s)
 {
-    PSK_LAUNCH((k_moe_q4_down<GB, S, KW>), dim3(kept_groups((a.dim + 15) / 16, slots, KW, 2), slots), dim3(64 * KW), 0, s, a, w2);
+    PSK_LAUNCH((k_moe_q4_down<GB, S, KW>), dim3(kept_groups((a.dim + 15) / 16, slots, KW), slots), dim3(64 * KW), 0, s, a, w2);
 }
 template <int T, int S, int G1, int G2>
 struct KeptSteps {
