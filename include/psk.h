@@ -550,8 +550,8 @@ typedef struct {
 /*
  * Y = X A^T: Y[t][i] = sum_j A[i][j] X[t][j] for one matrix in 4 bits (count = 1) and n vectors of `type`; n = 1 is the
  * matrix-vector product.  cols = 0 gives zeros.
- * Activations in 32 bits keep all their bits (each is multiplied in three parts), but what is less than 2^-133: those of 2^-110 and more lose nothing.
- * A Y in 32 bits below 2^-117 may lose its last bits.  Y has the type of X.
+ * Activations in 32 bits keep all their bits (each is multiplied in three parts), but what is less than 2^-133: those of 2^-110 and more
+ * lose nothing.  A Y in 32 bits below 2^-117 may lose its last bits.  Y has the type of X.
  */
 size_t psk_gemm_q4_workspace_bytes(int64_t rows, int64_t cols, int64_t n, int type);
 int psk_gemm_q4(const psk_q4 *A, int64_t n, int type, const void *X, int64_t ldx, void *Y, int64_t ldy, void *workspace,
@@ -582,7 +582,9 @@ int psk_moe_route(int64_t n, int64_t dim, int64_t experts, int32_t top_k, int sc
  * psk_moe_experts: weights of `type`, matrix e of W1 and W3 at stride1*e elements, rows ld1 apart (W2: stride2, ld2).  No alignment beyond the
  * element's is asked of them; rows that begin at multiples of 16 bytes are read fastest.
  * psk_moe_experts_q4: weights in 4 bits, count = experts in all three, W1 and W3 alike in rows, cols and group, all with one scale_type.
- * Values between the two products keep 32 bits (as the activations of psk_gemm_q4 do).  W2 is finite: what an infinite weight of it is multiplied into becomes infinite or NaN.
+ * Values between the two products keep 32 bits as the activations of psk_gemm_q4 do (psk_moe_experts_q4 with more than four tokens and at most 4096
+ * rows and columns: or are off by 2^-39 of the largest one among the 256 columns they belong to).
+ * W2 is finite: what an infinite weight of it is multiplied into becomes infinite or NaN.
  * The workspace is for both.
  */
 enum { PSK_ACT_SILU = 0, PSK_ACT_GELU = 1 };   /* v / (1 + exp(-v));  v (1 + erf(v / sqrt 2)) / 2 */
