@@ -8,7 +8,7 @@
 //
 // Three ways, by the rules in by_group, more_vectors and few_vectors_by_columns:
 //   up to four vectors            k_gemv_q4        32768 x 8192, one vector of bf16, groups of 64: 29.7 us = 4.8 TB/s of codes and scales
-//   more, up to 4096 (f32: 2048) columns  k_gemm_q4_kept   10240 x 4096, 16 vectors of bf16: 10.2 us; 8192 x 4096, 64 vectors of f16: 16.5 us
+//   more, up to 4096 (f32: 2048) columns  k_gemm_q4_kept   10240 x 4096, 16 vectors of bf16: 11.0 us; 8192 x 4096, 64 vectors of f16: 16.5 us
 //   more, longer rows             k_gemm_q4        4096 x 8192, 16 vectors of bf16: 9.6 us; 64 vectors of f16: 17.4 us
 #pragma once
 #include "psk_internal.h"

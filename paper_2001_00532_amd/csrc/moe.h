@@ -13,9 +13,9 @@
 // dies made k_moe_down five times as slow.)
 // Up to four tokens, every workgroup finds its expert and that one's positions itself from crd.
 //
-// Measured (kernels; floor: the matrices once at 7.1 TB/s): one token, 6 of 64 experts of 3 x 1024 x 2048 in bf16 11.3 + 6.1 + 3.5 us (10.7); 24
-// tokens, 4 of 32 experts of 3 x 1280 x 4096 in f16 5.1 + 105 + 61 + 4.7 (137); one token, 4 of 32 experts of 3 x 2048 x 4096 in 4 bits
-// 13.4 + 7.6 + 3.3 (7.4).
+// Measured (kernels; floor: the matrices once at 7.1 TB/s): one token, 6 of 64 experts of 3 x 1024 x 2048 in bf16 11.2 + 5.9 + 3.6 us (10.7); 24
+// tokens, 4 of 32 experts of 3 x 1280 x 4096 in f16 5.1 + 106 + 63 + 4.8 (137); one token, 4 of 32 experts of 3 x 2048 x 4096 in 4 bits
+// 13.1 + 6.6 + 3.1 (7.4).
 //
 // h keeps its 32 bits: it goes to memory as three parts of bf16 (Thirds), and f16 weights are cut into two parts for them.  The matrix instructions
 // that this takes have room where memory is waited for.  (4-bit weights and kept vectors: as it is, moe_q4.h.)
