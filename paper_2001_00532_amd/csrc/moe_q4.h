@@ -25,7 +25,7 @@ __global__ __launch_bounds__(64 * KW, 4) void k_moe_q4_up(Call a, WeightsQ4 w1, 
         Copied<Plain16<T>> x;
         x.set(a.copy, g.tile + t, copied_blocks(a.dim), k.lane);
         keep_copied(k, x);
-        const auto store = [&](int set, int v, int i, float h) {
+        const auto store = [&](int set, int v, int i, float h) {           // where keep_scaled looks for column c of vector v
             const int c = 16 * set + i;
             reinterpret_cast<float *>(a.h)[((((int64_t)(g.tile + t) * copied_blocks(a.inter) + (c >> 5)) * 2 + (c >> 2 & 1)) * 64 + 16 * (c >> 3 & 3) + v) * 4 + (c & 3)] = h;
         };
