@@ -597,6 +597,67 @@ int psk_moe_experts_q4(int64_t n, int32_t top_k, int act, int type, const void *
                        const float *vals, const psk_q4 *W1, const psk_q4 *W3, const psk_q4 *W2, void *Y, int64_t ldy,
                        void *workspace, size_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------------------------------------------------------------------------
+ * The two ends of a language model and its projections in 8 bits: tokens become rows of a table, rows of activations become logits.
+ * Conventions as for the products with weights in 4 bits.
+ */
+#define PSK_I8_MAX_COLS 131071          /* sums of products of two 8-bit integers stay within 32 bits */
+#define PSK_I8_MAX_LD (1 << 23)         /* largest leading dimension of codes */
+#define PSK_MAX_TOKENS (1 << 24)        /* largest n of the embedding */
+
+/*
+ * rows x cols weights code * scale: codes[i*ld + j] (-128 .. 127), a scale per row (channel).
+ *  - codes are 16-byte aligned, ld is a multiple of 16, and the ceil(cols/16)*16 first bytes of a row are readable (what they hold from
+ *    column cols on is of no account).
+ */
+typedef struct {
+    int64_t rows, cols, ld;
+    const int8_t *codes;
+    const float *scales;
+} psk_i8;
+
+/*
+ * Tokens (or a matrix of weights, row by row) in 8 bits: for row t of X (n x cols, `type`), with m = max_j |X[t][j]|,
+ *   codes[t*ldc + j] = the integer nearest to 127 X[t][j] / m, ties to even       scales[t] = m / 127
+ * The codes are those of exact arithmetic.  A row of zeros gets zeros and the scale 0; a row that holds an infinity or NaN gets zeros and
+ * the scale NaN, so that what it is multiplied into shows it.  (A scale below 2^-126 loses bits as every small number does.)
+ * codes: 16-byte aligned, ldc a multiple of 16 and ceil(cols/16)*16 at least; the bytes of a row from column cols up to there become zeros.
+ */
+int psk_quant_i8(int64_t n, int64_t cols, int type, const void *X, int64_t ldx, int8_t *codes, int64_t ldc, float *scales, void *stream);
+
+/*
+ * Y[t][i] = (sum_j q[t][j] A[i][j]) * a_i * s_t + bias[i]: n tokens by one matrix, with codes q and a scale s_t per token; A and a_i are the codes
+ * and scales of `A`, bias is float[rows] or NULL for none.  Sums are whole numbers and exact; the products with the scales are made in 32 bits
+ * in the order written and rounded once to `type`, the type of Y.  cols = 0 gives the bias.
+ * psk_gemm_i8: the codes X (laid out as those of psk_i8, ldx a multiple of 16) and scales are given.
+ * psk_linear_i8: X (n x cols, of `type`, as Y) is quantised in the call, as psk_quant_i8 does.
+ */
+size_t psk_gemm_i8_workspace_bytes(int64_t rows, int64_t cols, int64_t n);
+int psk_gemm_i8(const psk_i8 *A, int64_t n, const int8_t *X, int64_t ldx, const float *scales, const float *bias, int type, void *Y, int64_t ldy,
+                void *workspace, size_t workspace_bytes, void *stream);
+size_t psk_linear_i8_workspace_bytes(int64_t rows, int64_t cols, int64_t n, int type);
+int psk_linear_i8(const psk_i8 *A, int64_t n, int type, const void *X, int64_t ldx, const float *bias, void *Y, int64_t ldy, void *workspace,
+                  size_t workspace_bytes, void *stream);
+
+/*
+ * The embedding lookup: Y[t][:] = factor * E[ids[t]][:] for n tokens and a table of rows x dim; the product by a matrix with one stored entry
+ * per row.  A token outside [0, rows) stands for none: its row of Y becomes zeros.  Products in 32 bits, rounded once to the type of Y.
+ * psk_embed: a table of `type`.  psk_embed_i8: a table in 8 bits, which an output layer may share (psk_linear_i8); dim = E->cols.
+ */
+int psk_embed(int64_t n, int64_t rows, int64_t dim, const int32_t *ids, float factor, int type, const void *E, int64_t lde, int ytype, void *Y,
+              int64_t ldy, void *stream);
+int psk_embed_i8(const psk_i8 *E, int64_t n, const int32_t *ids, float factor, int ytype, void *Y, int64_t ldy, void *stream);
+
+/*
+ * Its gradient, the product by the transpose: dE[v][:] = factor * sum of dY[t][:] over the tokens t with ids[t] = v, for every row v of the table
+ * (rows without a token become zeros); with `accumulate` this is added to dE instead, and rows without a token are not touched.  Tokens outside
+ * [0, rows) and those equal to `padding` (-1: none) add nothing.  Sums in 32 bits, in an order that depends on the positions of the tokens alone;
+ * rounded once to gtype, which is PSK_F32 or `type`, the type of dY.
+ */
+size_t psk_embed_grad_workspace_bytes(int64_t n, int64_t rows, int64_t dim);
+int psk_embed_grad(int64_t n, int64_t rows, int64_t dim, const int32_t *ids, int32_t padding, float factor, int type, const void *dY, int64_t ldy,
+                   int gtype, void *dE, int64_t lde, int accumulate, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

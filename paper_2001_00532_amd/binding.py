@@ -37,6 +37,8 @@ EXPORTS = [
     "psk_spmv_slab_f64", "psk_cu_trace_set", "psk_calibrate_stream_read", "psk_calibrate_gather", "psk_calibrate_gather_lds",
     "psk_gemm_q4_workspace_bytes", "psk_gemm_q4", "psk_moe_route_workspace_bytes", "psk_moe_route", "psk_moe_workspace_bytes",
     "psk_moe_experts", "psk_moe_experts_q4",
+    "psk_quant_i8", "psk_gemm_i8_workspace_bytes", "psk_gemm_i8", "psk_linear_i8_workspace_bytes", "psk_linear_i8",
+    "psk_embed", "psk_embed_i8", "psk_embed_grad_workspace_bytes", "psk_embed_grad",
 ]
 
 
@@ -61,6 +63,14 @@ class psk_q4(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int64) for n in ("count", "rows", "cols")] + [(n, ctypes.c_int32) for n in ("group", "scale_type")] + \
                [(n, ctypes.c_void_p) for n in ("codes", "scales", "zeros")] + \
                [(n, ctypes.c_int64) for n in ("ld_codes", "ld_scales", "stride_codes", "stride_scales")]
+
+
+PSK_I8_MAX_COLS, PSK_I8_MAX_LD, PSK_MAX_TOKENS = 131071, 1 << 23, 1 << 24
+
+
+class psk_i8(ctypes.Structure):
+    """Mirror of the C struct psk_i8 (host memory; the pointers are device addresses)."""
+    _fields_ = [(n, ctypes.c_int64) for n in ("rows", "cols", "ld")] + [(n, ctypes.c_void_p) for n in ("codes", "scales")]
 
 
 class PskError(RuntimeError):
@@ -184,6 +194,17 @@ def lib() -> ctypes.CDLL:
         L.psk_moe_experts.restype = ci
         L.psk_moe_experts_q4.argtypes = [i64, i32, ci, ci, p, i64, p, p, q4, q4, q4, p, i64, p, sz, p]
         L.psk_moe_experts_q4.restype = ci
+        i8 = ctypes.POINTER(psk_i8)
+        L.psk_quant_i8.argtypes, L.psk_quant_i8.restype = [i64, i64, ci, p, i64, p, i64, p, p], ci
+        L.psk_gemm_i8_workspace_bytes.argtypes, L.psk_gemm_i8_workspace_bytes.restype = [i64, i64, i64], sz
+        L.psk_gemm_i8.argtypes, L.psk_gemm_i8.restype = [i8, i64, p, i64, p, p, ci, p, i64, p, sz, p], ci
+        L.psk_linear_i8_workspace_bytes.argtypes, L.psk_linear_i8_workspace_bytes.restype = [i64, i64, i64, ci], sz
+        L.psk_linear_i8.argtypes, L.psk_linear_i8.restype = [i8, i64, ci, p, i64, p, p, i64, p, sz, p], ci
+        L.psk_embed.argtypes, L.psk_embed.restype = [i64, i64, i64, p, f32, ci, p, i64, ci, p, i64, p], ci
+        L.psk_embed_i8.argtypes, L.psk_embed_i8.restype = [i8, i64, p, f32, ci, p, i64, p], ci
+        L.psk_embed_grad_workspace_bytes.argtypes, L.psk_embed_grad_workspace_bytes.restype = [i64, i64, i64], sz
+        L.psk_embed_grad.argtypes = [i64, i64, i64, p, i32, f32, ci, p, i64, ci, p, i64, ci, p, sz, p]
+        L.psk_embed_grad.restype = ci
         if _marshal is None:
             native = _native_side()
             if native is not None:
@@ -851,3 +872,159 @@ def psk_moe_experts_q4(X, crd, vals, W1: Q4, W3: Q4, W2: Q4, Y, act=PSK_ACT_SILU
     if st:
         _check(st, "psk_moe_experts_q4")
     return Y
+
+
+class I8:
+    """A matrix in 8 bits with a scale per row: the C struct (`desc`) and the tensors it points into.
+
+    codes: int8, rows x bytes, a row begins at a multiple of 16 bytes and holds ceil(cols / 16) * 16 at least.  scales: float32, rows.
+    psk_quant_i8 makes both from weights (row by row), or from tokens."""
+
+    def __init__(self, codes, scales, cols=None):
+        if codes.dtype != torch.int8 or scales.dtype != torch.float32:
+            raise ValueError("codes must be int8 and scales float32")
+        if codes.dim() != 2 or tuple(scales.shape) != (codes.shape[0],) or not scales.is_contiguous():
+            raise ValueError("codes must have two dimensions, and scales must be a contiguous tensor of one per row")
+        cols = codes.shape[1] if cols is None else int(cols)
+        if cols < 0 or codes.shape[1] < (cols + 15) // 16 * 16:
+            raise ValueError("a row of codes must hold %d bytes for %d columns" % ((cols + 15) // 16 * 16, cols))
+        if scales.device != codes.device:
+            raise ValueError("codes and scales must be on one device")
+        self.codes, self.scales = codes, scales
+        d = self.desc = psk_i8()
+        d.rows, d.cols, d.ld = codes.shape[0], cols, _ld_codes(codes)
+        d.codes, d.scales = _ptr(codes, torch.int8), _ptr(scales, torch.float32)
+        self.rows, self.cols, self._ref = d.rows, d.cols, ctypes.byref(d)
+
+
+def _ld_codes(codes):
+    return int(codes.stride(0)) if codes.shape[0] > 1 else (max(int(codes.stride(0)), codes.shape[1]) + 15) // 16 * 16
+
+
+def _vector(t, n, dtype, what):
+    """Address of a contiguous vector of n."""
+    if t is not None and (t.shape != (n,) or not t.is_contiguous()):
+        raise ValueError("%s: expected a contiguous tensor of %d, got %s" % (what, n, tuple(t.shape)))
+    return _ptr(t, dtype)
+
+
+def psk_quant_i8(X, codes, scales, stream=None):
+    """(codes, scales): the rows of X (n x cols) in 8 bits; codes int8 of n x bytes, whose rows hold ceil(cols / 16) * 16 bytes at least (I8)."""
+    if X.dim() != 2 or codes.dim() != 2:
+        raise ValueError("psk_quant_i8: X and codes must have two dimensions")
+    n, cols = X.shape
+    x, ldx = _rows(X, n, cols, X.dtype, "psk_quant_i8: X")
+    if codes.shape[0] != n or codes.shape[1] < (cols + 15) // 16 * 16:
+        raise ValueError("psk_quant_i8: codes must have %d rows of %d bytes at least" % (n, (cols + 15) // 16 * 16))
+    s = _vector(scales, n, torch.float32, "psk_quant_i8: scales")
+    _one_device("psk_quant_i8", X, codes, scales)
+    st = lib().psk_quant_i8(n, cols, _type(X, "psk_quant_i8"), x, ldx, _ptr(codes, torch.int8), _ld_codes(codes), s, _stream(stream))
+    if st:
+        _check(st, "psk_quant_i8")
+    return codes, scales
+
+
+def psk_gemm_i8_workspace_bytes(rows: int, cols: int, n: int) -> int:
+    return int(lib().psk_gemm_i8_workspace_bytes(int(rows), int(cols), int(n)))
+
+
+def psk_gemm_i8_workspace(A: I8, n: int, stream=None):
+    """A byte tensor that suits psk_gemm_i8 with n tokens."""
+    b = psk_gemm_i8_workspace_bytes(A.rows, A.cols, n)
+    if b == 0:
+        raise ValueError("invalid arguments for psk_gemm_i8_workspace_bytes")
+    return _alloc_bytes(b, A.codes.device, stream)
+
+
+def psk_gemm_i8(A: I8, X, scales, Y, bias=None, ws=None, stream=None):
+    """Y (n x rows) = X A^T for tokens in 8 bits: X int8 of n x bytes (as the codes of I8) and a scale per token."""
+    n, type = Y.shape[0], _type(Y, "psk_gemm_i8")
+    if X.dim() != 2 or X.shape[0] != n or X.shape[1] < (A.cols + 15) // 16 * 16:
+        raise ValueError("psk_gemm_i8: X must have %d rows of %d bytes at least" % (n, (A.cols + 15) // 16 * 16))
+    y, ldy = _rows(Y, n, A.rows, Y.dtype, "psk_gemm_i8: Y")
+    s, b = _vector(scales, n, torch.float32, "psk_gemm_i8: scales"), _vector(bias, A.rows, torch.float32, "psk_gemm_i8: bias")
+    _one_device("psk_gemm_i8", X, scales, Y, A.codes, bias, ws)
+    if ws is None:
+        ws = psk_gemm_i8_workspace(A, n, stream)
+    st = lib().psk_gemm_i8(A._ref, n, _ptr(X, torch.int8), _ld_codes(X), s, b, type, y, ldy, _ptr(ws), ws.numel(), _stream(stream))
+    if st:
+        _check(st, "psk_gemm_i8")
+    return Y
+
+
+def psk_linear_i8_workspace_bytes(rows: int, cols: int, n: int, type: int) -> int:
+    return int(lib().psk_linear_i8_workspace_bytes(int(rows), int(cols), int(n), int(type)))
+
+
+def psk_linear_i8_workspace(A: I8, X, stream=None):
+    """A byte tensor that suits psk_linear_i8 with tokens like X (n x cols)."""
+    b = psk_linear_i8_workspace_bytes(A.rows, A.cols, X.shape[0], _type(X, "X"))
+    if b == 0:
+        raise ValueError("invalid arguments for psk_linear_i8_workspace_bytes")
+    return _alloc_bytes(b, X.device, stream)
+
+
+def psk_linear_i8(A: I8, X, Y, bias=None, ws=None, stream=None):
+    """Y (n x rows) = X (n x cols) A^T, the tokens quantised in the call."""
+    n, dtype = X.shape[0], X.dtype
+    type = _type(X, "psk_linear_i8")
+    x, ldx = _rows(X, n, A.cols, dtype, "psk_linear_i8: X")
+    y, ldy = _rows(Y, n, A.rows, dtype, "psk_linear_i8: Y")
+    b = None if bias is None else _vector(bias, A.rows, torch.float32, "psk_linear_i8: bias")
+    _one_device("psk_linear_i8", X, Y, A.codes, bias, ws)
+    if ws is None:
+        ws = psk_linear_i8_workspace(A, X, stream)
+    st = lib().psk_linear_i8(A._ref, n, type, x, ldx, b, y, ldy, _ptr(ws), ws.numel(), _stream(stream))
+    if st:
+        _check(st, "psk_linear_i8")
+    return Y
+
+
+def psk_embed(ids, E, Y, factor=1.0, stream=None):
+    """Y (n x dim) = factor * the rows of E that the tokens `ids` (int32, n) name, zeros for a token outside the table.  E: rows x dim of
+    any of the three types, or an I8."""
+    n, ytype = Y.shape[0], _type(Y, "psk_embed")
+    i = _vector(ids, n, torch.int32, "psk_embed: ids")
+    if isinstance(E, I8):
+        y, ldy = _rows(Y, n, E.cols, Y.dtype, "psk_embed: Y")
+        _one_device("psk_embed", ids, E.codes, Y)
+        st = lib().psk_embed_i8(E._ref, n, i, float(factor), ytype, y, ldy, _stream(stream))
+    else:
+        rows, dim = E.shape
+        y, ldy = _rows(Y, n, dim, Y.dtype, "psk_embed: Y")
+        e, lde = _rows(E, rows, dim, E.dtype, "psk_embed: E")
+        _one_device("psk_embed", ids, E, Y)
+        st = lib().psk_embed(n, rows, dim, i, float(factor), _type(E, "psk_embed"), e, lde, ytype, y, ldy, _stream(stream))
+    if st:
+        _check(st, "psk_embed")
+    return Y
+
+
+def psk_embed_grad_workspace_bytes(n: int, rows: int, dim: int) -> int:
+    return int(lib().psk_embed_grad_workspace_bytes(int(n), int(rows), int(dim)))
+
+
+def psk_embed_grad_workspace(dY, dE, stream=None):
+    """A byte tensor that suits psk_embed_grad with gradients like dY (n x dim) and dE (rows x dim)."""
+    b = psk_embed_grad_workspace_bytes(dY.shape[0], dE.shape[0], dE.shape[1])
+    if b == 0:
+        raise ValueError("invalid arguments for psk_embed_grad_workspace_bytes")
+    return _alloc_bytes(b, dE.device, stream)
+
+
+def psk_embed_grad(ids, dY, dE, factor=1.0, padding=-1, accumulate=False, ws=None, stream=None):
+    """dE (rows x dim) = (dE if accumulate) + factor * the sums of the rows of dY (n x dim) whose tokens are the same, in the order of their
+    positions.  Tokens outside the table, and those equal to `padding`, add nothing."""
+    (n, dim), rows = dY.shape, dE.shape[0]
+    type, gtype = _type(dY, "psk_embed_grad"), _type(dE, "psk_embed_grad")
+    i = _vector(ids, n, torch.int32, "psk_embed_grad: ids")
+    y, ldy = _rows(dY, n, dim, dY.dtype, "psk_embed_grad: dY")
+    e, lde = _rows(dE, rows, dim, dE.dtype, "psk_embed_grad: dE")
+    _one_device("psk_embed_grad", ids, dY, dE, ws)
+    if ws is None:
+        ws = psk_embed_grad_workspace(dY, dE, stream)
+    st = lib().psk_embed_grad(n, rows, dim, i, int(padding), float(factor), type, y, ldy, gtype, e, lde, int(bool(accumulate)), _ptr(ws), ws.numel(),
+                              _stream(stream))
+    if st:
+        _check(st, "psk_embed_grad")
+    return dE

@@ -1,0 +1,68 @@
+// The embedding lookup (formulas: embed.h).  Bound by reading the rows of different tokens and writing Y.
+#include "embed.h"
+
+namespace psk {
+namespace {
+
+// L lanes to a row, 256 / L rows per workgroup at once.
+template <int ET, int YT>
+__global__ __launch_bounds__(256) void k_embed(int n, int rows, int dim, int lanes_log, const int *__restrict__ ids, float factor, const void *E, int64_t lde,
+                                               const float *__restrict__ scales, void *Y, int64_t ldy)
+{
+    const int lanes = 1 << lanes_log, sub = threadIdx.x & (lanes - 1), units = (dim + 7) >> 3;
+    const int64_t step = (int64_t)gridDim.x * (256 >> lanes_log);
+    for (int64_t t = (int64_t)blockIdx.x * (256 >> lanes_log) + (threadIdx.x >> lanes_log); t < n; t += step) {
+        const int id = ids[t];
+        const bool none = (unsigned)id >= (unsigned)rows;
+        const typename Bits<ET>::type *e = static_cast<const typename Bits<ET>::type *>(E) + (none ? 0 : id * lde);
+        typename Bits<YT>::type *y = static_cast<typename Bits<YT>::type *>(Y) + t * ldy;
+        float f = factor;
+        if constexpr (ET == I8) f *= none ? 0.0f : scales[id];
+        if (dim < 8) {
+            for (int k = sub; k < dim; k += lanes) store_as<YT>(Y, t * ldy + k, none ? 0.0f : element<ET>(e, k) * f);
+            continue;
+        }
+        for (int u = sub; u < units; u += lanes) {
+            const int k = unit_of(u, dim).col;
+            float v[8] = {};
+            if (!none) {
+                Raw8<ET> r;
+                load_raw<ET>(r, e + k);
+                widen_raw<ET>(r, v);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] *= f;
+            }
+            store8<YT>(y + k, v);
+        }
+    }
+}
+
+template <int ET, int YT>
+hipError_t launch(int n, int rows, int dim, const int *ids, float factor, const void *E, int64_t lde, const float *scales, void *Y, int64_t ldy, hipStream_t s)
+{
+    const int units = (dim + 7) / 8;
+    int log = 0;
+    while (log < 8 && (1 << log) < units) ++log;
+    const int64_t blocks = ((int64_t)n + (256 >> log) - 1) / (256 >> log);
+    PSK_LAUNCH((k_embed<ET, YT>), dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s, n, rows, dim, log, ids, factor, E, lde, scales, Y, ldy);
+    return take_launch_status();
+}
+
+template <int ET>
+hipError_t launch_y(int ytype, int n, int rows, int dim, const int *ids, float factor, const void *E, int64_t lde, const float *scales, void *Y, int64_t ldy,
+                    hipStream_t s)
+{
+    const auto f = ytype == F32 ? launch<ET, F32> : (ytype == F16 ? launch<ET, F16> : launch<ET, BF16>);
+    return f(n, rows, dim, ids, factor, E, lde, scales, Y, ldy, s);
+}
+
+}  // namespace
+
+hipError_t launch_embed(int n, int rows, int dim, const int *ids, float factor, int etype, const void *E, int64_t lde, const float *scales, int ytype,
+                        void *Y, int64_t ldy, hipStream_t s)
+{
+    const auto f = etype == F32 ? launch_y<F32> : (etype == F16 ? launch_y<F16> : (etype == BF16 ? launch_y<BF16> : launch_y<I8>));
+    return f(ytype, n, rows, dim, ids, factor, E, lde, scales, Y, ldy, s);
+}
+
+}  // namespace psk

@@ -1,0 +1,87 @@
+// Products of 8-bit integers with a scale for each token and channel.
+//
+//   q[t][j] = the integer nearest to 127 X[t][j] / m_t (ties to even), m_t = max_j |X[t][j]|, s_t = m_t / 127
+//   Y[t][i] = (sum_j q[t][j] A[i][j]) a_i s_t + b_i
+//
+// Sums are whole numbers in 32 bits and exact (2^14 times 131071 columns is less than 2^31), so they do not depend on their order.
+#pragma once
+#include "psk_internal.h"
+#include "psk_mfma.h"
+
+namespace psk {
+
+typedef int v4i_e __attribute__((ext_vector_type(4), aligned(4)));
+typedef unsigned short v4s __attribute__((ext_vector_type(4)));
+typedef unsigned short v4s_u __attribute__((ext_vector_type(4), aligned(2)));
+
+// Eight elements from column k on, zeros from column `cols` on.
+template <int T>
+__device__ __forceinline__ void load_cols(const void *row, int k, int cols, float (&v)[8])
+{
+    if constexpr (T == F32) {
+        const float *p = static_cast<const float *>(row);
+        if (k + 8 <= cols) {
+            const v4f_e a = *reinterpret_cast<const v4f_e *>(p + k), b = *reinterpret_cast<const v4f_e *>(p + k + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = k + i < cols ? p[k + i] : 0.0f;
+        }
+    } else {
+        const v4u u = load8(static_cast<const unsigned short *>(row), k, cols);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = widen<T>((unsigned short)(u[i / 2] >> 16 * (i & 1)));
+    }
+}
+
+// The sizes' bits, which order as the sizes do, infinity and NaN last.
+__device__ __forceinline__ unsigned size_bits(float v) { return __builtin_bit_cast(unsigned, v) & 0x7fffffffu; }
+constexpr unsigned INFINITE = 0x7f800000u;
+
+// How a token is quantised.  A quotient in 32 bits is off by less than 2^-14, so where it is farther than 2^-10 from the middle between two integers,
+// the nearest one is right; nearer, 254 |x| and (2k + 1) m, which 64 bits hold without rounding, are compared.  `up` keeps the reciprocal of a small m finite.
+struct Quantiser {
+    float m, up, inverse;
+    bool none;                                             // only zeros, or something that is not finite: the codes are zeros
+    __device__ __forceinline__ Quantiser(unsigned bits)
+    {
+        m = __builtin_bit_cast(float, bits);
+        none = bits == 0 || bits >= INFINITE;
+        up = m < 0x1p-100f ? 0x1p100f : 1.0f;
+        inverse = none ? 0.0f : 127.0f / (m * up);
+    }
+    __device__ __forceinline__ float scale() const { return none && m != 0.0f ? __builtin_nanf("") : m / 127.0f; }
+    __device__ __forceinline__ int code(float x) const
+    {
+        if (none) return 0;
+        const float q = x * up * inverse, r = rintf(q);
+        int c = (int)r;
+        if (fabsf(fabsf(q - r) - 0.5f) < 0x1p-10f) {
+            const int k = (int)fabsf(q);
+            const double d = 254.0 * fabs((double)x) - (double)(2 * k + 1) * (double)m;
+            c = k + (d > 0.0 || (d == 0.0 && (k & 1)));
+            c = x < 0.0f ? -c : c;
+        }
+        return c;
+    }
+};
+__device__ __forceinline__ unsigned pack4(const int *c)
+{
+    return (unsigned)(c[0] & 255) | (unsigned)(c[1] & 255) << 8 | (unsigned)(c[2] & 255) << 16 | (unsigned)c[3] << 24;
+}
+
+__device__ __forceinline__ unsigned wave_max(unsigned v)
+{
+#pragma unroll
+    for (int d = 1; d < WAVE; d *= 2) v = max(v, (unsigned)__shfl_xor((int)v, d, WAVE));
+    return v;
+}
+
+// What becomes of a sum.
+struct Finish {
+    const float *a, *s, *bias;                             // of channels, of tokens, of channels or NULL
+};
+__device__ __forceinline__ float finish(int sum, float a, float s, float b) { return (float)sum * a * s + b; }
+
+}  // namespace psk

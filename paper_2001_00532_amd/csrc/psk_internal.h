@@ -251,6 +251,8 @@ struct SlabBuildSpace {
     size_t bytes;
 };
 size_t scan_tmp_ints(int64_t n);
+// exclusive scan of in[0 .. n) into out (in place allowed); tmp: scan_tmp_ints(n)
+hipError_t launch_exclusive_scan(const int32_t *in, int32_t *out, int64_t n, int32_t *tmp, hipStream_t s);
 SlabBuildSpace carve_slab_build(void *base, int64_t rows, int64_t cols, int64_t nnz, int32_t W);
 hipError_t launch_slab_build(int32_t rows, int32_t cols, int32_t nnz, const int32_t *pos, const int32_t *crd,
                              const float *vals, const SlabBuildSpace &w, float *svals, uint16_t *scol,
@@ -314,5 +316,15 @@ hipError_t launch_moe_16(const MoeCall &c, int type, const void *W1, const void 
                          int64_t stride2, hipStream_t s);
 template <int T>
 hipError_t launch_moe_q4_of(const MoeCall &c, int scale_type, const WeightsQ4 &w1, const WeightsQ4 &w3, const WeightsQ4 &w2, hipStream_t s);
+
+// Products of 8-bit integers (gemm_i8.h) and the embedding (embed.h).  A table of psk_i8 has the type 3 and its scales.
+hipError_t launch_quant_i8(int n, int cols, int fill, int type, const void *X, int64_t ldx, int8_t *codes, int64_t ldc, float *scales, hipStream_t s);
+hipError_t launch_gemm_i8(int rows, int cols, int n, const int8_t *A, int64_t lda, const float *a, const int8_t *X, int64_t ldx, const float *xs,
+                          const float *bias, int type, void *Y, int64_t ldy, hipStream_t s);
+hipError_t launch_embed(int n, int rows, int dim, const int *ids, float factor, int etype, const void *E, int64_t lde, const float *scales, int ytype, void *Y,
+                        int64_t ldy, hipStream_t s);
+size_t embed_grad_workspace_bytes(int64_t n, int64_t dim);
+hipError_t launch_embed_grad(int n, int rows, int dim, const int *ids, int padding, float factor, int type, const void *dY, int64_t ldy, int gtype, void *dE,
+                             int64_t lde, int accumulate, void *workspace, hipStream_t s);
 
 }  // namespace psk

@@ -368,6 +368,11 @@ static void launch_scan(const int32_t *in, int32_t *out, int64_t n, int32_t *bsu
     if (nonzero) PSK_LAUNCH(k_scan_apply<true>, dim3((unsigned)nb), dim3(256), 0, s, in, out, (long long)n, bsum);
     else PSK_LAUNCH(k_scan_apply<false>, dim3((unsigned)nb), dim3(256), 0, s, in, out, (long long)n, bsum);
 }
+hipError_t launch_exclusive_scan(const int32_t *in, int32_t *out, int64_t n, int32_t *tmp, hipStream_t s)
+{
+    launch_scan(in, out, n, tmp, false, s);
+    return take_launch_status();
+}
 
 // ------------------------------------------------------------------ the analysis step: CSR -> slab hierarchy
 // H[s * nblk + b] = number of positions of block b (BUILD_BT consecutive CSR positions) that fall into slab s.
