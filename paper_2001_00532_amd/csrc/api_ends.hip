@@ -79,8 +79,10 @@ int psk_gemm_i8(const psk_i8 *A, int64_t n, const int8_t *X, int64_t ldx, const 
         if (st != PSK_OK) return st;
     }
     if (misaligned(Y, bytes_of(type)) || misaligned(scales, 4) || misaligned(bias, 4)) return PSK_ERR_ALIGNMENT;
-    return hip_status(launch_gemm_i8((int)A->rows, (int)A->cols, (int)n, A->codes, A->ld, A->scales, X, ldx, scales, bias, type, Y, ldy,
-                                     static_cast<hipStream_t>(stream)));
+    if (gemv_i8_takes((int)A->cols, (int)n))
+        return hip_status(launch_gemv_i8((int)A->rows, (int)A->cols, (int)n, A->codes, A->ld, A->scales, X, ldx, scales, bias, type, Y, ldy,
+                                         static_cast<hipStream_t>(stream)));
+    return hip_status(launch_gemm_i8((int)A->rows, (int)A->cols, (int)n, A->codes, A->ld, A->scales, X, ldx, scales, bias, type, Y, ldy, static_cast<hipStream_t>(stream)));
 }
 
 size_t psk_linear_i8_workspace_bytes(int64_t rows, int64_t cols, int64_t n, int type)
@@ -101,6 +103,8 @@ int psk_linear_i8(const psk_i8 *A, int64_t n, int type, const void *X, int64_t l
     if (!Y || (A->cols > 0 && !X)) return PSK_ERR_NULL;
     if (misaligned(X, bytes_of(type)) || misaligned(Y, bytes_of(type)) || misaligned(bias, 4)) return PSK_ERR_ALIGNMENT;
     const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (gemv_i8_takes((int)A->cols, (int)n))
+        return hip_status(launch_gemv_i8((int)A->rows, (int)A->cols, (int)n, A->codes, A->ld, A->scales, X, ldx, nullptr, bias, type, Y, ldy, s));
     const int64_t ld = line(A->cols);
     int8_t *const codes = static_cast<int8_t *>(workspace);
     float *const scales = reinterpret_cast<float *>(codes + align256((size_t)n * (size_t)ld + 1));

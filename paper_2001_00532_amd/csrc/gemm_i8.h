@@ -5,8 +5,7 @@
 //
 // Sums are whole numbers in 32 bits and exact (2^14 times 131071 columns is less than 2^31), so they do not depend on their order.
 #pragma once
-#include "psk_internal.h"
-#include "psk_mfma.h"
+#include "row8.h"
 
 namespace psk {
 
@@ -14,25 +13,27 @@ typedef int v4i_e __attribute__((ext_vector_type(4), aligned(4)));
 typedef unsigned short v4s __attribute__((ext_vector_type(4)));
 typedef unsigned short v4s_u __attribute__((ext_vector_type(4), aligned(2)));
 
-// Eight elements from column k on, zeros from column `cols` on.
+// Eight elements from column k on, zeros from column `cols` on, of a row that has eight: asked for by row_load and had by row_get.  Where the row ends
+// among them, its last eight are loaded and moved.
 template <int T>
-__device__ __forceinline__ void load_cols(const void *row, int k, int cols, float (&v)[8])
+__device__ __forceinline__ void row_load(Raw8<T> &r, const void *row, int k, int cols)
 {
-    if constexpr (T == F32) {
-        const float *p = static_cast<const float *>(row);
-        if (k + 8 <= cols) {
-            const v4f_e a = *reinterpret_cast<const v4f_e *>(p + k), b = *reinterpret_cast<const v4f_e *>(p + k + 4);
+    load_raw<T>(r, static_cast<const typename Bits<T>::type *>(row) + min(k, cols - 8));
+}
+template <int T>
+__device__ __forceinline__ void row_get(const Raw8<T> &r, int k, int cols, float (&v)[8])
+{
+    widen_raw<T>(r, v);
+    if (cols & 7) {
+        const int by = k < cols ? max(k + 8 - cols, 0) : 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-        } else {
+        for (int d = 4; d > 0; d /= 2)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = k + i < cols ? p[k + i] : 0.0f;
-        }
-    } else {
-        const v4u u = load8(static_cast<const unsigned short *>(row), k, cols);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = widen<T>((unsigned short)(u[i / 2] >> 16 * (i & 1)));
+            for (int i = 0; i < 8; ++i) v[i] = by & d ? (i + d < 8 ? v[(i + d) & 7] : 0.0f) : v[i];
     }
+    const bool behind = k >= cols;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = behind ? 0.0f : v[i];
 }
 
 // The sizes' bits, which order as the sizes do, infinity and NaN last.
@@ -75,6 +76,17 @@ __device__ __forceinline__ unsigned wave_max(unsigned v)
 {
 #pragma unroll
     for (int d = 1; d < WAVE; d *= 2) v = max(v, (unsigned)__shfl_xor((int)v, d, WAVE));
+    return v;
+}
+
+// The first `left` of 16 bytes.
+__device__ __forceinline__ v4i first_bytes(v4i v, int left)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int b = min(max(left - 4 * i, 0), 4);
+        v[i] = b == 0 ? 0 : v[i] & (int)(0xffffffffu >> (32 - 8 * b));
+    }
     return v;
 }
 

@@ -23,17 +23,6 @@ __device__ __forceinline__ void step_barrier()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory");
 }
 
-// The first `left` of 16 bytes.
-__device__ __forceinline__ v4i first_bytes(v4i v, int left)
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int b = min(max(left - 4 * i, 0), 4);
-        v[i] = b == 0 ? 0 : v[i] & (int)(0xffffffffu >> (32 - 8 * b));
-    }
-    return v;
-}
-
 template <int YT>
 __device__ __forceinline__ void put4(void *Y, int64_t at, const float (&v)[4], int count)
 {

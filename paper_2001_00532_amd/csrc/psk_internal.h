@@ -321,6 +321,9 @@ hipError_t launch_moe_q4_of(const MoeCall &c, int scale_type, const WeightsQ4 &w
 hipError_t launch_quant_i8(int n, int cols, int fill, int type, const void *X, int64_t ldx, int8_t *codes, int64_t ldc, float *scales, hipStream_t s);
 hipError_t launch_gemm_i8(int rows, int cols, int n, const int8_t *A, int64_t lda, const float *a, const int8_t *X, int64_t ldx, const float *xs,
                           const float *bias, int type, void *Y, int64_t ldy, hipStream_t s);
+bool gemv_i8_takes(int cols, int n);
+hipError_t launch_gemv_i8(int rows, int cols, int n, const int8_t *A, int64_t lda, const float *a, const void *X, int64_t ldx, const float *xs,
+                          const float *bias, int type, void *Y, int64_t ldy, hipStream_t s);
 hipError_t launch_embed(int n, int rows, int dim, const int *ids, float factor, int etype, const void *E, int64_t lde, const float *scales, int ytype, void *Y,
                         int64_t ldy, hipStream_t s);
 size_t embed_grad_workspace_bytes(int64_t n, int64_t dim);
