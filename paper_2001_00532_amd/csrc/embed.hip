@@ -4,12 +4,12 @@
 namespace psk {
 namespace {
 
-// L lanes to a row, 256 / L rows per workgroup at once.
-template <int ET, int YT>
+// 2^lanes_log lanes to a row, W columns to a lane.
+template <int ET, int YT, int W>
 __global__ __launch_bounds__(256) void k_embed(int n, int rows, int dim, int lanes_log, const int *__restrict__ ids, float factor, const void *E, int64_t lde,
                                                const float *__restrict__ scales, void *Y, int64_t ldy)
 {
-    const int lanes = 1 << lanes_log, sub = threadIdx.x & (lanes - 1), units = (dim + 7) >> 3;
+    const int lanes = 1 << lanes_log, sub = threadIdx.x & (lanes - 1), units = (dim + W - 1) / W;
     const int64_t step = (int64_t)gridDim.x * (256 >> lanes_log);
     for (int64_t t = (int64_t)blockIdx.x * (256 >> lanes_log) + (threadIdx.x >> lanes_log); t < n; t += step) {
         const int id = ids[t];
@@ -18,21 +18,21 @@ __global__ __launch_bounds__(256) void k_embed(int n, int rows, int dim, int lan
         typename Bits<YT>::type *y = static_cast<typename Bits<YT>::type *>(Y) + t * ldy;
         float f = factor;
         if constexpr (ET == I8) f *= none ? 0.0f : scales[id];
-        if (dim < 8) {
+        if (dim < W) {
             for (int k = sub; k < dim; k += lanes) store_as<YT>(Y, t * ldy + k, none ? 0.0f : element<ET>(e, k) * f);
             continue;
         }
         for (int u = sub; u < units; u += lanes) {
-            const int k = unit_of(u, dim).col;
-            float v[8] = {};
+            const int k = unit_of<W>(u, dim).col;
+            float v[W] = {};
             if (!none) {
-                Raw8<ET> r;
+                typename RawOf<ET, W>::type r;
                 load_raw<ET>(r, e + k);
                 widen_raw<ET>(r, v);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] *= f;
+                for (int i = 0; i < W; ++i) v[i] *= f;
             }
-            store8<YT>(y + k, v);
+            store_row<YT>(y + k, v);
         }
     }
 }
@@ -40,11 +40,12 @@ __global__ __launch_bounds__(256) void k_embed(int n, int rows, int dim, int lan
 template <int ET, int YT>
 hipError_t launch(int n, int rows, int dim, const int *ids, float factor, const void *E, int64_t lde, const float *scales, void *Y, int64_t ldy, hipStream_t s)
 {
-    const int units = (dim + 7) / 8;
+    constexpr int W = ET == F32 || YT == F32 ? 4 : 8;
+    const int units = (dim + W - 1) / W;
     int log = 0;
     while (log < 8 && (1 << log) < units) ++log;
     const int64_t blocks = ((int64_t)n + (256 >> log) - 1) / (256 >> log);
-    PSK_LAUNCH((k_embed<ET, YT>), dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s, n, rows, dim, log, ids, factor, E, lde, scales, Y, ldy);
+    PSK_LAUNCH((k_embed<ET, YT, W>), dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s, n, rows, dim, log, ids, factor, E, lde, scales, Y, ldy);
     return take_launch_status();
 }
 

@@ -5,12 +5,12 @@
 // begin and end in it.  Of a row that spans tiles, each tile leaves its part in 32 bits, and a third step adds the parts in order.
 // Rows that no token has are cleared beside the tiles.  Bound by reading dY and writing dE.
 #include "embed.h"
+#include <algorithm>
 
 namespace psk {
 namespace {
 
 constexpr int SORT = 2048;                                 // positions per workgroup where several sort
-constexpr int ONE = 16384;                                 // positions that one workgroup sorts by itself
 constexpr int MAX_BITS = 9;                                // of a digit
 constexpr int BASES = 128;                                 // workgroups whose counts every one of them adds up by itself
 
@@ -29,23 +29,26 @@ struct Clear {
 };
 constexpr int RANGE = 1 << 15;                             // rows whose bits are in LDS at once
 
-// L lanes to a row.
+// Zeros for a row of `bytes` bytes, 2^log lanes to it, 16 bytes at a time; the last 16 are the row's last.  Less than 16: element by element.
 template <int GT>
 __device__ __forceinline__ void clear_row(const Clear &c, int64_t row, int sub, int lanes)
 {
     typedef typename Bits<GT>::type B;
+    constexpr int EACH = 16 / sizeof(B);
+    typedef B piece __attribute__((ext_vector_type(EACH), aligned(sizeof(B))));
     B *const p = static_cast<B *>(c.dE) + row * c.lde;
-    const float zeros[8] = {};
-    if (c.dim < 8) {
+    if (c.dim < EACH) {
         if (sub < c.dim) p[sub] = B(0);
     } else {
-        for (int unit = sub; 8 * unit < c.dim; unit += lanes) store8<GT>(p + unit_of(unit, c.dim).col, zeros);
+        for (int k = EACH * sub; k < c.dim; k += EACH * lanes) *reinterpret_cast<piece *>(p + min(k, c.dim - EACH)) = piece(B(0));
     }
 }
+template <int GT>
 __device__ __forceinline__ int lanes_log(int dim)
 {
+    constexpr int EACH = GT == F32 ? 4 : 8;
     int log = 3;
-    while (log < 6 && (8 << log) < dim) ++log;
+    while (log < 6 && (EACH << log) < dim) ++log;
     return log;
 }
 // Beside the sort: workgroup `part` of `parts` reads all tokens and clears those of its rows that none of them names.
@@ -53,15 +56,20 @@ template <int GT, int THREADS>
 __device__ __forceinline__ void clear_unnamed(const Clear &c, const int *__restrict__ ids, int n, int padding, int part, int parts, unsigned *bits)
 {
     const int64_t per = ((int64_t)c.rows + parts - 1) / parts, begin = part * per, end = min(begin + per, (int64_t)c.rows);
-    const int log = lanes_log(c.dim), sub = threadIdx.x & ((1 << log) - 1);
+    const int log = lanes_log<GT>(c.dim), sub = threadIdx.x & ((1 << log) - 1);
     for (int64_t first = begin; first < end; first += RANGE) {
         const int count = (int)min(end - first, (int64_t)RANGE);
         for (int i = threadIdx.x; i < (count + 31) / 32; i += THREADS) bits[i] = 0;
         __syncthreads();
-        for (int t = threadIdx.x; t < n; t += THREADS) {
-            const int id = ids[t];
-            const int64_t at = id - first;
-            if (id != padding && at >= 0 && at < count) atomicOr(&bits[at >> 5], 1u << (at & 31));
+        for (int t = threadIdx.x; t < n; t += 8 * THREADS) {
+            int id[8];                                     // eight loads in flight; behind the last token that is read again
+#pragma unroll
+            for (int i = 0; i < 8; ++i) id[i] = ids[min(t + i * THREADS, n - 1)];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int64_t at = id[i] - first;
+                if (id[i] != padding && at >= 0 && at < count) atomicOr(&bits[at >> 5], 1u << (at & 31));
+            }
         }
         __syncthreads();
         for (int r = threadIdx.x >> log; r < count; r += THREADS >> log)
@@ -84,7 +92,7 @@ __device__ __forceinline__ void clear_absent(const Clear &c, const int *__restri
     __syncthreads();                                       // the last rows' bits have been read
     if ((threadIdx.x & 63) == 0) empty[threadIdx.x >> 6] = m;
     __syncthreads();
-    const int log = lanes_log(c.dim), sub = threadIdx.x & ((1 << log) - 1);
+    const int log = lanes_log<GT>(c.dim), sub = threadIdx.x & ((1 << log) - 1);
     for (int r = threadIdx.x >> log; r < 256; r += 256 >> log)
         if (empty[r >> 6] >> (r & 63) & 1) clear_row<GT>(c, first + r, sub, 1 << log);
 }
@@ -93,10 +101,13 @@ __device__ __forceinline__ void clear_absent(const Clear &c, const int *__restri
 // Lanes of the wave with the same digit as this one, of those that have one.
 __device__ __forceinline__ unsigned long long same_digit(int d, int bits, bool valid)
 {
-    unsigned long long m = __ballot(valid);
+    const unsigned long long all = __ballot(valid);
+    const int one = __builtin_amdgcn_readlane(d, __builtin_ctzll(all | 1ull << 63));
+    if (__ballot(valid && d == one) == all) return all;    // often there is one, or the same one many times
+    unsigned long long m = all;
     for (int b = 0; b < bits; ++b) {
-        const unsigned long long one = __ballot(d >> b & 1);
-        m &= d >> b & 1 ? one : ~one;
+        const unsigned long long set = __ballot(d >> b & 1);
+        m &= d >> b & 1 ? set : ~set;
     }
     return m;
 }
@@ -130,73 +141,93 @@ __device__ __forceinline__ int block_exclusive(int v, int *part)
     return sum;
 }
 
-// Up to ONE positions: the first workgroup sorts them, in LDS, while the others clear.  A wave owns a sixteenth of the positions, and each thread holds
-// its own in registers while their order in LDS changes.
+// Up to NEAR tokens and RANGES ranges of rows: a workgroup owns `per` rows, reads all tokens, and so knows by itself how many positions are before those of
+// its rows.  It counts its own, wave by wave (a wave has a sixteenth of the tokens), puts them in their places, and clears the rows that had none.
+// One launch; a token's workgroups read 4 bytes of L2 each, 16384 tokens and 256 workgroups 16 MB.
+// 16000 tokens, 4000 rows: 9 us; by one workgroup that sorted them in LDS while the others cleared 35.
+constexpr int NEAR = 65536, RANGES = 1024, MOST_ROWS = 512;
+
 template <int GT, bool CLEAR>
-__global__ __launch_bounds__(1024) void k_sort_one(const int *__restrict__ ids, int n, int padding, int digit, int passes, int *__restrict__ keys_out,
-                                                   int *__restrict__ at_out, Clear c)
+__global__ __launch_bounds__(1024) void k_sort_ranges(const int *__restrict__ ids, int n, int padding, int per, int bits, int *__restrict__ keys_out,
+                                                      int *__restrict__ at_out, int *__restrict__ joins, Clear c)
 {
-    constexpr int EACH = ONE / 1024, WAVES = 16;
-    __shared__ int keys[ONE];
-    __shared__ unsigned short at[ONE];
-    __shared__ int seen[WAVES][1 << MAX_BITS];
-    __shared__ int part[WAVES];
-    if (CLEAR && blockIdx.x > 0) {
-        clear_unnamed<GT, 1024>(c, ids, n, padding, blockIdx.x - 1, gridDim.x - 1, reinterpret_cast<unsigned *>(keys));
-        return;
-    }
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, mask = (1 << digit) - 1;
-    const int rounds = (n + 1023) / 1024;                  // of 64 positions per wave
-    const int begin = wave * rounds * 64;
-    int key[EACH], rank[EACH], from[EACH];
+    constexpr int WAVES = 16, U = 16;                      // rounds of 64 tokens whose loads are in flight
+    __shared__ int seen[WAVES][MOST_ROWS];
+    __shared__ int part[WAVES], less[WAVES];
+    __shared__ unsigned long long present[MOST_ROWS / 64];
+    if (blockIdx.x == 0 && threadIdx.x < 2) joins[threadIdx.x] = 0;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int first = blockIdx.x * per, count = min(per, c.rows - first);
+    const int rounds = (n + 1023) / 1024, begin = wave * rounds * 64;
+    for (int d = threadIdx.x; d < WAVES * MOST_ROWS; d += 1024) (&seen[0][0])[d] = 0;
+    __syncthreads();
+    int before = 0;                                        // tokens of earlier rows
+    auto each_round = [&](auto f) {
+        for (int r = 0; r < rounds; r += U) {
+            int id[U];
 #pragma unroll
-    for (int r = 0; r < EACH; ++r) {
-        const int i = begin + 64 * r + lane;
-        from[r] = i;
-        key[r] = r < rounds && i < n ? key_of(ids, i, c.rows, padding) : c.rows;
-    }
-    for (int pass = 0; pass < passes; ++pass) {
-        const int shift = pass * digit;
-        for (int d = threadIdx.x; d < WAVES << MAX_BITS; d += 1024) (&seen[0][0])[d] = 0;
-        __syncthreads();
+            for (int i = 0; i < U; ++i) id[i] = ids[min(begin + 64 * (r + i) + lane, n - 1)];
 #pragma unroll
-        for (int r = 0; r < EACH; ++r)
-            if (r < rounds) rank[r] = place_in_wave(key[r] >> shift & mask, digit, begin + 64 * r + lane < n, lane, seen[wave]);
-        __syncthreads();
-        int sum = 0;
-        if (threadIdx.x <= (unsigned)mask) {
-            for (int w = 0; w < WAVES; ++w) {
-                const int v = seen[w][threadIdx.x];
-                seen[w][threadIdx.x] = sum;
-                sum += v;
+            for (int i = 0; i < U; ++i) {
+                const int at = begin + 64 * (r + i) + lane;
+                f(at, r + i < rounds && at < n && id[i] != padding ? id[i] : -1);
             }
         }
-        const int base = block_exclusive<1024>(sum, part);
-        if (threadIdx.x <= (unsigned)mask)
-            for (int w = 0; w < WAVES; ++w) seen[w][threadIdx.x] += base;
-        __syncthreads();
+    };
+    each_round([&](int, int id) {
+        before += id >= 0 && id < first;
+        const bool mine = id >= first && id < first + count;
+        if (__ballot(mine)) {                              // counts only: nothing waits for LDS
+            const unsigned long long same = same_digit(id - first, bits, mine);
+            if (mine && !(same & ((1ull << lane) - 1))) atomicAdd(&seen[wave][id - first], __popcll(same));
+        }
+    });
+    before += __shfl_xor(before, 1);
+    before += __shfl_xor(before, 2);
+    before += __shfl_xor(before, 4);
+    before += __shfl_xor(before, 8);
+    before += __shfl_xor(before, 16);
+    before += __shfl_xor(before, 32);
+    if (lane == 0) less[wave] = before;
+    __syncthreads();
+    int earlier = 0, own = 0;
+    for (int w = 0; w < WAVES; ++w) earlier += less[w];
+    if (threadIdx.x < MOST_ROWS) {
+        int v[WAVES];
 #pragma unroll
-        for (int r = 0; r < EACH; ++r) {
-            const int i = begin + 64 * r + lane;
-            if (r >= rounds || i >= n) continue;
-            const int to = seen[wave][key[r] >> shift & mask] + rank[r];
-            if (pass == passes - 1) {
-                keys_out[to] = key[r];
-                at_out[to] = from[r];
-            } else {
-                keys[to] = key[r];
-                at[to] = (unsigned short)from[r];
+        for (int w = 0; w < WAVES; ++w) v[w] = seen[w][threadIdx.x];
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            seen[w][threadIdx.x] = own;
+            own += v[w];
+        }
+        const unsigned long long m = __ballot(own > 0);
+        if (lane == 0) present[wave] = m;
+    }
+    const int base = earlier + block_exclusive<1024>(own, part);
+    if (threadIdx.x < MOST_ROWS) {
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) seen[w][threadIdx.x] += base;
+    }
+    if (threadIdx.x == 1023) part[0] = base;               // behind the last row of this range
+    __syncthreads();
+    const int end = part[0];
+    if (end > earlier)
+        each_round([&](int at, int id) {
+            const bool mine = id >= first && id < first + count;
+            if (!__ballot(mine)) return;
+            const int to = place_in_wave(id - first, bits, mine, lane, seen[wave]);
+            if (mine) {
+                keys_out[to] = id;
+                at_out[to] = at;
             }
-        }
-        if (pass == passes - 1) break;
-        __syncthreads();
-#pragma unroll
-        for (int r = 0; r < EACH; ++r) {
-            const int i = begin + 64 * r + lane;
-            if (r >= rounds || i >= n) continue;
-            key[r] = keys[i];
-            from[r] = at[i];
-        }
+        });
+    if (blockIdx.x == gridDim.x - 1)                       // positions that are in no row
+        for (int i = end + threadIdx.x; i < n; i += 1024) keys_out[i] = c.rows;
+    if constexpr (CLEAR) {
+        const int log = lanes_log<GT>(c.dim), sub = threadIdx.x & ((1 << log) - 1);
+        for (int r = threadIdx.x >> log; r < count; r += 1024 >> log)
+            if (!(present[r >> 6] >> (r & 63) & 1)) clear_row<GT>(c, first + r, sub, 1 << log);
     }
 }
 
@@ -204,7 +235,7 @@ __global__ __launch_bounds__(1024) void k_sort_one(const int *__restrict__ ids, 
 // FIRST: keys come from the tokens, and a position is its own place; workgroups behind the counting ones clear.
 template <bool FIRST, int GT>
 __global__ __launch_bounds__(256) void k_sort_count(const int *__restrict__ keys, int n, int padding, int shift, int bits, int blocks, int *__restrict__ count,
-                                                    Clear c)
+                                                    int *__restrict__ joins, Clear c)
 {
     __shared__ int s[RANGE / 32];
     static_assert(RANGE / 32 >= 1 << MAX_BITS, "room for the counts");
@@ -212,6 +243,7 @@ __global__ __launch_bounds__(256) void k_sort_count(const int *__restrict__ keys
         clear_unnamed<GT, 256>(c, keys, n, padding, blockIdx.x - blocks, gridDim.x - blocks, reinterpret_cast<unsigned *>(s));
         return;
     }
+    if (FIRST && blockIdx.x == 0 && threadIdx.x < 2) joins[threadIdx.x] = 0;
     for (int d = threadIdx.x; d < 1 << bits; d += 256) s[d] = 0;
     __syncthreads();
     const int begin = blockIdx.x * SORT;
@@ -220,7 +252,11 @@ __global__ __launch_bounds__(256) void k_sort_count(const int *__restrict__ keys
         atomicAdd(&s[k >> shift & ((1 << bits) - 1)], 1);
     }
     __syncthreads();
-    for (int d = threadIdx.x; d < 1 << bits; d += 256) count[(int64_t)d * blocks + blockIdx.x] = s[d];
+    for (int d = threadIdx.x; d < 1 << MAX_BITS; d += 256) {
+        const int v = d < 1 << bits ? s[d] : 0;
+        if (blocks <= BASES) count[((int)blockIdx.x << MAX_BITS) + d] = v;       // workgroup by workgroup: each of them reads all
+        else if (d < 1 << bits) count[(int64_t)d * blocks + blockIdx.x] = v;     // digit by digit: to be scanned
+    }
 }
 
 // SCANNED: `count` holds the places where each workgroup's digits begin; otherwise the counts.  A wave takes a quarter of the workgroup's
@@ -246,18 +282,22 @@ __global__ __launch_bounds__(256) void k_sort_place(const int *__restrict__ keys
         }
         __syncthreads();
     } else {
-        int all[DIGITS], sum = 0;
+        static_assert(DIGITS == 2, "two counts to a load");
+        int all[DIGITS] = {};
+        for (int b = 0; b < blocks; b += 8) {
+            int2 v[8];
 #pragma unroll
-        for (int e = 0; e < DIGITS; ++e) {
-            const int d = threadIdx.x * DIGITS + e;
-            all[e] = 0;
-            for (int b = 0; d < 1 << bits && b < blocks; ++b) {
-                const int v = count[(int64_t)d * blocks + b];
-                if (b < (int)blockIdx.x) base[e] += v;
-                all[e] += v;
+            for (int i = 0; i < 8; ++i) v[i] = reinterpret_cast<const int2 *>(count)[(min(b + i, blocks - 1) << (MAX_BITS - 1)) + threadIdx.x];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool is = b + i < blocks, before = b + i < (int)blockIdx.x;
+                all[0] += is ? v[i].x : 0;
+                all[1] += is ? v[i].y : 0;
+                base[0] += before ? v[i].x : 0;
+                base[1] += before ? v[i].y : 0;
             }
-            sum += all[e];
         }
+        const int sum = all[0] + all[1];
         int smaller = block_exclusive<256>(sum, part);
 #pragma unroll
         for (int e = 0; e < DIGITS; ++e) {
@@ -296,11 +336,10 @@ __global__ __launch_bounds__(256) void k_sort_place(const int *__restrict__ keys
 }
 
 // ------------------------------------------------------------------ sums
-constexpr int TILE = 64;                                   // positions per tile, one to a lane
-constexpr int CHUNK = 512;                                 // columns per wave, eight to a lane
+constexpr int MAX_TILE = 64;                               // positions per tile, at most one to a lane
 
 struct Grad {
-    int n, rows, dim, accumulate;
+    int n, rows, dim, accumulate, tile;
     const int *keys, *at;
     const void *dY;
     int64_t ldy;
@@ -308,7 +347,17 @@ struct Grad {
     int64_t lde;
     float factor;
     float *head, *tail;                                    // of each tile, dim: the part of a row that began before it, of one that goes on behind it
+    int *joins;                                            // Joins
 };
+
+// Tiles with a row that begins in them and goes on behind them, in any order: two counts, those whose row has few parts from 2 on, the others from the end.
+constexpr int MANY = 32;                                   // parts
+__device__ __forceinline__ void note_join(const Grad &g, int tile, int row)
+{
+    const int64_t far = ((int64_t)tile + 1 + MANY) * g.tile;
+    if (far < g.n && g.keys[far] == row) g.joins[2 + (g.n - 1) / g.tile - atomicAdd(g.joins + 1, 1)] = tile;
+    else g.joins[2 + atomicAdd(g.joins, 1)] = tile;
+}
 
 template <int GT>
 __device__ __forceinline__ void put_element(const Grad &g, int64_t at, float sum)
@@ -316,40 +365,39 @@ __device__ __forceinline__ void put_element(const Grad &g, int64_t at, float sum
     const float v = g.factor * sum;
     store_as<GT>(g.dE, at, g.accumulate ? element<GT>(g.dE, at) + v : v);
 }
-// Eight columns of row `row` of dE from column u.col on, without the first u.skip.
+// Four columns of row `row` of dE from column u.col on, without the first u.skip.
 template <int GT>
-__device__ __forceinline__ void put_row(const Grad &g, int row, Unit u, const float (&sum)[8])
+__device__ __forceinline__ void put_row(const Grad &g, int row, Unit u, const float (&sum)[4])
 {
-    typedef typename Bits<GT>::type B;
     const int64_t at = row * g.lde + u.col;
     if (u.skip == 0) {
-        float v[8];
-        B *p = static_cast<B *>(g.dE) + at;
+        float v[4];
+        typename Bits<GT>::type *p = static_cast<typename Bits<GT>::type *>(g.dE) + at;
         if (g.accumulate) {
-            Raw8<GT> r;
+            Raw4<GT> r;
             load_raw<GT>(r, p);
             widen_raw<GT>(r, v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += g.factor * sum[i];
+            for (int i = 0; i < 4; ++i) v[i] += g.factor * sum[i];
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = g.factor * sum[i];
+            for (int i = 0; i < 4; ++i) v[i] = g.factor * sum[i];
         }
-        store8<GT>(p, v);
+        store_row<GT>(p, v);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 1; i < 4; ++i)
             if (i >= u.skip) put_element<GT>(g, at + i, sum[i]);
     }
 }
 
-// One wave: the tile's positions, columns from `unit` of this lane on.
-template <int T, int GT>
+// One wave: the tile's positions, 256 J columns, four of each 256 to a lane.
+template <int T, int GT, int J>
 __device__ __forceinline__ void tile_sum(const Grad &g, int tile, int chunk, int lane)
 {
     constexpr int U = 8;                                   // rows of dY in flight
     typedef typename Bits<T>::type B;
-    const int p0 = tile * TILE, count = min(TILE, g.n - p0), p = min(p0 + lane, g.n - 1);
+    const int p0 = tile * g.tile, count = min(g.tile, g.n - p0), p = min(p0 + lane, g.n - 1);
     const int key = g.keys[p], at = g.at[p];
     const int before = p0 > 0 ? g.keys[p0 - 1] : -1, behind = p0 + count < g.n ? g.keys[p0 + count] : -1;
     const int next = __shfl_down(key, 1);
@@ -357,48 +405,60 @@ __device__ __forceinline__ void tile_sum(const Grad &g, int tile, int chunk, int
     const bool last = lane == count - 1;
     const unsigned long long ends = __ballot(lane < count && (last || next != key));
     const int valid = __popcll(__ballot(lane < count && key < g.rows));
-    const int unit = chunk * (CHUNK / 8) + lane;
-    const bool mine = 8 * unit < g.dim;
-    const Unit u = unit_of(mine ? unit : 0, g.dim);
-    float sum[8] = {};
+    bool mine[J];
+    Unit u[J];
+#pragma unroll
+    for (int q = 0; q < J; ++q) {
+        const int unit = (chunk * J + q) * 64 + lane;
+        mine[q] = 4 * unit < g.dim;
+        u[q] = unit_of<4>(mine[q] ? unit : 0, g.dim);
+    }
+    float sum[J][4] = {};
     for (int i = 0; i < valid; i += U) {
-        Raw8<T> r[U];
+        Raw4<T> r[U][J];
 #pragma unroll
         for (int j = 0; j < U; ++j) {
-            const int64_t row = rl(at, min(i + j, valid - 1));
-            load_raw<T>(r[j], static_cast<const B *>(g.dY) + row * g.ldy + u.col);
+            const B *row = static_cast<const B *>(g.dY) + rl(at, min(i + j, valid - 1)) * g.ldy;
+#pragma unroll
+            for (int q = 0; q < J; ++q) load_raw<T>(r[j][q], row + u[q].col);
         }
 #pragma unroll
         for (int j = 0; j < U; ++j) {
             if (i + j >= valid) break;
-            float v[8];
-            widen_raw<T>(r[j], v);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum[k] += v[k];
+            for (int q = 0; q < J; ++q) {
+                float v[4];
+                widen_raw<T>(r[j][q], v);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum[q][k] += v[k];
+            }
             if (ends >> (i + j) & 1) {
                 const int row = rl(key, i + j);
                 const bool began = row != before, goes_on = i + j == count - 1 && row == behind;
-                if (mine) {
-                    if (began && !goes_on) {
-                        put_row<GT>(g, row, u, sum);
-                    } else {
-                        float *to = (began ? g.tail : g.head) + (int64_t)tile * g.dim + u.col;
-                        *reinterpret_cast<v4f_e *>(to) = v4f{sum[0], sum[1], sum[2], sum[3]};      // what is there twice is the same
-                        *reinterpret_cast<v4f_e *>(to + 4) = v4f{sum[4], sum[5], sum[6], sum[7]};
-                    }
-                }
+                if (began && goes_on && chunk == 0 && lane == 0) note_join(g, tile, row);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
+                for (int q = 0; q < J; ++q) {
+                    if (mine[q]) {
+                        if (began && !goes_on) {
+                            put_row<GT>(g, row, u[q], sum[q]);
+                        } else {                           // columns that two lanes have are the same
+                            float *to = (began ? g.tail : g.head) + (int64_t)tile * g.dim + u[q].col;
+                            *reinterpret_cast<v4f_e *>(to) = v4f{sum[q][0], sum[q][1], sum[q][2], sum[q][3]};
+                        }
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) sum[q][k] = 0.0f;
+                }
             }
         }
     }
 }
 
-// Rows of less than eight columns: a wave per tile, a lane per column.
+// Rows of less than four columns: a wave per tile, a lane per column.
 template <int T, int GT>
 __device__ __forceinline__ void tile_sum_narrow(const Grad &g, int tile, int lane)
 {
-    const int p0 = tile * TILE, p1 = min(p0 + TILE, g.n);
+    const int p0 = tile * g.tile, p1 = min(p0 + g.tile, g.n);
     if (lane >= g.dim) return;
     const int before = p0 > 0 ? g.keys[p0 - 1] : -1, behind = p1 < g.n ? g.keys[p1] : -1;
     float sum = 0.0f;
@@ -410,11 +470,12 @@ __device__ __forceinline__ void tile_sum_narrow(const Grad &g, int tile, int lan
         const bool began = row != before, goes_on = p == p1 - 1 && row == behind;
         if (began && !goes_on) put_element<GT>(g, row * g.lde + lane, sum);
         else (began ? g.tail : g.head)[(int64_t)tile * g.dim + lane] = sum;
+        if (began && goes_on && lane == 0) note_join(g, tile, row);
         sum = 0.0f;
     }
 }
 
-template <int T, int GT>
+template <int T, int GT, int J>
 __global__ __launch_bounds__(256) void k_grad_sum(Grad g, int chunks, int64_t sums, int64_t all)
 {
     __shared__ unsigned long long empty[4];
@@ -423,83 +484,237 @@ __global__ __launch_bounds__(256) void k_grad_sum(Grad g, int chunks, int64_t su
         const int64_t w = b * 4 + wave;
         if (b * 4 >= sums) clear_absent<GT>(Clear{g.dE, g.lde, g.rows, g.dim}, g.keys, g.n, (b - (sums + 3) / 4) * 256, empty);
         else if (w >= sums) continue;
-        else if (g.dim < 8) tile_sum_narrow<T, GT>(g, (int)w, lane);
-        else tile_sum<T, GT>(g, (int)(w / chunks), (int)(w % chunks), lane);
+        else if (g.dim < 4) tile_sum_narrow<T, GT>(g, (int)w, lane);
+        else tile_sum<T, GT, J>(g, (int)(w / chunks), (int)(w % chunks), lane);
     }
 }
 
-// A row that begins in a tile and goes on behind it: its parts in order, a quarter of them to a wave, whose sums meet in LDS.  A workgroup per tile
-// and chunk of columns; most have nothing to do.
-template <int GT>
-__global__ __launch_bounds__(256) void k_grad_join(Grad g, int tiles, int chunks)
+// A row that begins in a tile and goes on behind it: its parts in order.  Few parts: a workgroup takes the tile and 2048 columns, a wave 256 of them.  Many:
+// the tile and 256 columns, a wave takes an eighth of the parts, and their sums meet in LDS.
+// (Without the lists, a workgroup to every tile and 256 columns took 25 us for 16384 tokens of 4096 columns, most to find nothing.)
+constexpr int JOIN = 8;                                    // waves
+struct Part {                                              // a lane's columns
+    bool mine;
+    Unit u;
+};
+__device__ __forceinline__ Part part_of(const Grad &g, int quad, int lane)
 {
-    constexpr int U = 8;                                   // parts in flight
-    __shared__ float meet[3][64][8];
+    const int unit = quad * 64 + lane;
+    Part p;
+    p.mine = g.dim < 4 ? lane < g.dim && quad == 0 : 4 * unit < g.dim;
+    p.u = g.dim < 4 ? Unit{p.mine ? lane : 0, 0} : unit_of<4>(p.mine ? unit : 0, g.dim);
+    return p;
+}
+// Parts from .. to - 1.
+template <int U>                                           // in flight
+__device__ __forceinline__ void add_parts(const Grad &g, const float *head, int from, int to, float (&sum)[4])
+{
+    if (g.dim < 4) {
+        for (int i = from; i < to; ++i) sum[0] += head[(int64_t)i * g.dim];
+        return;
+    }
+    for (int i = from; i < to; i += U) {
+        Raw4<F32> r[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) load_raw<F32>(r[j], head + (int64_t)min(i + j, to - 1) * g.dim);
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum[k] += i + j < to ? r[j].a[k] : 0.0f;
+    }
+}
+template <int GT>
+__device__ __forceinline__ void put_joined(const Grad &g, int tile, int row, const Part &p, float (&sum)[4])
+{
+    if (!p.mine) return;
+    const float *const tail = g.tail + (int64_t)tile * g.dim + p.u.col;
+    if (g.dim < 4) {
+        put_element<GT>(g, row * g.lde + p.u.col, sum[0] + tail[0]);
+    } else {
+        const v4f v = *reinterpret_cast<const v4f_e *>(tail);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum[k] += v[k];
+        put_row<GT>(g, row, p.u, sum);
+    }
+}
+template <int GT>
+__global__ __launch_bounds__(64 * JOIN) void k_grad_join(Grad g, int tiles, int groups, int quads)
+{
+    __shared__ float meet[JOIN - 1][4][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t all = (int64_t)tiles * chunks;
+    const int64_t few = (int64_t)g.joins[0] * groups, all = few + (int64_t)g.joins[1] * quads;
     for (int64_t w = blockIdx.x; w < all; w += gridDim.x) {
-        const int tile = (int)(w / chunks), p0 = tile * TILE, p1 = p0 + TILE;
-        if (p1 >= g.n) continue;
-        const int row = g.keys[p1 - 1];
-        if (row >= g.rows || g.keys[p1] != row || (p0 > 0 && g.keys[p0 - 1] == row)) continue;
+        const bool many = w < all - few;                   // the long ones first
+        const int64_t v = many ? w : w - (all - few);
+        const int tile = many ? g.joins[2 + tiles - 1 - v / quads] : g.joins[2 + v / groups], row = g.keys[(tile + 1) * g.tile];
         int more = 0;                                      // tiles behind it that begin with the row
         for (;;) {
             const int t = tile + 1 + more + lane;
-            const int same = __builtin_ctzll(~__ballot(t < tiles && g.keys[t < tiles ? t * TILE : 0] == row) | (1ull << 63));
+            const int same = __builtin_ctzll(~__ballot(t < tiles && g.keys[t < tiles ? t * g.tile : 0] == row) | (1ull << 63));
             more += same;                                  // at most 63 of a round
             if (same < 63) break;
         }
-        const bool narrow = g.dim < 8;
-        const int unit = (int)(w % chunks) * (CHUNK / 8) + lane;
-        const bool mine = narrow ? lane < g.dim : 8 * unit < g.dim;
-        const Unit u = narrow ? Unit{mine ? lane : 0, 0} : unit_of(mine ? unit : 0, g.dim);
-        const int each = (more + 3) / 4, from = min(wave * each, more), to = min(from + each, more);
-        const float *const head = g.head + (int64_t)(tile + 1) * g.dim + u.col;
-        float sum[8] = {};
-        if (narrow) {
-            for (int i = from; i < to; ++i) sum[0] += head[(int64_t)i * g.dim];
-        } else {
-            for (int i = from; i < to; i += U) {
-                Raw8<F32> r[U];
-#pragma unroll
-                for (int j = 0; j < U; ++j) load_raw<F32>(r[j], head + (int64_t)min(i + j, to - 1) * g.dim);
-#pragma unroll
-                for (int j = 0; j < U; ++j) {
-                    if (i + j >= to) break;
-                    float v[8];
-                    widen_raw<F32>(r[j], v);
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) sum[k] += v[k];
-                }
-            }
+        const Part p = part_of(g, (int)(many ? v % quads : v % groups * JOIN + wave), lane);
+        const float *const head = g.head + (int64_t)(tile + 1) * g.dim + p.u.col;
+        float sum[4] = {};
+        if (!many) {
+            if (p.mine) add_parts<4>(g, head, 0, more, sum);
+            put_joined<GT>(g, tile, row, p, sum);
+            continue;
         }
-        __syncthreads();                                   // the last row's sums have been read
+        const int each = (more + JOIN - 1) / JOIN, from = min(wave * each, more);
+        if (p.mine) add_parts<16>(g, head, from, min(from + each, more), sum);
+        __syncthreads();                                   // the last sums have been read
         if (wave > 0) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) meet[wave - 1][lane][k] = sum[k];
+            for (int k = 0; k < 4; ++k) meet[wave - 1][k][lane] = sum[k];
         }
         __syncthreads();
-        if (wave > 0 || !mine) continue;
-        for (int q = 0; q < 3; ++q)
+        if (wave == 0) {
+            for (int o = 0; o < JOIN - 1; ++o)
 #pragma unroll
-            for (int k = 0; k < 8; ++k) sum[k] += meet[q][lane][k];
-        const float *const tail = g.tail + (int64_t)tile * g.dim + u.col;
-        if (narrow) {
-            put_element<GT>(g, row * g.lde + lane, sum[0] + tail[0]);
-        } else {
-            float v[8];
-            Raw8<F32> r;
-            load_raw<F32>(r, tail);
-            widen_raw<F32>(r, v);
-#pragma unroll
-            for (int k = 0; k < 8; ++k) sum[k] += v[k];
-            put_row<GT>(g, row, u, sum);
+                for (int k = 0; k < 4; ++k) sum[k] += meet[o][k][lane];
+            put_joined<GT>(g, tile, row, p, sum);
         }
+    }
+}
+
+// 256 J columns to a wave: a wave's work is about J + 1 for each position.
+int quads_per_lane(int64_t dim)
+{
+    int best = 1;
+    int64_t least = INT64_MAX;
+    for (int j = 1; j <= 3; ++j) {
+        const int64_t cost = (dim + 256 * j - 1) / (256 * j) * (j + 1);
+        if (cost < least) {
+            least = cost;
+            best = j;
+        }
+    }
+    return best;
+}
+// Positions to a tile: as many as leave 4096 waves, but 16 to 64 (up to FEW tokens 8): one row's parts are added up by one compute unit for each 256
+// columns.  16000 tokens of 512 columns, nine tenths of them one: tiles of 8 join in 34 us and add up in 10.
+constexpr int FEW = 2048;
+int tile_of(int64_t n, int64_t dim)
+{
+    const int64_t j = 256 * quads_per_lane(dim), chunks = (dim + j - 1) / j;
+    int tile = MAX_TILE;
+    while (tile > (n <= FEW ? 8 : 16) && n * chunks < (int64_t)tile * 4096) tile /= 2;
+    return tile;
+}
+// As many tiles as n or fewer tokens are cut into at most, so that a workspace for n is one for fewer.
+int64_t most_tiles(int64_t n, int64_t dim)
+{
+    const int64_t j = 256 * quads_per_lane(dim), chunks = (dim + j - 1) / j, few = std::max((std::min(n, (int64_t)FEW) + 7) / 8, std::min((n + 15) / 16, 8192 / std::max(chunks, (int64_t)1) + 1));
+    return std::max((n + MAX_TILE - 1) / MAX_TILE, few);
+}
+
+// ------------------------------------------------------------------ few tokens
+// Up to SMALL tokens of 4 MB in all: one launch.  A workgroup owns rows and 256 J of the columns, finds its tokens and their order as k_sort_ranges does, adds them
+// up, a row to a wave (rows of more than LONG tokens: a sixteenth of them to a wave, whose sums meet in LDS), and clears the other rows.
+// 512 tokens of 1024 columns, 8192 rows, f32: 10 us; by three launches 22.
+constexpr int SMALL = 1024, LONG = 64;
+
+template <int T, int GT>
+__global__ __launch_bounds__(1024) void k_grad_few(Grad g, const int *__restrict__ ids, int padding, int per, int bits, int width)
+{
+    constexpr int WAVES = 16, U = 8;
+    __shared__ int seen[WAVES][MOST_ROWS];
+    __shared__ int key[SMALL], at[SMALL], start[SMALL + 1], part[WAVES];
+    __shared__ unsigned long long present[MOST_ROWS / 64];
+    __shared__ float meet[WAVES][4][64];
+    typedef typename Bits<T>::type B;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int first = blockIdx.x * per, count = min(per, g.rows - first), col0 = blockIdx.y * width, cols = min(width, g.dim - col0);
+    const int id = (int)threadIdx.x < g.n ? ids[threadIdx.x] : -1;
+    for (int d = threadIdx.x; d < WAVES * MOST_ROWS; d += 1024) (&seen[0][0])[d] = 0;
+    __syncthreads();
+    const bool mine = id >= first && id < first + count && id != padding;
+    int rank = 0;
+    if (__ballot(mine)) rank = place_in_wave(id - first, bits, mine, lane, seen[wave]);
+    __syncthreads();
+    int own = 0;
+    if (threadIdx.x < MOST_ROWS) {
+        int v[WAVES];
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) v[w] = seen[w][threadIdx.x];
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            seen[w][threadIdx.x] = own;
+            own += v[w];
+        }
+        const unsigned long long m = __ballot(own > 0);
+        if (lane == 0) present[wave] = m;
+    }
+    const int base = block_exclusive<1024>(own, part);
+    const int nth = block_exclusive<1024>(own > 0, part);  // rows before this one that have tokens
+    if (own > 0) start[nth] = base;
+    if (threadIdx.x < MOST_ROWS) {
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) seen[w][threadIdx.x] += base;
+    }
+    if (threadIdx.x == 1023) {
+        start[nth] = base;                                 // behind the last row
+        part[0] = nth;
+    }
+    __syncthreads();
+    const int segments = part[0];
+    if (mine) {
+        const int to = seen[wave][id - first] + rank;
+        key[to] = id;
+        at[to] = threadIdx.x;
+    }
+    __syncthreads();
+    auto sum_up = [&](int from, int to, int col, float (&sum)[4]) {
+        for (int i = from; i < to; i += U) {
+            Raw4<T> r[U];
+#pragma unroll
+            for (int j = 0; j < U; ++j) load_raw<T>(r[j], static_cast<const B *>(g.dY) + at[min(i + j, to - 1)] * g.ldy + col);
+#pragma unroll
+            for (int j = 0; j < U; ++j) {
+                float v[4];
+                widen_raw<T>(r[j], v);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum[k] += i + j < to ? v[k] : 0.0f;
+            }
+        }
+    };
+    const int quads = (cols + 255) / 256;
+    for (int i = wave; i < segments * quads; i += WAVES) {
+        const int s = i / quads, from = start[s], to = start[s + 1], c = col0 + (i % quads * 64 + lane) * 4;
+        if (to - from > LONG || c >= col0 + cols) continue;
+        const int col = min(c, g.dim - 4);
+        float sum[4] = {};
+        sum_up(from, to, col, sum);
+        put_row<GT>(g, key[from], Unit{col, c - col}, sum);
+    }
+    for (int i = 0; i < segments * quads; ++i) {
+        const int s = i / quads, from = start[s], to = start[s + 1], c = col0 + (i % quads * 64 + lane) * 4;
+        if (to - from <= LONG) continue;                   // (the same for all waves)
+        const int each = (to - from + WAVES - 1) / WAVES, begin = from + wave * each, col = min(c, g.dim - 4);
+        float sum[4] = {};
+        sum_up(begin, min(begin + each, to), col, sum);
+        __syncthreads();                                   // the last sums have been read
+#pragma unroll
+        for (int k = 0; k < 4; ++k) meet[wave][k][lane] = sum[k];
+        __syncthreads();
+        if (wave > 0 || c >= col0 + cols) continue;
+        for (int o = 1; o < WAVES; ++o)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum[k] += meet[o][k][lane];
+        put_row<GT>(g, key[from], Unit{col, c - col}, sum);
+    }
+    if (!g.accumulate) {
+        const Clear c = {static_cast<typename Bits<GT>::type *>(g.dE) + col0, g.lde, g.rows, cols};
+        const int log = lanes_log<GT>(cols), sub = threadIdx.x & ((1 << log) - 1);
+        for (int r = threadIdx.x >> log; r < count; r += 1024 >> log)
+            if (!(present[r >> 6] >> (r & 63) & 1)) clear_row<GT>(c, first + r, sub, 1 << log);
     }
 }
 
 struct Space {
-    int *keys[2], *at[2], *count, *scan;
+    int *keys[2], *at[2], *count, *scan, *joins;
     float *head, *tail;
     size_t bytes;
 };
@@ -512,7 +727,7 @@ Space carve_grad(void *base, int64_t n, int64_t dim)
         used += align256(bytes + 1);
         return q;
     };
-    const int64_t blocks = (n + SORT - 1) / SORT, tiles = (n + TILE - 1) / TILE, counts = blocks << MAX_BITS;
+    const int64_t blocks = (n + SORT - 1) / SORT, tiles = most_tiles(n, dim), counts = blocks << MAX_BITS;
     Space w;
     for (int i = 0; i < 2; ++i) {
         w.keys[i] = reinterpret_cast<int *>(take((size_t)n * 4));
@@ -520,6 +735,7 @@ Space carve_grad(void *base, int64_t n, int64_t dim)
     }
     w.count = reinterpret_cast<int *>(take((size_t)counts * 4));
     w.scan = reinterpret_cast<int *>(take(scan_tmp_ints(counts) * 4));
+    w.joins = reinterpret_cast<int *>(take((size_t)(tiles + 2) * 4));
     w.head = reinterpret_cast<float *>(take((size_t)tiles * (size_t)dim * 4));
     w.tail = reinterpret_cast<float *>(take((size_t)tiles * (size_t)dim * 4));
     w.bytes = used;
@@ -528,31 +744,44 @@ Space carve_grad(void *base, int64_t n, int64_t dim)
 
 unsigned at_most(int64_t blocks, int64_t most) { return (unsigned)(blocks < most ? blocks : most); }
 
-// BESIDE: rows without a token are cleared in the launch of the sort's first step, by workgroups that read all tokens.  More than 64 K tokens
-// take these longer than the search in the sorted ones.
+// Rows without a token are cleared by the workgroups that sort, or, with up to NEAR tokens, by others of the first launch that read all tokens; more
+// tokens take these longer than the search in the sorted ones.
 template <int T, int GT>
 hipError_t run(int n, int rows, int dim, const int *ids, int padding, float factor, const void *dY, int64_t ldy, void *dE, int64_t lde, int accumulate,
                const Space &w, hipStream_t s)
 {
     const Clear c = {dE, lde, rows, dim};
-    const bool beside = !accumulate && n > 0 && n <= 65536;
-    const int blocks = (n + SORT - 1) / SORT;
-    int bits = 1;
-    while (rows >> bits) ++bits;                           // keys are 0 .. rows
-    const int passes = (bits + MAX_BITS - 1) / MAX_BITS, digit = (bits + passes - 1) / passes;
+    const bool beside = !accumulate && n > 0 && n <= NEAR;
     const int *keys = ids, *at = nullptr;
-    if (n > 0 && n <= ONE) {
-        const unsigned clear = beside ? at_most(((int64_t)rows + 15) / 16, 255) : 0;
-        if (beside) PSK_LAUNCH((k_sort_one<GT, true>), dim3(1 + clear), dim3(1024), 0, s, ids, n, padding, digit, passes, w.keys[0], w.at[0], c);
-        else PSK_LAUNCH((k_sort_one<GT, false>), dim3(1), dim3(1024), 0, s, ids, n, padding, digit, passes, w.keys[0], w.at[0], c);
+    if (n > 0 && n <= SMALL && dim >= 4 && rows <= RANGES * MOST_ROWS && (int64_t)n * dim * (T == F32 ? 4 : 2) <= 4 << 20) {
+        // as many columns to a workgroup as leave about 512 of them
+        const int quads = (dim + 255) / 256, split = quads < 4 ? quads : 4, width = (quads + split - 1) / split * 256, groups = (dim + width - 1) / width;
+        int per = (rows * groups + 511) / 512, bits = 1;
+        if (per > MOST_ROWS) per = MOST_ROWS;
+        while ((per - 1) >> bits) ++bits;
+        const Grad g = {n, rows, dim, accumulate, 0, nullptr, nullptr, dY, ldy, dE, lde, factor, nullptr, nullptr, nullptr};
+        PSK_LAUNCH((k_grad_few<T, GT>), dim3((rows + per - 1) / per, groups), dim3(1024), 0, s, g, ids, padding, per, bits, width);
+        return take_launch_status();
+    }
+    int per = (rows + 255) / 256;
+    if (per > MOST_ROWS) per = MOST_ROWS;
+    if (n > 0 && n <= NEAR && rows <= RANGES * MOST_ROWS) {
+        int bits = 1;
+        while ((per - 1) >> bits) ++bits;
+        const auto sort = beside ? k_sort_ranges<GT, true> : k_sort_ranges<GT, false>;
+        PSK_LAUNCH(sort, dim3((rows + per - 1) / per), dim3(1024), 0, s, ids, n, padding, per, bits, w.keys[0], w.at[0], w.joins, c);
         keys = w.keys[0];
         at = w.at[0];
     } else {
+        const int blocks = (n + SORT - 1) / SORT;
+        int bits = 1;
+        while (rows >> bits) ++bits;                       // keys are 0 .. rows
+        const int passes = (bits + MAX_BITS - 1) / MAX_BITS, digit = (bits + passes - 1) / passes;
         for (int pass = 0; n > 0 && pass < passes; ++pass) {
             const int shift = pass * digit;
             const unsigned clear = beside && pass == 0 ? at_most(((int64_t)rows + 3) / 4, 1024) : 0;
-            if (pass == 0) PSK_LAUNCH((k_sort_count<true, GT>), dim3(blocks + clear), dim3(256), 0, s, keys, n, padding, shift, digit, blocks, w.count, c);
-            else PSK_LAUNCH((k_sort_count<false, GT>), dim3(blocks), dim3(256), 0, s, keys, n, padding, shift, digit, blocks, w.count, c);
+            if (pass == 0) PSK_LAUNCH((k_sort_count<true, GT>), dim3(blocks + clear), dim3(256), 0, s, keys, n, padding, shift, digit, blocks, w.count, w.joins, c);
+            else PSK_LAUNCH((k_sort_count<false, GT>), dim3(blocks), dim3(256), 0, s, keys, n, padding, shift, digit, blocks, w.count, w.joins, c);
             const bool scan = blocks > BASES;
             if (scan) {
                 const hipError_t e = launch_exclusive_scan(w.count, w.count, (int64_t)blocks << digit, w.scan, s);
@@ -565,11 +794,12 @@ hipError_t run(int n, int rows, int dim, const int *ids, int padding, float fact
             at = a;
         }
     }
-    const Grad g = {n, rows, dim, accumulate, keys, at, dY, ldy, dE, lde, factor, w.head, w.tail};
-    const int tiles = (n + TILE - 1) / TILE, chunks = dim < 8 ? 1 : (dim + CHUNK - 1) / CHUNK;
+    const Grad g = {n, rows, dim, accumulate, tile_of(n, dim), keys, at, dY, ldy, dE, lde, factor, w.head, w.tail, w.joins};
+    const int tiles = (n + g.tile - 1) / g.tile, j = quads_per_lane(dim), chunks = (dim + 256 * j - 1) / (256 * j), quads = (dim + 255) / 256, groups = (quads + JOIN - 1) / JOIN;
     const int64_t sums = (int64_t)tiles * chunks, all = (sums + 3) / 4 + (accumulate || beside ? 0 : ((int64_t)rows + 255) / 256);
-    PSK_LAUNCH((k_grad_sum<T, GT>), dim3(at_most(all, 65536)), dim3(256), 0, s, g, chunks, sums, all);
-    if (tiles > 1) PSK_LAUNCH((k_grad_join<GT>), dim3(at_most(sums, 65536)), dim3(256), 0, s, g, tiles, chunks);
+    const auto sum = j == 1 ? k_grad_sum<T, GT, 1> : (j == 2 ? k_grad_sum<T, GT, 2> : k_grad_sum<T, GT, 3>);
+    PSK_LAUNCH(sum, dim3(at_most(all, 65536)), dim3(256), 0, s, g, chunks, sums, all);
+    if (tiles > 1) PSK_LAUNCH((k_grad_join<GT>), dim3(at_most((int64_t)tiles * groups, 1024)), dim3(64 * JOIN), 0, s, g, tiles, groups, quads);
     return take_launch_status();
 }
 

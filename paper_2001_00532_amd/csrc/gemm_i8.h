@@ -9,9 +9,6 @@
 
 namespace psk {
 
-typedef int v4i_e __attribute__((ext_vector_type(4), aligned(4)));
-typedef unsigned short v4s __attribute__((ext_vector_type(4)));
-typedef unsigned short v4s_u __attribute__((ext_vector_type(4), aligned(2)));
 
 // Eight elements from column k on, zeros from column `cols` on, of a row that has eight: asked for by row_load and had by row_get.  Where the row ends
 // among them, its last eight are loaded and moved.

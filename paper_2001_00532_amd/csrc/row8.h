@@ -1,4 +1,4 @@
-// Rows of any of the types by eight elements, at any address.
+// Rows of any of the types by eight or four elements, at any address.
 #pragma once
 #include "psk_internal.h"
 #include "psk_mfma.h"
@@ -9,6 +9,10 @@ constexpr int I8 = 3;                                      // codes of psk_i8; n
 
 typedef int8_t v8i8 __attribute__((ext_vector_type(8)));
 typedef int8_t v8i8_u __attribute__((ext_vector_type(8), aligned(1)));
+typedef int8_t v4i8 __attribute__((ext_vector_type(4)));
+typedef int8_t v4i8_u __attribute__((ext_vector_type(4), aligned(1)));
+typedef unsigned short v4s __attribute__((ext_vector_type(4)));
+typedef unsigned short v4s_u __attribute__((ext_vector_type(4), aligned(2)));
 typedef unsigned short v8s __attribute__((ext_vector_type(8)));
 typedef unsigned short v8s_u __attribute__((ext_vector_type(8), aligned(2)));
 
@@ -68,6 +72,49 @@ __device__ __forceinline__ void store8(typename Bits<T>::type *p, const float (&
         for (int i = 0; i < 8; ++i) r[i] = narrow<T>(v[i]);
         *reinterpret_cast<v8s_u *>(p) = r;
     }
+}
+
+// Four elements: of 32 bits a wave's load or store is then one piece of 1 KB, where eight to a lane would be two with gaps.
+template <int T> struct Raw4;
+template <> struct Raw4<F32> { v4f a; };
+template <> struct Raw4<F16> { v4s a; };
+template <> struct Raw4<BF16> { v4s a; };
+template <> struct Raw4<I8> { v4i8 a; };
+template <int T>
+__device__ __forceinline__ void load_raw(Raw4<T> &r, const typename Bits<T>::type *p)
+{
+    if constexpr (T == F32) r.a = *reinterpret_cast<const v4f_e *>(p);
+    else if constexpr (T == I8) r.a = *reinterpret_cast<const v4i8_u *>(p);
+    else r.a = *reinterpret_cast<const v4s_u *>(p);
+}
+template <int T>
+__device__ __forceinline__ void widen_raw(const Raw4<T> &r, float (&v)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (T == F32) v[i] = r.a[i];
+        else if constexpr (T == I8) v[i] = (float)r.a[i];
+        else v[i] = widen<T>(r.a[i]);
+    }
+}
+template <int T>
+__device__ __forceinline__ void store_row(typename Bits<T>::type *p, const float (&v)[4])
+{
+    if constexpr (T == F32) *reinterpret_cast<v4f_e *>(p) = v4f{v[0], v[1], v[2], v[3]};
+    else *reinterpret_cast<v4s_u *>(p) = v4s{narrow<T>(v[0]), narrow<T>(v[1]), narrow<T>(v[2]), narrow<T>(v[3])};
+}
+template <int T>
+__device__ __forceinline__ void store_row(typename Bits<T>::type *p, const float (&v)[8]) { store8<T>(p, v); }
+template <int T, int W> struct RawOf { typedef Raw8<T> type; };
+template <int T> struct RawOf<T, 4> { typedef Raw4<T> type; };
+
+// Columns of a row go by W; the last W are the row's last, so some of them may be among those before too (`skip` of them).
+struct Unit { int col, skip; };
+template <int W>
+__device__ __forceinline__ Unit unit_of(int unit, int dim)
+{
+    const int at = W * unit, col = min(at, dim - W);
+    return Unit{col, at - col};
 }
 
 }  // namespace psk
