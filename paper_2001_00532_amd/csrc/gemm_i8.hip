@@ -5,6 +5,15 @@
 // bytes, row by row) meets each bank once.  One barrier a step: behind it the step's operands are there and the stage before is free.
 #include "gemm_i8.h"
 
+#ifndef BIG_M
+#define BIG_M 32
+#endif
+#ifndef BIG_WR
+#define BIG_WR 4
+#endif
+#ifndef MID_M
+#define MID_M 16
+#endif
 namespace psk {
 namespace {
 
@@ -23,35 +32,38 @@ __device__ __forceinline__ void step_barrier()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory");
 }
 
-template <int YT>
-__device__ __forceinline__ void put4(void *Y, int64_t at, const float (&v)[4], int count)
-{
-    if (count >= 4) {
-        if constexpr (YT == F32) {
-            *reinterpret_cast<v4f_e *>(static_cast<float *>(Y) + at) = v4f{v[0], v[1], v[2], v[3]};
-        } else {
-            *reinterpret_cast<v4s_u *>(static_cast<unsigned short *>(Y) + at) = v4s{narrow<YT>(v[0]), narrow<YT>(v[1]), narrow<YT>(v[2]), narrow<YT>(v[3])};
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 3; ++i)
-            if (i < count) store_as<YT>(Y, at + i, v[i]);
-    }
-}
+typedef int v16i __attribute__((ext_vector_type(16)));
 
-// BT tokens x BR channels by WT x WR waves, S stages.
-template <int YT, int BT, int BR, int WT, int WR, int S>
+// One matrix instruction: M channels x M tokens over 1024 / M columns, 16 bytes of a row to a lane.
+template <int M> struct Product;
+template <> struct Product<16> {
+    typedef v4i Sum;
+    static __device__ __forceinline__ Sum go(v4i a, v4i x, Sum c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, x, c, 0, 0, 0); }
+};
+template <> struct Product<32> {
+    typedef v16i Sum;
+    static __device__ __forceinline__ Sum go(v4i a, v4i x, Sum c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, x, c, 0, 0, 0); }
+};
+
+// By how much the eight pieces of a row are turned.  A read of 16 bytes a lane goes through the banks by sixteen lanes, 0-3, 12-15, 20-23 and 24-27 first: rows of
+// their own in an instruction of 32, four rows and three of the next piece in one of 16.
+template <int M>
+__device__ __forceinline__ int turn(int row) { return M == 32 ? (row & 7) ^ (row >> 4 & 1) : row & 7; }
+
+// BT tokens x BR channels by WT x WR waves, S stages, instructions of M x M.
+template <int YT, int BT, int BR, int WT, int WR, int S, int M>
 __global__ __launch_bounds__(64 * WT * WR) void k_gemm_i8(int rows, int cols, int n, const int8_t *A, int64_t lda, const int8_t *X, int64_t ldx, Finish f, void *Y,
                                                           int64_t ldy, unsigned tiles_r, unsigned tiles)
 {
-    constexpr int NW = WT * WR, LOADS = (BT + BR) / 8 / NW, TT = BT / WT / 16, TR = BR / WR / 16, STAGE = (BT + BR) * STEP;
+    constexpr int NW = WT * WR, LOADS = (BT + BR) / 8 / NW, TT = BT / WT / M, TR = BR / WR / M, STAGE = (BT + BR) * STEP, PARTS = M / 8;
     static_assert((BT + BR) % (8 * NW) == 0, "whole loads");
+    typedef typename Product<M>::Sum Sum;
     __shared__ __attribute__((aligned(1024))) int8_t lds[S * STAGE];
     const unsigned tile = blockIdx.y * gridDim.x + blockIdx.x;
     if (tile >= tiles) return;
     const int t0 = (int)(tile / tiles_r) * BT, r0 = (int)(tile % tiles_r) * BR;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wt = wave / WR, wr = wave % WR;
-    const int blocks = (cols + STEP - 1) / STEP, most = ((cols + 15) & ~15) - 16 - (blocks - 1) * STEP;      // the last piece of the last step
+    const int blocks = (cols + STEP - 1) / STEP, left = cols - (blocks - 1) * STEP, most = ((left + 15) & ~15) - 16;      // the last piece of the last step
 
     // where a lane's 16 bytes come from: row 8 q + lane / 8 of the stage, piece lane % 8 turned by the row
     const int8_t *const x0 = X + (int64_t)t0 * ldx, *const a0 = A + (int64_t)r0 * lda;
@@ -59,7 +71,7 @@ __global__ __launch_bounds__(64 * WT * WR) void k_gemm_i8(int rows, int cols, in
     unsigned from[LOADS], end[LOADS];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-        const int q = i * NW + wave, row = 8 * q + (lane >> 3), piece = 16 * ((lane & 7) ^ (lane >> 3));
+        const int q = i * NW + wave, row = 8 * q + (lane >> 3), piece = 16 * ((lane & 7) ^ turn<M>(row));
         const bool x = 8 * q < BT;
         base[i] = x ? x0 : a0;
         from[i] = x ? (unsigned)min(row, n - 1 - t0) * (unsigned)ldx : (unsigned)min(row - BT, rows - 1 - r0) * (unsigned)lda;
@@ -77,72 +89,142 @@ __global__ __launch_bounds__(64 * WT * WR) void k_gemm_i8(int rows, int cols, in
             for (int i = 0; i < LOADS; ++i) to_lds(base[i] + k, end[i], to + i * NW * 1024);
         }
     };
-    for (int k = 0; k < S - 1 && k < blocks; ++k) fetch(k);
-
-    v4i acc[TR][TT];
-#pragma unroll
-    for (int r = 0; r < TR; ++r)
-#pragma unroll
-        for (int t = 0; t < TT; ++t) acc[r][t] = v4i{0, 0, 0, 0};
-    const int in16 = lane & 15, quarter = lane >> 4;
-    for (int k = 0; k < blocks; ++k) {
+    // Step k is there for all waves, and step k - 1 has been read by all.  Behind the last column the tokens' codes become zeros (once).
+    auto arrive = [&](int k) {
         if (k + S - 2 < blocks - 1) step_barrier<(S - 2) * LOADS>();
         else step_barrier<0>();
         if (k + S - 1 < blocks) fetch(k + S - 1);
-        const int8_t *const st = lds + k % S * STAGE;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int place = in16 * STEP + 16 * ((4 * h + quarter) ^ (lane & 7));
-            v4i x[TT], a[TR];
-#pragma unroll
-            for (int t = 0; t < TT; ++t) x[t] = *reinterpret_cast<const v4i *>(st + ((wt * TT + t) * 16) * STEP + place);
-#pragma unroll
-            for (int r = 0; r < TR; ++r) a[r] = *reinterpret_cast<const v4i *>(st + (BT + (wr * TR + r) * 16) * STEP + place);
-            if (k == blocks - 1) {
-#pragma unroll
-                for (int t = 0; t < TT; ++t) x[t] = first_bytes(x[t], cols - k * STEP - 64 * h - 16 * quarter);
+        if (k == blocks - 1 && left < STEP) {
+            int8_t *const st = lds + k % S * STAGE;
+            for (int i = threadIdx.x; i < BT * 8; i += 64 * NW) {
+                const int piece = 16 * ((i & 7) ^ turn<M>(i >> 3));
+                v4i *const at = reinterpret_cast<v4i *>(st + 16 * i);
+                if (piece + 16 > left) *at = first_bytes(*at, left - piece);
             }
+            step_barrier<0>();
+        }
+    };
+    const int in = lane & (M - 1), part = lane / M;
+    const int xrow = (wt * TT * M + in) * STEP, arow = (BT + wr * TR * M + in) * STEP;
+    struct Operands { v4i x[TT], a[TR]; };
+    auto read = [&](Operands &o, int k, int h) {
+        const int8_t *const st = lds + k % S * STAGE + 16 * ((64 / M * h + part) ^ turn<M>(in));
 #pragma unroll
-            for (int r = 0; r < TR; ++r)
+        for (int t = 0; t < TT; ++t) o.x[t] = *reinterpret_cast<const v4i *>(st + xrow + t * M * STEP);
 #pragma unroll
-                for (int t = 0; t < TT; ++t) acc[r][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a[r], x[t], acc[r][t], 0, 0, 0);
+        for (int r = 0; r < TR; ++r) o.a[r] = *reinterpret_cast<const v4i *>(st + arow + r * M * STEP);
+    };
+    Sum acc[TR][TT];
+#pragma unroll
+    for (int r = 0; r < TR; ++r)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) acc[r][t] = Sum{};
+    auto multiply = [&](const Operands &o) {
+#pragma unroll
+        for (int r = 0; r < TR; ++r)
+#pragma unroll
+            for (int t = 0; t < TT; ++t) acc[r][t] = Product<M>::go(o.a[r], o.x[t], acc[r][t]);
+    };
+
+    // The operands of a part are read while the part before is multiplied, across the barrier too.
+    for (int k = 0; k < S - 1 && k < blocks; ++k) fetch(k);
+    Operands o[2];
+    if (blocks > 0) {
+        arrive(0);
+        read(o[0], 0, 0);
+    }
+    for (int k = 0; k < blocks; ++k) {
+#pragma unroll
+        for (int h = 0; h < PARTS; ++h) {
+            if (h + 1 < PARTS) {
+                read(o[(h + 1) & 1], k, h + 1);
+            } else if (k + 1 < blocks) {
+                arrive(k + 1);
+                read(o[0], k + 1, 0);
+            }
+            multiply(o[h & 1]);
         }
     }
-    // channel 4 (lane / 16) + i of token lane % 16
+    // A lane has four channels of a token, 4 (lane / M) + 0 .. 3 of every 256 / M.  They change places in LDS, M tokens of the wave at a time, and leave in
+    // pieces of 16 bytes, a token's one after the other.  (Stored as they are, and with the tokens' scales loaded one by one, they took 22 us for a tile.)
+    constexpr int G = M * M / 256, ES = YT == F32 ? 4 : 2, EACH = 16 / ES, PIECES = TR * M / EACH, PITCH = PIECES * 16 + 16;
+    static_assert(NW * M * PITCH <= S * STAGE, "room in LDS");
+    const int row0 = r0 + wr * TR * M;
+    float a[TR][G][4], b[TR][G][4], s[TT];
 #pragma unroll
-    for (int r = 0; r < TR; ++r) {
-        const int row = r0 + (wr * TR + r) * 16 + 4 * quarter;
-        float a[4], b[4];
+    for (int t = 0; t < TT; ++t) s[t] = f.s[min(t0 + (wt * TT + t) * M + in, n - 1)];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            a[i] = f.a[min(row + i, rows - 1)];
-            b[i] = f.bias ? f.bias[min(row + i, rows - 1)] : 0.0f;
-        }
+    for (int r = 0; r < TR; ++r)
 #pragma unroll
-        for (int t = 0; t < TT; ++t) {
-            const int token = t0 + (wt * TT + t) * 16 + in16;
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[r][g][i] = f.a[min(row0 + r * M + 256 / M * g + 4 * part + i, rows - 1)];
+    if (f.bias) {
+#pragma unroll
+        for (int r = 0; r < TR; ++r)
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) b[r][g][i] = f.bias[min(row0 + r * M + 256 / M * g + 4 * part + i, rows - 1)];
+    } else {
+#pragma unroll
+        for (int r = 0; r < TR; ++r)
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) b[r][g][i] = 0.0f;
+    }
+    step_barrier<0>();                                     // the last step has been read
+    int8_t *const room = lds + wave * M * PITCH;
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+#pragma unroll
+        for (int r = 0; r < TR; ++r)
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                float v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = finish(acc[r][t][4 * g + i], a[r][g][i], s[t], b[r][g][i]);
+                int8_t *const at = room + in * PITCH + (r * M + 256 / M * g + 4 * part) * ES;
+                if constexpr (YT == F32) *reinterpret_cast<v4f *>(at) = v4f{v[0], v[1], v[2], v[3]};
+                else *reinterpret_cast<v4s *>(at) = v4s{narrow<YT>(v[0]), narrow<YT>(v[1]), narrow<YT>(v[2]), narrow<YT>(v[3])};
+            }
+        wave_fence();
+#pragma unroll
+        for (int i = 0; i < M * PIECES; i += 64) {
+            const int at = i + lane, token = t0 + (wt * TT + t) * M + at / PIECES, row = row0 + at % PIECES * EACH;
+            if (M * PIECES % 64 && at >= M * PIECES) continue;
+            const int8_t *const from = room + at / PIECES * PITCH + at % PIECES * 16;
+            const v4u v = *reinterpret_cast<const v4u *>(from);
             if (token >= n || row >= rows) continue;
-            const float s = f.s[token];
-            const float v[4] = {finish(acc[r][t][0], a[0], s, b[0]), finish(acc[r][t][1], a[1], s, b[1]), finish(acc[r][t][2], a[2], s, b[2]),
-                                finish(acc[r][t][3], a[3], s, b[3])};
-            put4<YT>(Y, token * ldy + row, v, rows - row);
+            char *const to = static_cast<char *>(Y) + (token * ldy + row) * ES;
+            if (row + EACH <= rows) {
+                if constexpr (YT == F32) *reinterpret_cast<v4f_e *>(to) = __builtin_bit_cast(v4f, v);
+                else *reinterpret_cast<v4u_u *>(to) = v;
+            } else {
+                for (int e = 0; row + e < rows; ++e) {
+                    if constexpr (YT == F32) reinterpret_cast<float *>(to)[e] = reinterpret_cast<const float *>(from)[e];
+                    else reinterpret_cast<unsigned short *>(to)[e] = reinterpret_cast<const unsigned short *>(from)[e];
+                }
+            }
         }
+        wave_fence();
     }
 }
 
-template <int YT, int BT, int BR, int WT, int WR, int S>
+template <int YT, int BT, int BR, int WT, int WR, int S, int M>
 void tiles(int rows, int cols, int n, const int8_t *A, int64_t lda, const int8_t *X, int64_t ldx, const Finish &f, void *Y, int64_t ldy, hipStream_t s)
 {
     const unsigned r = (unsigned)((rows + BR - 1) / BR), all = r * (unsigned)((n + BT - 1) / BT), x = all < 65536 ? all : 65536;
-    PSK_LAUNCH((k_gemm_i8<YT, BT, BR, WT, WR, S>), dim3(x, (all + x - 1) / x), dim3(64 * WT * WR), 0, s, rows, cols, n, A, lda, X, ldx, f, Y, ldy, r, all);
+    PSK_LAUNCH((k_gemm_i8<YT, BT, BR, WT, WR, S, M>), dim3(x, (all + x - 1) / x), dim3(64 * WT * WR), 0, s, rows, cols, n, A, lda, X, ldx, f, Y, ldy, r, all);
 }
 
 template <int YT>
 hipError_t launch(int rows, int cols, int n, const int8_t *A, int64_t lda, const int8_t *X, int64_t ldx, const Finish &f, void *Y, int64_t ldy, hipStream_t s)
 {
-    if (n <= 64) tiles<YT, 32, 64, 1, 4, 4>(rows, cols, n, A, lda, X, ldx, f, Y, ldy, s);
-    else if (n <= 512) tiles<YT, 128, 128, 2, 2, 3>(rows, cols, n, A, lda, X, ldx, f, Y, ldy, s);
-    else tiles<YT, 256, 256, 2, 4, 2>(rows, cols, n, A, lda, X, ldx, f, Y, ldy, s);
+    if (n <= 64) tiles<YT, 32, 64, 1, 4, 4, 16>(rows, cols, n, A, lda, X, ldx, f, Y, ldy, s);
+    else if (n <= 512) tiles<YT, 128, 128, 2, 2, 3, MID_M>(rows, cols, n, A, lda, X, ldx, f, Y, ldy, s);
+    else tiles<YT, 256, 256, 2, BIG_WR, 2, BIG_M>(rows, cols, n, A, lda, X, ldx, f, Y, ldy, s);
     return take_launch_status();
 }
 
