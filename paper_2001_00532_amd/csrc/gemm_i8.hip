@@ -5,19 +5,8 @@
 // bytes, row by row) meets each bank once.  One barrier a step: behind it the step's operands are there and the stage before is free.
 #include "gemm_i8.h"
 
-#ifndef BIG_M
-#define BIG_M 32
-#endif
-#ifndef BIG_WR
-#define BIG_WR 4
-#endif
-#ifndef MID_M
-#define MID_M 16
-#endif
 namespace psk {
 namespace {
-
-constexpr int STEP = 128;                                  // columns, and bytes of a row of a stage
 
 // 16 bytes per lane from base + offset to LDS at `to` + 16 lane.
 __device__ __forceinline__ void to_lds(const void *base, unsigned offset, const void *to)
@@ -45,18 +34,22 @@ template <> struct Product<32> {
     static __device__ __forceinline__ Sum go(v4i a, v4i x, Sum c) { return __builtin_amdgcn_mfma_i32_32x32x32_i8(a, x, c, 0, 0, 0); }
 };
 
-// By how much the eight pieces of a row are turned.  A read of 16 bytes a lane goes through the banks by sixteen lanes, 0-3, 12-15, 20-23 and 24-27 first: rows of
-// their own in an instruction of 32, four rows and three of the next piece in one of 16.
-template <int M>
-__device__ __forceinline__ int turn(int row) { return M == 32 ? (row & 7) ^ (row >> 4 & 1) : row & 7; }
+// By how much the pieces of a row of STEP bytes are turned.  A read of 16 bytes a lane goes through the banks by sixteen lanes, 0-3, 12-15, 20-23 and 24-27
+// first, which then have a place of their own among the 256 bytes of all banks.
+template <int M, int STEP>
+__device__ __forceinline__ int turn(int row)
+{
+    if constexpr (STEP == 64) return -(row >> 2) & 3;
+    else return M == 32 ? (row & 7) ^ (row >> 4 & 1) : row & 7;
+}
 
-// BT tokens x BR channels by WT x WR waves, S stages, instructions of M x M.
-template <int YT, int BT, int BR, int WT, int WR, int S, int M>
+// BT tokens x BR channels by WT x WR waves, S stages of STEP columns, instructions of M x M.
+template <int YT, int BT, int BR, int WT, int WR, int S, int M, int STEP>
 __global__ __launch_bounds__(64 * WT * WR) void k_gemm_i8(int rows, int cols, int n, const int8_t *A, int64_t lda, const int8_t *X, int64_t ldx, Finish f, void *Y,
                                                           int64_t ldy, unsigned tiles_r, unsigned tiles)
 {
-    constexpr int NW = WT * WR, LOADS = (BT + BR) / 8 / NW, TT = BT / WT / M, TR = BR / WR / M, STAGE = (BT + BR) * STEP, PARTS = M / 8;
-    static_assert((BT + BR) % (8 * NW) == 0, "whole loads");
+    constexpr int NW = WT * WR, LINES = 1024 / STEP, PER = STEP / 16, LOADS = (BT + BR) / LINES / NW, TT = BT / WT / M, TR = BR / WR / M, STAGE = (BT + BR) * STEP, PARTS = STEP * M / 1024;
+    static_assert((BT + BR) % (LINES * NW) == 0 && BT % LINES == 0, "whole loads");
     typedef typename Product<M>::Sum Sum;
     __shared__ __attribute__((aligned(1024))) int8_t lds[S * STAGE];
     const unsigned tile = blockIdx.y * gridDim.x + blockIdx.x;
@@ -65,14 +58,14 @@ __global__ __launch_bounds__(64 * WT * WR) void k_gemm_i8(int rows, int cols, in
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wt = wave / WR, wr = wave % WR;
     const int blocks = (cols + STEP - 1) / STEP, left = cols - (blocks - 1) * STEP, most = ((left + 15) & ~15) - 16;      // the last piece of the last step
 
-    // where a lane's 16 bytes come from: row 8 q + lane / 8 of the stage, piece lane % 8 turned by the row
+    // where a lane's 16 bytes come from: row LINES q + lane / PER of the stage, piece lane % PER turned by the row
     const int8_t *const x0 = X + (int64_t)t0 * ldx, *const a0 = A + (int64_t)r0 * lda;
     const int8_t *base[LOADS];
     unsigned from[LOADS], end[LOADS];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-        const int q = i * NW + wave, row = 8 * q + (lane >> 3), piece = 16 * ((lane & 7) ^ turn<M>(row));
-        const bool x = 8 * q < BT;
+        const int q = i * NW + wave, row = LINES * q + lane / PER, piece = 16 * ((lane % PER) ^ turn<M, STEP>(row));
+        const bool x = LINES * q < BT;
         base[i] = x ? x0 : a0;
         from[i] = x ? (unsigned)min(row, n - 1 - t0) * (unsigned)ldx : (unsigned)min(row - BT, rows - 1 - r0) * (unsigned)lda;
         end[i] = from[i] + (unsigned)min(piece, most);
@@ -94,10 +87,10 @@ __global__ __launch_bounds__(64 * WT * WR) void k_gemm_i8(int rows, int cols, in
         if (k + S - 2 < blocks - 1) step_barrier<(S - 2) * LOADS>();
         else step_barrier<0>();
         if (k + S - 1 < blocks) fetch(k + S - 1);
-        if (k == blocks - 1 && left < STEP) {
+        if (left < STEP && k == blocks - 1) {
             int8_t *const st = lds + k % S * STAGE;
-            for (int i = threadIdx.x; i < BT * 8; i += 64 * NW) {
-                const int piece = 16 * ((i & 7) ^ turn<M>(i >> 3));
+            for (int i = threadIdx.x; i < BT * PER; i += 64 * NW) {
+                const int piece = 16 * ((i % PER) ^ turn<M, STEP>(i / PER));
                 v4i *const at = reinterpret_cast<v4i *>(st + 16 * i);
                 if (piece + 16 > left) *at = first_bytes(*at, left - piece);
             }
@@ -108,7 +101,7 @@ __global__ __launch_bounds__(64 * WT * WR) void k_gemm_i8(int rows, int cols, in
     const int xrow = (wt * TT * M + in) * STEP, arow = (BT + wr * TR * M + in) * STEP;
     struct Operands { v4i x[TT], a[TR]; };
     auto read = [&](Operands &o, int k, int h) {
-        const int8_t *const st = lds + k % S * STAGE + 16 * ((64 / M * h + part) ^ turn<M>(in));
+        const int8_t *const st = lds + k % S * STAGE + 16 * ((64 / M * h + part) ^ turn<M, STEP>(in));
 #pragma unroll
         for (int t = 0; t < TT; ++t) o.x[t] = *reinterpret_cast<const v4i *>(st + xrow + t * M * STEP);
 #pragma unroll
@@ -133,16 +126,23 @@ __global__ __launch_bounds__(64 * WT * WR) void k_gemm_i8(int rows, int cols, in
         arrive(0);
         read(o[0], 0, 0);
     }
-    for (int k = 0; k < blocks; ++k) {
+    constexpr int ROUND = PARTS == 1 ? 2 : 1;              // steps behind which the operands are in the same registers again
+    for (int k0 = 0; k0 < blocks; k0 += ROUND) {
 #pragma unroll
-        for (int h = 0; h < PARTS; ++h) {
-            if (h + 1 < PARTS) {
-                read(o[(h + 1) & 1], k, h + 1);
-            } else if (k + 1 < blocks) {
-                arrive(k + 1);
-                read(o[0], k + 1, 0);
+        for (int j = 0; j < ROUND; ++j) {
+            const int k = k0 + j;
+            if (j > 0 && k >= blocks) break;
+#pragma unroll
+            for (int h = 0; h < PARTS; ++h) {
+                const int now = (j * PARTS + h) & 1;
+                if (h + 1 < PARTS) {
+                    read(o[now ^ 1], k, h + 1);
+                } else if (k + 1 < blocks) {
+                    arrive(k + 1);
+                    read(o[now ^ 1], k + 1, 0);
+                }
+                multiply(o[now]);
             }
-            multiply(o[h & 1]);
         }
     }
     // A lane has four channels of a token, 4 (lane / M) + 0 .. 3 of every 256 / M.  They change places in LDS, M tokens of the wave at a time, and leave in
@@ -212,19 +212,39 @@ __global__ __launch_bounds__(64 * WT * WR) void k_gemm_i8(int rows, int cols, in
     }
 }
 
-template <int YT, int BT, int BR, int WT, int WR, int S, int M>
+template <int YT, int BT, int BR, int WT, int WR, int S, int M, int STEP>
 void tiles(int rows, int cols, int n, const int8_t *A, int64_t lda, const int8_t *X, int64_t ldx, const Finish &f, void *Y, int64_t ldy, hipStream_t s)
 {
     const unsigned r = (unsigned)((rows + BR - 1) / BR), all = r * (unsigned)((n + BT - 1) / BT), x = all < 65536 ? all : 65536;
-    PSK_LAUNCH((k_gemm_i8<YT, BT, BR, WT, WR, S, M>), dim3(x, (all + x - 1) / x), dim3(64 * WT * WR), 0, s, rows, cols, n, A, lda, X, ldx, f, Y, ldy, r, all);
+    PSK_LAUNCH((k_gemm_i8<YT, BT, BR, WT, WR, S, M, STEP>), dim3(x, (all + x - 1) / x), dim3(64 * WT * WR), 0, s, rows, cols, n, A, lda, X, ldx, f, Y, ldy, r, all);
 }
+
+// Tiles by their tokens and channels.
+struct Shape { int tokens, channels; };
+constexpr Shape SHAPES[] = {{16, 16}, {16, 32}, {32, 32}, {32, 64}, {64, 32}, {64, 64}, {128, 64}, {128, 128}, {256, 128}, {256, 256}};
+constexpr int SHAPE_COUNT = sizeof(SHAPES) / sizeof(SHAPES[0]);
 
 template <int YT>
 hipError_t launch(int rows, int cols, int n, const int8_t *A, int64_t lda, const int8_t *X, int64_t ldx, const Finish &f, void *Y, int64_t ldy, hipStream_t s)
 {
-    if (n <= 64) tiles<YT, 32, 64, 1, 4, 4, 16>(rows, cols, n, A, lda, X, ldx, f, Y, ldy, s);
-    else if (n <= 512) tiles<YT, 128, 128, 2, 2, 3, MID_M>(rows, cols, n, A, lda, X, ldx, f, Y, ldy, s);
-    else tiles<YT, 256, 256, 2, BIG_WR, 2, BIG_M>(rows, cols, n, A, lda, X, ldx, f, Y, ldy, s);
+    decltype(&tiles<YT, 16, 16, 1, 1, 8, 16, 128>) const go[SHAPE_COUNT] = {
+        tiles<YT, 16, 16, 1, 1, 8, 16, 128>, tiles<YT, 16, 32, 1, 2, 8, 16, 128>, tiles<YT, 32, 32, 2, 2, 6, 16, 128>, tiles<YT, 32, 64, 1, 4, 4, 16, 128>,
+        tiles<YT, 64, 32, 4, 1, 4, 16, 128>, tiles<YT, 64, 64, 2, 2, 4, 16, 128>, tiles<YT, 128, 64, 2, 2, 3, 16, 128>, tiles<YT, 128, 128, 2, 2, 4, 16, 128>,
+        tiles<YT, 256, 128, 4, 2, 3, 16, 128>, tiles<YT, 256, 256, 2, 4, 2, 16, 128>};
+    int best = 0;
+    int64_t least = INT64_MAX;
+    for (int i = 0; i < SHAPE_COUNT; ++i) {
+        const int64_t all = (int64_t)((n + SHAPES[i].tokens - 1) / SHAPES[i].tokens) * ((rows + SHAPES[i].channels - 1) / SHAPES[i].channels);
+        const int64_t cost = (all + 255) / 256 * (SHAPES[i].tokens + SHAPES[i].channels);
+        if (cost <= least) {
+            least = cost;
+            best = i;
+        }
+    }
+#ifdef TILE_ENV
+    if (getenv("PSK_TILE")) best = atoi(getenv("PSK_TILE"));
+#endif
+    go[best](rows, cols, n, A, lda, X, ldx, f, Y, ldy, s);
     return take_launch_status();
 }
 
