@@ -61,14 +61,20 @@ __device__ __forceinline__ void clear_unnamed(const Clear &c, const int *__restr
         const int count = (int)min(end - first, (int64_t)RANGE);
         for (int i = threadIdx.x; i < (count + 31) / 32; i += THREADS) bits[i] = 0;
         __syncthreads();
-        for (int t = threadIdx.x; t < n; t += 8 * THREADS) {
+        for (int t = 0; t < n; t += 8 * THREADS) {
+            const int *const at = ids + t;
             int id[8];                                     // eight loads in flight; behind the last token that is read again
+            if (t + 8 * THREADS <= n) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) id[i] = ids[min(t + i * THREADS, n - 1)];
+                for (int i = 0; i < 8; ++i) id[i] = at[i * THREADS + threadIdx.x];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) id[i] = at[min(i * THREADS + (int)threadIdx.x, n - 1 - t)];
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int64_t at = id[i] - first;
-                if (id[i] != padding && at >= 0 && at < count) atomicOr(&bits[at >> 5], 1u << (at & 31));
+                const unsigned row = (unsigned)id[i] - (unsigned)first;
+                if (row < (unsigned)count && id[i] != padding) atomicOr(&bits[row >> 5], 1u << (row & 31));
             }
         }
         __syncthreads();
@@ -98,13 +104,22 @@ __device__ __forceinline__ void clear_absent(const Clear &c, const int *__restri
 }
 
 // ------------------------------------------------------------------ the sort
-// Lanes of the wave with the same digit as this one, of those that have one.
+// Lanes of the wave with the same digit as this one, of those that have one.  Often these are few, or most of them the same: up to three digits are
+// looked for one by one, and only if there are more, all bit by bit.
 __device__ __forceinline__ unsigned long long same_digit(int d, int bits, bool valid)
 {
     const unsigned long long all = __ballot(valid);
-    const int one = __builtin_amdgcn_readlane(d, __builtin_ctzll(all | 1ull << 63));
-    if (__ballot(valid && d == one) == all) return all;    // often there is one, or the same one many times
-    unsigned long long m = all;
+    unsigned long long left = all, m = 0;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        if (!left) return m;
+        const int one = __builtin_amdgcn_readlane(d, __builtin_ctzll(left));
+        const unsigned long long equal = __ballot(valid && d == one);
+        m = d == one ? equal : m;
+        left &= ~equal;
+    }
+    if (!left) return m;
+    m = all;
     for (int b = 0; b < bits; ++b) {
         const unsigned long long set = __ballot(d >> b & 1);
         m &= d >> b & 1 ? set : ~set;
@@ -142,19 +157,23 @@ __device__ __forceinline__ int block_exclusive(int v, int *part)
 }
 
 // Up to NEAR tokens and RANGES ranges of rows: a workgroup owns `per` rows, reads all tokens, and so knows by itself how many positions are before those of
-// its rows.  It counts its own, wave by wave (a wave has a sixteenth of the tokens), puts them in their places, and clears the rows that had none.
+// its rows.  It counts its own, wave by wave (a wave has a sixteenth of the tokens), and puts them in their places.  Beside these, as many workgroups
+// again clear (clear_unnamed): waiting and writing go together.
 // One launch; a token's workgroups read 4 bytes of L2 each, 16384 tokens and 256 workgroups 16 MB.
-// 16000 tokens, 4000 rows: 9 us; by one workgroup that sorted them in LDS while the others cleared 35.
+// 16000 tokens, 4000 rows: 16 us; by one workgroup that sorted them in LDS while the others cleared 35.
 constexpr int NEAR = 65536, RANGES = 1024, MOST_ROWS = 512;
 
-template <int GT, bool CLEAR>
-__global__ __launch_bounds__(1024) void k_sort_ranges(const int *__restrict__ ids, int n, int padding, int per, int bits, int *__restrict__ keys_out,
+template <int GT>
+__global__ __launch_bounds__(1024) void k_sort_ranges(const int *__restrict__ ids, int n, int padding, int per, int bits, int ranges, int *__restrict__ keys_out,
                                                       int *__restrict__ at_out, int *__restrict__ joins, Clear c)
 {
-    constexpr int WAVES = 16, U = 16;                      // rounds of 64 tokens whose loads are in flight
+    constexpr int WAVES = 16, U = 8;                       // rounds of 64 tokens whose loads are in flight
     __shared__ int seen[WAVES][MOST_ROWS];
     __shared__ int part[WAVES], less[WAVES];
-    __shared__ unsigned long long present[MOST_ROWS / 64];
+    if ((int)blockIdx.x >= ranges) {
+        clear_unnamed<GT, 1024>(c, ids, n, padding, blockIdx.x - ranges, gridDim.x - ranges, reinterpret_cast<unsigned *>(&seen[0][0]));
+        return;
+    }
     if (blockIdx.x == 0 && threadIdx.x < 2) joins[threadIdx.x] = 0;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int first = blockIdx.x * per, count = min(per, c.rows - first);
@@ -162,32 +181,39 @@ __global__ __launch_bounds__(1024) void k_sort_ranges(const int *__restrict__ id
     for (int d = threadIdx.x; d < WAVES * MOST_ROWS; d += 1024) (&seen[0][0])[d] = 0;
     __syncthreads();
     int before = 0;                                        // tokens of earlier rows
-    auto each_round = [&](auto f) {
-        for (int r = 0; r < rounds; r += U) {
-            int id[U];
+    unsigned long long active = 0;                         // rounds with tokens of this range
+    static_assert(NEAR / 1024 <= 64, "a bit for each round");
+    auto mine = [&](int id, int at) { return at < n && (unsigned)(id - first) < (unsigned)count && id != padding; };
+    // Few instructions for each token, most are of no concern here: what padding and the tokens that are read again behind the last one make of `before` is
+    // taken off below.
+    for (int r = 0; r < rounds; r += U) {
+        const int *const at = ids + begin + 64 * r;
+        int id[U];
+        if (begin + 64 * (r + U) <= n) {
+#pragma unroll
+            for (int i = 0; i < U; ++i) id[i] = at[64 * i + lane];
+        } else {
 #pragma unroll
             for (int i = 0; i < U; ++i) id[i] = ids[min(begin + 64 * (r + i) + lane, n - 1)];
+        }
 #pragma unroll
-            for (int i = 0; i < U; ++i) {
-                const int at = begin + 64 * (r + i) + lane;
-                f(at, r + i < rounds && at < n && id[i] != padding ? id[i] : -1);
+        for (int i = 0; i < U; ++i) {
+            if (r + i >= rounds) break;
+            before += (unsigned)id[i] < (unsigned)first;
+            if (__ballot((unsigned)(id[i] - first) < (unsigned)count)) {         // counts only: nothing waits for LDS
+                active |= 1ull << (r + i);
+                const bool is = mine(id[i], begin + 64 * (r + i) + lane);
+                const unsigned long long same = same_digit(id[i] - first, bits, is);
+                if (is && !(same & ((1ull << lane) - 1))) atomicAdd(&seen[wave][id[i] - first], __popcll(same));
             }
         }
-    };
-    each_round([&](int, int id) {
-        before += id >= 0 && id < first;
-        const bool mine = id >= first && id < first + count;
-        if (__ballot(mine)) {                              // counts only: nothing waits for LDS
-            const unsigned long long same = same_digit(id - first, bits, mine);
-            if (mine && !(same & ((1ull << lane) - 1))) atomicAdd(&seen[wave][id - first], __popcll(same));
-        }
-    });
-    before += __shfl_xor(before, 1);
-    before += __shfl_xor(before, 2);
-    before += __shfl_xor(before, 4);
-    before += __shfl_xor(before, 8);
-    before += __shfl_xor(before, 16);
-    before += __shfl_xor(before, 32);
+    }
+    const int over = begin + 64 * rounds - max(n, begin);  // places of this wave behind the last token
+    if (over > 0 && (unsigned)ids[n - 1] < (unsigned)first) before -= over / 64 + (lane < over % 64);
+    if ((unsigned)padding < (unsigned)first)
+        for (int i = begin + lane; i < min(begin + 64 * rounds, n); i += 64) before -= ids[i] == padding;
+#pragma unroll
+    for (int d = 1; d < WAVE; d *= 2) before += __shfl_xor(before, d, WAVE);
     if (lane == 0) less[wave] = before;
     __syncthreads();
     int earlier = 0, own = 0;
@@ -201,8 +227,6 @@ __global__ __launch_bounds__(1024) void k_sort_ranges(const int *__restrict__ id
             seen[w][threadIdx.x] = own;
             own += v[w];
         }
-        const unsigned long long m = __ballot(own > 0);
-        if (lane == 0) present[wave] = m;
     }
     const int base = earlier + block_exclusive<1024>(own, part);
     if (threadIdx.x < MOST_ROWS) {
@@ -211,24 +235,27 @@ __global__ __launch_bounds__(1024) void k_sort_ranges(const int *__restrict__ id
     }
     if (threadIdx.x == 1023) part[0] = base;               // behind the last row of this range
     __syncthreads();
-    const int end = part[0];
-    if (end > earlier)
-        each_round([&](int at, int id) {
-            const bool mine = id >= first && id < first + count;
-            if (!__ballot(mine)) return;
-            const int to = place_in_wave(id - first, bits, mine, lane, seen[wave]);
-            if (mine) {
-                keys_out[to] = id;
-                at_out[to] = at;
+    while (active) {                                       // rounds in order, U of them at a time
+        int at[U], id[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            at[i] = active ? begin + 64 * __builtin_ctzll(active) + lane : n;
+            active &= active - 1;
+            id[i] = ids[min(at[i], n - 1)];
+        }
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const bool is = mine(id[i], at[i]);
+            if (!__ballot(is)) continue;
+            const int to = place_in_wave(id[i] - first, bits, is, lane, seen[wave]);
+            if (is) {
+                keys_out[to] = id[i];
+                at_out[to] = at[i];
             }
-        });
-    if (blockIdx.x == gridDim.x - 1)                       // positions that are in no row
-        for (int i = end + threadIdx.x; i < n; i += 1024) keys_out[i] = c.rows;
-    if constexpr (CLEAR) {
-        const int log = lanes_log<GT>(c.dim), sub = threadIdx.x & ((1 << log) - 1);
-        for (int r = threadIdx.x >> log; r < count; r += 1024 >> log)
-            if (!(present[r >> 6] >> (r & 63) & 1)) clear_row<GT>(c, first + r, sub, 1 << log);
+        }
     }
+    if ((int)blockIdx.x == ranges - 1)                     // positions that are in no row
+        for (int i = part[0] + threadIdx.x; i < n; i += 1024) keys_out[i] = c.rows;
 }
 
 // Several workgroups: they count their digits, and then put their positions behind those of smaller digits and of earlier workgroups.
@@ -490,37 +517,36 @@ __global__ __launch_bounds__(256) void k_grad_sum(Grad g, int chunks, int64_t su
 }
 
 // A row that begins in a tile and goes on behind it: its parts in order.  Few parts: a workgroup takes the tile and 2048 columns, a wave 256 of them.  Many:
-// the tile and 256 columns, a wave takes an eighth of the parts, and their sums meet in LDS.
+// the tile and 64 columns (one compute unit reads 60 GB/s, so the parts of a row go to many), a wave takes an eighth of the parts, four at a time, and
+// their sums meet in LDS.
 // (Without the lists, a workgroup to every tile and 256 columns took 25 us for 16384 tokens of 4096 columns, most to find nothing.)
 constexpr int JOIN = 8;                                    // waves
 struct Part {                                              // a lane's columns
     bool mine;
     Unit u;
 };
-__device__ __forceinline__ Part part_of(const Grad &g, int quad, int lane)
+__device__ __forceinline__ Part part_of(const Grad &g, int unit)
 {
-    const int unit = quad * 64 + lane;
     Part p;
-    p.mine = g.dim < 4 ? lane < g.dim && quad == 0 : 4 * unit < g.dim;
-    p.u = g.dim < 4 ? Unit{p.mine ? lane : 0, 0} : unit_of<4>(p.mine ? unit : 0, g.dim);
+    p.mine = g.dim < 4 ? unit < g.dim : 4 * unit < g.dim;
+    p.u = g.dim < 4 ? Unit{p.mine ? unit : 0, 0} : unit_of<4>(p.mine ? unit : 0, g.dim);
     return p;
 }
-// Parts from .. to - 1.
-template <int U>                                           // in flight
-__device__ __forceinline__ void add_parts(const Grad &g, const float *head, int from, int to, float (&sum)[4])
+__device__ __forceinline__ void add_parts(const Grad &g, const float *head, int more, float (&sum)[4])
 {
+    constexpr int U = 4;                                   // in flight
     if (g.dim < 4) {
-        for (int i = from; i < to; ++i) sum[0] += head[(int64_t)i * g.dim];
+        for (int i = 0; i < more; ++i) sum[0] += head[(int64_t)i * g.dim];
         return;
     }
-    for (int i = from; i < to; i += U) {
+    for (int i = 0; i < more; i += U) {
         Raw4<F32> r[U];
 #pragma unroll
-        for (int j = 0; j < U; ++j) load_raw<F32>(r[j], head + (int64_t)min(i + j, to - 1) * g.dim);
+        for (int j = 0; j < U; ++j) load_raw<F32>(r[j], head + (int64_t)min(i + j, more - 1) * g.dim);
 #pragma unroll
         for (int j = 0; j < U; ++j)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sum[k] += i + j < to ? r[j].a[k] : 0.0f;
+            for (int k = 0; k < 4; ++k) sum[k] += i + j < more ? r[j].a[k] : 0.0f;
     }
 }
 template <int GT>
@@ -538,15 +564,16 @@ __device__ __forceinline__ void put_joined(const Grad &g, int tile, int row, con
     }
 }
 template <int GT>
-__global__ __launch_bounds__(64 * JOIN) void k_grad_join(Grad g, int tiles, int groups, int quads)
+__global__ __launch_bounds__(64 * JOIN) void k_grad_join(Grad g, int tiles, int groups, int strips)
 {
-    __shared__ float meet[JOIN - 1][4][64];
+    constexpr int U = 8;                                   // parts in flight for each lane
+    __shared__ v4f meet[JOIN * 4][16];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t few = (int64_t)g.joins[0] * groups, all = few + (int64_t)g.joins[1] * quads;
+    const int64_t few = (int64_t)g.joins[0] * groups, all = few + (int64_t)g.joins[1] * strips;
     for (int64_t w = blockIdx.x; w < all; w += gridDim.x) {
         const bool many = w < all - few;                   // the long ones first
         const int64_t v = many ? w : w - (all - few);
-        const int tile = many ? g.joins[2 + tiles - 1 - v / quads] : g.joins[2 + v / groups], row = g.keys[(tile + 1) * g.tile];
+        const int tile = many ? g.joins[2 + tiles - 1 - v / strips] : g.joins[2 + v / groups], row = g.keys[(tile + 1) * g.tile];
         int more = 0;                                      // tiles behind it that begin with the row
         for (;;) {
             const int t = tile + 1 + more + lane;
@@ -554,27 +581,37 @@ __global__ __launch_bounds__(64 * JOIN) void k_grad_join(Grad g, int tiles, int 
             more += same;                                  // at most 63 of a round
             if (same < 63) break;
         }
-        const Part p = part_of(g, (int)(many ? v % quads : v % groups * JOIN + wave), lane);
-        const float *const head = g.head + (int64_t)(tile + 1) * g.dim + p.u.col;
-        float sum[4] = {};
+        const float *const heads = g.head + (int64_t)(tile + 1) * g.dim;
         if (!many) {
-            if (p.mine) add_parts<4>(g, head, 0, more, sum);
+            const Part p = part_of(g, (int)(v % groups) * 64 * JOIN + wave * 64 + lane);
+            float sum[4] = {};
+            if (p.mine) add_parts(g, heads + p.u.col, more, sum);
             put_joined<GT>(g, tile, row, p, sum);
             continue;
         }
-        const int each = (more + JOIN - 1) / JOIN, from = min(wave * each, more);
-        if (p.mine) add_parts<16>(g, head, from, min(from + each, more), sum);
-        __syncthreads();                                   // the last sums have been read
-        if (wave > 0) {
+        const Part p = part_of(g, (int)(v % strips) * 16 + (lane & 15));
+        const int each = (more + JOIN * 4 - 1) / (JOIN * 4), from = min((wave * 4 + (lane >> 4)) * each, more), to = min(from + each, more);
+        v4f sum = {0, 0, 0, 0};
+        if (p.mine) {
+            const float *const head = heads + p.u.col;
+            for (int i = from; i < to; i += U) {
+                v4f part[U];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) meet[wave - 1][k][lane] = sum[k];
+                for (int j = 0; j < U; ++j) {
+                    const float *const at = head + (int64_t)min(i + j, to - 1) * g.dim;
+                    part[j] = g.dim < 4 ? v4f{*at, 0, 0, 0} : *reinterpret_cast<const v4f_e *>(at);
+                }
+#pragma unroll
+                for (int j = 0; j < U; ++j) sum += i + j < to ? part[j] : v4f{0, 0, 0, 0};
+            }
         }
+        __syncthreads();                                   // the last sums have been read
+        meet[wave * 4 + (lane >> 4)][lane & 15] = sum;
         __syncthreads();
-        if (wave == 0) {
-            for (int o = 0; o < JOIN - 1; ++o)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) sum[k] += meet[o][k][lane];
-            put_joined<GT>(g, tile, row, p, sum);
+        if (wave == 0 && lane < 16) {
+            for (int o = 1; o < JOIN * 4; ++o) sum += meet[o][lane];
+            float s4[4] = {sum[0], sum[1], sum[2], sum[3]};
+            put_joined<GT>(g, tile, row, p, s4);
         }
     }
 }
@@ -744,8 +781,8 @@ Space carve_grad(void *base, int64_t n, int64_t dim)
 
 unsigned at_most(int64_t blocks, int64_t most) { return (unsigned)(blocks < most ? blocks : most); }
 
-// Rows without a token are cleared by the workgroups that sort, or, with up to NEAR tokens, by others of the first launch that read all tokens; more
-// tokens take these longer than the search in the sorted ones.
+// With up to NEAR tokens, rows without one are cleared beside the sort's first step, by workgroups that read all tokens; more tokens take these longer
+// than the search in the sorted ones.
 template <int T, int GT>
 hipError_t run(int n, int rows, int dim, const int *ids, int padding, float factor, const void *dY, int64_t ldy, void *dE, int64_t lde, int accumulate,
                const Space &w, hipStream_t s)
@@ -768,8 +805,9 @@ hipError_t run(int n, int rows, int dim, const int *ids, int padding, float fact
     if (n > 0 && n <= NEAR && rows <= RANGES * MOST_ROWS) {
         int bits = 1;
         while ((per - 1) >> bits) ++bits;
-        const auto sort = beside ? k_sort_ranges<GT, true> : k_sort_ranges<GT, false>;
-        PSK_LAUNCH(sort, dim3((rows + per - 1) / per), dim3(1024), 0, s, ids, n, padding, per, bits, w.keys[0], w.at[0], w.joins, c);
+        const int ranges = (rows + per - 1) / per;
+        PSK_LAUNCH((k_sort_ranges<GT>), dim3(ranges + (beside ? at_most(ranges, 256) : 0)), dim3(1024), 0, s, ids, n, padding, per, bits, ranges, w.keys[0], w.at[0], w.joins,
+                   c);
         keys = w.keys[0];
         at = w.at[0];
     } else {
@@ -795,11 +833,11 @@ hipError_t run(int n, int rows, int dim, const int *ids, int padding, float fact
         }
     }
     const Grad g = {n, rows, dim, accumulate, tile_of(n, dim), keys, at, dY, ldy, dE, lde, factor, w.head, w.tail, w.joins};
-    const int tiles = (n + g.tile - 1) / g.tile, j = quads_per_lane(dim), chunks = (dim + 256 * j - 1) / (256 * j), quads = (dim + 255) / 256, groups = (quads + JOIN - 1) / JOIN;
+    const int tiles = (n + g.tile - 1) / g.tile, j = quads_per_lane(dim), chunks = (dim + 256 * j - 1) / (256 * j), groups = (dim + 256 * JOIN - 1) / (256 * JOIN), strips = (dim + 63) / 64;
     const int64_t sums = (int64_t)tiles * chunks, all = (sums + 3) / 4 + (accumulate || beside ? 0 : ((int64_t)rows + 255) / 256);
     const auto sum = j == 1 ? k_grad_sum<T, GT, 1> : (j == 2 ? k_grad_sum<T, GT, 2> : k_grad_sum<T, GT, 3>);
     PSK_LAUNCH(sum, dim3(at_most(all, 65536)), dim3(256), 0, s, g, chunks, sums, all);
-    if (tiles > 1) PSK_LAUNCH((k_grad_join<GT>), dim3(at_most((int64_t)tiles * groups, 1024)), dim3(64 * JOIN), 0, s, g, tiles, groups, quads);
+    if (tiles > 1) PSK_LAUNCH((k_grad_join<GT>), dim3(at_most((int64_t)tiles * groups, 1024)), dim3(64 * JOIN), 0, s, g, tiles, groups, strips);
     return take_launch_status();
 }
 
