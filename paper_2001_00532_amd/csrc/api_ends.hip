@@ -36,9 +36,10 @@ int check_i8(const psk_i8 *A, int64_t most)
     return A->cols == 0 ? PSK_OK : check_codes(A->codes, A->ld, A->cols);
 }
 
-// Codes of tokens in a workspace: whole lines, zeros behind the columns.
+// Codes of tokens in a workspace: whole lines, zeros behind the columns; their scales; what psk_gemm_i8 has there.
 int64_t line(int64_t cols) { return (cols + 127) / 128 * 128; }
-size_t linear_bytes(int64_t cols, int64_t n) { return align256((size_t)n * (size_t)line(cols) + 1) + align256((size_t)n * 4 + 1); }
+size_t codes_bytes(int64_t cols, int64_t n) { return align256((size_t)n * (size_t)line(cols) + 1); }
+size_t scales_bytes(int64_t n) { return align256((size_t)n * 4 + 1); }
 
 }  // namespace
 
@@ -61,7 +62,7 @@ int psk_quant_i8(int64_t n, int64_t cols, int type, const void *X, int64_t ldx, 
 size_t psk_gemm_i8_workspace_bytes(int64_t rows, int64_t cols, int64_t n)
 {
     if (rows < 0 || rows > kMaxEdge || cols < 0 || cols > PSK_I8_MAX_COLS || n < 0 || n > PSK_MAX_VECTORS) return 0;
-    return 256;
+    return align256(gemm_i8_workspace_bytes((int)rows, (int)cols, (int)n) + 1);
 }
 
 int psk_gemm_i8(const psk_i8 *A, int64_t n, const int8_t *X, int64_t ldx, const float *scales, const float *bias, int type, void *Y, int64_t ldy,
@@ -82,13 +83,14 @@ int psk_gemm_i8(const psk_i8 *A, int64_t n, const int8_t *X, int64_t ldx, const 
     if (gemv_i8_takes((int)A->cols, (int)n))
         return hip_status(launch_gemv_i8((int)A->rows, (int)A->cols, (int)n, A->codes, A->ld, A->scales, X, ldx, scales, bias, type, Y, ldy,
                                          static_cast<hipStream_t>(stream)));
-    return hip_status(launch_gemm_i8((int)A->rows, (int)A->cols, (int)n, A->codes, A->ld, A->scales, X, ldx, scales, bias, type, Y, ldy, static_cast<hipStream_t>(stream)));
+    return hip_status(launch_gemm_i8((int)A->rows, (int)A->cols, (int)n, A->codes, A->ld, A->scales, X, ldx, scales, bias, type, Y, ldy, workspace,
+                                     static_cast<hipStream_t>(stream)));
 }
 
 size_t psk_linear_i8_workspace_bytes(int64_t rows, int64_t cols, int64_t n, int type)
 {
-    if (!type_ok(type) || psk_gemm_i8_workspace_bytes(rows, cols, n) == 0) return 0;
-    return linear_bytes(cols, n);
+    const size_t sums = psk_gemm_i8_workspace_bytes(rows, cols, n);
+    return !type_ok(type) || sums == 0 ? 0 : codes_bytes(cols, n) + scales_bytes(n) + sums;
 }
 
 int psk_linear_i8(const psk_i8 *A, int64_t n, int type, const void *X, int64_t ldx, const float *bias, void *Y, int64_t ldy, void *workspace,
@@ -107,10 +109,11 @@ int psk_linear_i8(const psk_i8 *A, int64_t n, int type, const void *X, int64_t l
         return hip_status(launch_gemv_i8((int)A->rows, (int)A->cols, (int)n, A->codes, A->ld, A->scales, X, ldx, nullptr, bias, type, Y, ldy, s));
     const int64_t ld = line(A->cols);
     int8_t *const codes = static_cast<int8_t *>(workspace);
-    float *const scales = reinterpret_cast<float *>(codes + align256((size_t)n * (size_t)ld + 1));
+    float *const scales = reinterpret_cast<float *>(codes + codes_bytes(A->cols, n));
+    void *const sums = reinterpret_cast<char *>(scales) + scales_bytes(n);
     const hipError_t e = launch_quant_i8((int)n, (int)A->cols, (int)ld, type, X, ldx, codes, ld, scales, s);
     if (e != hipSuccess) return PSK_ERR_HIP;
-    return hip_status(launch_gemm_i8((int)A->rows, (int)A->cols, (int)n, A->codes, A->ld, A->scales, codes, ld, scales, bias, type, Y, ldy, s));
+    return hip_status(launch_gemm_i8((int)A->rows, (int)A->cols, (int)n, A->codes, A->ld, A->scales, codes, ld, scales, bias, type, Y, ldy, sums, s));
 }
 
 int psk_embed(int64_t n, int64_t rows, int64_t dim, const int32_t *ids, float factor, int type, const void *E, int64_t lde, int ytype, void *Y,

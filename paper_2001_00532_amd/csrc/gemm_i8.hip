@@ -32,16 +32,24 @@ __device__ __forceinline__ void step_barrier()
 // then have a place of their own among the 256 bytes of all banks.
 __device__ __forceinline__ int turn(int row) { return row & 7; }
 
-// BT tokens x BR channels by WT x WR waves, S stages.
+// BT tokens x BR channels by WT x WR waves, S stages.  YT = SUMS: workgroup z has the columns from z * part on, and its sums go to Y as they are, n rows of `ldy`
+// (a multiple of 4).
+constexpr int SUMS = -1;
 template <int YT, int BT, int BR, int WT, int WR, int S>
 __global__ __launch_bounds__(64 * WT * WR) void k_gemm_i8(int rows, int cols, int n, const int8_t *A, int64_t lda, const int8_t *X, int64_t ldx, Finish f, void *Y,
-                                                          int64_t ldy, unsigned tiles_r, unsigned tiles)
+                                                          int64_t ldy, unsigned tiles_r, unsigned tiles, int part_cols)
 {
     constexpr int NW = WT * WR, LOADS = (BT + BR) / 8 / NW, TT = BT / WT / M, TR = BR / WR / M, STAGE = (BT + BR) * STEP, READS = TT + TR;
     static_assert((BT + BR) % (8 * NW) == 0, "whole loads");
     __shared__ __attribute__((aligned(1024))) int8_t lds[S * STAGE];
     const unsigned tile = blockIdx.y * gridDim.x + blockIdx.x;
     if (tile >= tiles) return;
+    if constexpr (YT == SUMS) {
+        const int first = blockIdx.z * part_cols;
+        X += first;
+        A += first;
+        cols = min(cols - first, part_cols);
+    }
     const int t0 = (int)(tile / tiles_r) * BT, r0 = (int)(tile % tiles_r) * BR;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wt = wave / WR, wr = wave % WR;
     const int blocks = (cols + STEP - 1) / STEP, left = cols - (blocks - 1) * STEP, most = ((left + 15) & ~15) - 16;      // the last piece of the last step
@@ -138,70 +146,99 @@ __global__ __launch_bounds__(64 * WT * WR) void k_gemm_i8(int rows, int cols, in
         multiply(o[1], [](int) {});
     }
 
-    // A lane has four channels of a token, 4 (lane / 16) + 0 .. 3 of every 16.  They change places in LDS, 16 tokens of the wave at a time, and leave in
-    // pieces of 16 bytes, a token's one after the other.  (Stored as they are, and with the tokens' scales loaded one by one, they took 22 us for a tile.)
-    constexpr int ES = YT == F32 ? 4 : 2, EACH = 16 / ES, PIECES = TR * M / EACH, PITCH = PIECES * 16 + 16;
-    static_assert(NW * M * PITCH <= S * STAGE, "room in LDS");
-    const int row0 = r0 + wr * TR * M;
-    float a[TR][4], b[TR][4], s[TT];
+    if constexpr (YT == SUMS) {
+        v4i *const to = static_cast<v4i *>(Y) + blockIdx.z * (n * ldy >> 2);
 #pragma unroll
-    for (int t = 0; t < TT; ++t) s[t] = f.s[min(t0 + (wt * TT + t) * M + in, n - 1)];
+        for (int t = 0; t < TT; ++t)
 #pragma unroll
-    for (int r = 0; r < TR; ++r)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) a[r][i] = f.a[min(row0 + r * M + 4 * part + i, rows - 1)];
-    if (f.bias) {
-#pragma unroll
-        for (int r = 0; r < TR; ++r)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) b[r][i] = f.bias[min(row0 + r * M + 4 * part + i, rows - 1)];
+            for (int r = 0; r < TR; ++r) {
+                const int token = t0 + (wt * TT + t) * M + in, row = r0 + (wr * TR + r) * M + 4 * part;
+                if (token < n && row < rows) to[(token * ldy + row) >> 2] = acc[r][t];
+            }
     } else {
+        // A lane has four channels of a token, 4 (lane / 16) + 0 .. 3 of every 16.  They change places in LDS, 16 tokens of the wave at a time, and leave in
+        // pieces of 16 bytes, a token's one after the other.  (Stored as they are, and with the tokens' scales loaded one by one, they took 22 us for a tile.)
+        constexpr int ES = YT == F32 ? 4 : 2, EACH = 16 / ES, PIECES = TR * M / EACH, PITCH = PIECES * 16 + 16;
+        static_assert(NW * M * PITCH <= S * STAGE, "room in LDS");
+        const int row0 = r0 + wr * TR * M;
+        float a[TR][4], b[TR][4], s[TT];
+#pragma unroll
+        for (int t = 0; t < TT; ++t) s[t] = f.s[min(t0 + (wt * TT + t) * M + in, n - 1)];
 #pragma unroll
         for (int r = 0; r < TR; ++r)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) b[r][i] = 0.0f;
-    }
-    step_barrier<0>();                                     // the last step has been read
-    int8_t *const room = lds + wave * M * PITCH;
+            for (int i = 0; i < 4; ++i) a[r][i] = f.a[min(row0 + r * M + 4 * part + i, rows - 1)];
+        if (f.bias) {
 #pragma unroll
-    for (int t = 0; t < TT; ++t) {
+            for (int r = 0; r < TR; ++r)
 #pragma unroll
-        for (int r = 0; r < TR; ++r) {
-            float v[4];
+                for (int i = 0; i < 4; ++i) b[r][i] = f.bias[min(row0 + r * M + 4 * part + i, rows - 1)];
+        } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = finish(acc[r][t][i], a[r][i], s[t], b[r][i]);
-            int8_t *const at = room + in * PITCH + (r * M + 4 * part) * ES;
-            if constexpr (YT == F32) *reinterpret_cast<v4f *>(at) = v4f{v[0], v[1], v[2], v[3]};
-            else *reinterpret_cast<v4s *>(at) = v4s{narrow<YT>(v[0]), narrow<YT>(v[1]), narrow<YT>(v[2]), narrow<YT>(v[3])};
+            for (int r = 0; r < TR; ++r)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) b[r][i] = 0.0f;
         }
-        wave_fence();
+        step_barrier<0>();                                     // the last step has been read
+        int8_t *const room = lds + wave * M * PITCH;
 #pragma unroll
-        for (int i = 0; i < M * PIECES; i += 64) {
-            const int at = i + lane, token = t0 + (wt * TT + t) * M + at / PIECES, row = row0 + at % PIECES * EACH;
-            if (M * PIECES % 64 && at >= M * PIECES) continue;
-            const int8_t *const from = room + at / PIECES * PITCH + at % PIECES * 16;
-            const v4u v = *reinterpret_cast<const v4u *>(from);
-            if (token >= n || row >= rows) continue;
-            char *const to = static_cast<char *>(Y) + (token * ldy + row) * ES;
-            if (row + EACH <= rows) {
-                if constexpr (YT == F32) *reinterpret_cast<v4f_e *>(to) = __builtin_bit_cast(v4f, v);
-                else *reinterpret_cast<v4u_u *>(to) = v;
-            } else {
-                for (int e = 0; row + e < rows; ++e) {
-                    if constexpr (YT == F32) reinterpret_cast<float *>(to)[e] = reinterpret_cast<const float *>(from)[e];
-                    else reinterpret_cast<unsigned short *>(to)[e] = reinterpret_cast<const unsigned short *>(from)[e];
+        for (int t = 0; t < TT; ++t) {
+#pragma unroll
+            for (int r = 0; r < TR; ++r) {
+                float v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = finish(acc[r][t][i], a[r][i], s[t], b[r][i]);
+                int8_t *const at = room + in * PITCH + (r * M + 4 * part) * ES;
+                if constexpr (YT == F32) *reinterpret_cast<v4f *>(at) = v4f{v[0], v[1], v[2], v[3]};
+                else *reinterpret_cast<v4s *>(at) = v4s{narrow<YT>(v[0]), narrow<YT>(v[1]), narrow<YT>(v[2]), narrow<YT>(v[3])};
+            }
+            wave_fence();
+#pragma unroll
+            for (int i = 0; i < M * PIECES; i += 64) {
+                const int at = i + lane, token = t0 + (wt * TT + t) * M + at / PIECES, row = row0 + at % PIECES * EACH;
+                if (M * PIECES % 64 && at >= M * PIECES) continue;
+                const int8_t *const from = room + at / PIECES * PITCH + at % PIECES * 16;
+                const v4u v = *reinterpret_cast<const v4u *>(from);
+                if (token >= n || row >= rows) continue;
+                char *const to = static_cast<char *>(Y) + (token * ldy + row) * ES;
+                if (row + EACH <= rows) {
+                    if constexpr (YT == F32) *reinterpret_cast<v4f_e *>(to) = __builtin_bit_cast(v4f, v);
+                    else *reinterpret_cast<v4u_u *>(to) = v;
+                } else {
+                    for (int e = 0; row + e < rows; ++e) {
+                        if constexpr (YT == F32) reinterpret_cast<float *>(to)[e] = reinterpret_cast<const float *>(from)[e];
+                        else reinterpret_cast<unsigned short *>(to)[e] = reinterpret_cast<const unsigned short *>(from)[e];
+                    }
                 }
             }
+            wave_fence();
         }
-        wave_fence();
+    }
+}
+
+// The sums of all parts of the columns, and what becomes of them; a thread takes four channels of a token.
+template <int YT>
+__global__ __launch_bounds__(256) void k_gemm_i8_join(int rows, int n, int parts, const v4i *__restrict__ sums, int64_t pitch, Finish f, void *Y, int64_t ldy)
+{
+    const int64_t quads = pitch >> 2, all = n * quads;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int token = (int)(i / quads), row = (int)(i % quads) * 4;
+        v4i sum = sums[i];
+        for (int p = 1; p < parts; ++p) sum += sums[p * all + i];
+        const float s = f.s[token];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (row + e < rows) store_as<YT>(Y, token * ldy + row + e, finish(sum[e], f.a[row + e], s, f.bias ? f.bias[row + e] : 0.0f));
     }
 }
 
 template <int YT, int BT, int BR, int WT, int WR, int S>
-void tiles(int rows, int cols, int n, const int8_t *A, int64_t lda, const int8_t *X, int64_t ldx, const Finish &f, void *Y, int64_t ldy, hipStream_t s)
+void tiles(int rows, int cols, int n, const int8_t *A, int64_t lda, const int8_t *X, int64_t ldx, const Finish &f, void *Y, int64_t ldy, int parts, int part_cols,
+           hipStream_t s)
 {
     const unsigned r = (unsigned)((rows + BR - 1) / BR), all = r * (unsigned)((n + BT - 1) / BT), x = all < 65536 ? all : 65536;
-    PSK_LAUNCH((k_gemm_i8<YT, BT, BR, WT, WR, S>), dim3(x, (all + x - 1) / x), dim3(64 * WT * WR), 0, s, rows, cols, n, A, lda, X, ldx, f, Y, ldy, r, all);
+    PSK_LAUNCH((k_gemm_i8<YT, BT, BR, WT, WR, S>), dim3(x, (all + x - 1) / x, parts), dim3(64 * WT * WR), 0, s, rows, cols, n, A, lda, X, ldx, f, Y, ldy, r, all,
+               part_cols);
 }
 
 // Tiles by their tokens and channels, and how long a step of 128 columns of one takes, in 10 ns: of the first 256 tiles (a compute unit has one), and
@@ -212,34 +249,75 @@ constexpr Shape SHAPES[] = {{16, 16, 19, 6}, {16, 32, 19, 9}, {32, 32, 22, 11}, 
                             {256, 128, 78, 80}, {256, 256, 118, 118}};
 constexpr int SHAPE_COUNT = sizeof(SHAPES) / sizeof(SHAPES[0]);
 
+// Few tiles of many columns: the columns in 2 to 16 parts, whose sums another launch adds up.  That takes 4.5 us and writing and reading the sums at 4 TB/s; they
+// have SUM_ROOM at most.  300 channels, 16384 columns, 7 tokens, quantised on the way: 18.7 us, 33 in one part; 1024 x 8192 with 64 tokens 11.0 and 14.3.  (With 3 us
+// instead, 4096 x 4096 and 5 tokens went in two parts and took 11.6 us for 9.1.)
+constexpr int MOST_PARTS = 16;
+constexpr int64_t SUM_ROOM = 16 << 20;
+struct Choice { int shape, parts, part_cols; };
+int64_t pitch_of(int rows) { return ((int64_t)rows + 3) / 4 * 4; }
+Choice choose(int rows, int cols, int n)
+{
+    const int steps = (cols + STEP - 1) / STEP;
+    Choice best = {0, 1, cols};
+    int64_t least = INT64_MAX;
+    for (int parts = 1; parts <= MOST_PARTS; parts *= 2) {
+        const int64_t bytes = parts * (int64_t)n * pitch_of(rows) * 4;
+        const int each = (steps + parts - 1) / parts;
+        if (parts > 1 && (bytes > SUM_ROOM || (int64_t)each * (parts - 1) >= steps)) break;
+        const int64_t join = parts > 1 ? 4500 + bytes * 2 / 4000 : 0;            // ns
+        for (int i = 0; i < SHAPE_COUNT; ++i) {
+            const int64_t all = (int64_t)((n + SHAPES[i].tokens - 1) / SHAPES[i].tokens) * ((rows + SHAPES[i].channels - 1) / SHAPES[i].channels) * parts;
+            const int64_t cost = join + (SHAPES[i].first + (all - 1) / 256 * SHAPES[i].more) * 10 * (each > 0 ? each : 1);
+            if (cost < least) {
+                least = cost;
+                best = {i, parts, each * STEP};
+            }
+        }
+    }
+    return best;
+}
+
 template <int YT>
-hipError_t launch(int rows, int cols, int n, const int8_t *A, int64_t lda, const int8_t *X, int64_t ldx, const Finish &f, void *Y, int64_t ldy, hipStream_t s)
+void launch_shape(int shape, int rows, int cols, int n, const int8_t *A, int64_t lda, const int8_t *X, int64_t ldx, const Finish &f, void *Y, int64_t ldy, int parts,
+                  int part_cols, hipStream_t s)
 {
     decltype(&tiles<YT, 16, 16, 1, 1, 8>) const go[SHAPE_COUNT] = {
         tiles<YT, 16, 16, 1, 1, 8>, tiles<YT, 16, 32, 1, 2, 8>, tiles<YT, 32, 32, 2, 2, 6>, tiles<YT, 32, 64, 1, 4, 4>, tiles<YT, 64, 32, 4, 1, 4>,
         tiles<YT, 64, 64, 2, 2, 4>, tiles<YT, 128, 64, 4, 2, 4>, tiles<YT, 128, 128, 2, 4, 4>, tiles<YT, 256, 128, 4, 2, 3>, tiles<YT, 256, 256, 2, 4, 2>};
-    int best = 0;
-    int64_t least = INT64_MAX;
-    for (int i = 0; i < SHAPE_COUNT; ++i) {
-        const int64_t all = (int64_t)((n + SHAPES[i].tokens - 1) / SHAPES[i].tokens) * ((rows + SHAPES[i].channels - 1) / SHAPES[i].channels);
-        const int64_t cost = SHAPES[i].first + (all - 1) / 256 * SHAPES[i].more;
-        if (cost < least) {
-            least = cost;
-            best = i;
-        }
+    go[shape](rows, cols, n, A, lda, X, ldx, f, Y, ldy, parts, part_cols, s);
+}
+
+template <int YT>
+hipError_t launch(int rows, int cols, int n, const int8_t *A, int64_t lda, const int8_t *X, int64_t ldx, const Finish &f, void *Y, int64_t ldy, void *sums, hipStream_t s)
+{
+    const Choice c = choose(rows, cols, n);
+    if (c.parts == 1) {
+        launch_shape<YT>(c.shape, rows, cols, n, A, lda, X, ldx, f, Y, ldy, 1, cols, s);
+    } else {
+        const int64_t pitch = pitch_of(rows), blocks = (n * pitch / 4 + 255) / 256;
+        launch_shape<SUMS>(c.shape, rows, cols, n, A, lda, X, ldx, f, sums, pitch, c.parts, c.part_cols, s);
+        PSK_LAUNCH((k_gemm_i8_join<YT>), dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, s, rows, n, c.parts, static_cast<const v4i *>(sums), pitch, f, Y,
+                   ldy);
     }
-    go[best](rows, cols, n, A, lda, X, ldx, f, Y, ldy, s);
     return take_launch_status();
 }
 
 }  // namespace
 
+// Room for the sums of parts of the columns: that for n tokens is enough for fewer.
+size_t gemm_i8_workspace_bytes(int rows, int cols, int n)
+{
+    const int64_t most = MOST_PARTS * (int64_t)n * pitch_of(rows) * 4;
+    return cols <= STEP ? 0 : (size_t)(most < SUM_ROOM ? most : SUM_ROOM);
+}
+
 hipError_t launch_gemm_i8(int rows, int cols, int n, const int8_t *A, int64_t lda, const float *a, const int8_t *X, int64_t ldx, const float *xs, const float *bias,
-                          int type, void *Y, int64_t ldy, hipStream_t s)
+                          int type, void *Y, int64_t ldy, void *sums, hipStream_t s)
 {
     const Finish f = {a, xs, bias};
     const auto go = type == F32 ? launch<F32> : (type == F16 ? launch<F16> : launch<BF16>);
-    return go(rows, cols, n, A, lda, X, ldx, f, Y, ldy, s);
+    return go(rows, cols, n, A, lda, X, ldx, f, Y, ldy, sums, s);
 }
 
 }  // namespace psk

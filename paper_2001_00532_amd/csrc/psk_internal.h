@@ -319,8 +319,9 @@ hipError_t launch_moe_q4_of(const MoeCall &c, int scale_type, const WeightsQ4 &w
 
 // Products of 8-bit integers (gemm_i8.h) and the embedding (embed.h).  A table of psk_i8 has the type 3 and its scales.
 hipError_t launch_quant_i8(int n, int cols, int fill, int type, const void *X, int64_t ldx, int8_t *codes, int64_t ldc, float *scales, hipStream_t s);
+size_t gemm_i8_workspace_bytes(int rows, int cols, int n);
 hipError_t launch_gemm_i8(int rows, int cols, int n, const int8_t *A, int64_t lda, const float *a, const int8_t *X, int64_t ldx, const float *xs,
-                          const float *bias, int type, void *Y, int64_t ldy, hipStream_t s);
+                          const float *bias, int type, void *Y, int64_t ldy, void *sums, hipStream_t s);
 bool gemv_i8_takes(int cols, int n);
 hipError_t launch_gemv_i8(int rows, int cols, int n, const int8_t *A, int64_t lda, const float *a, const void *X, int64_t ldx, const float *xs,
                           const float *bias, int type, void *Y, int64_t ldy, hipStream_t s);

@@ -111,6 +111,22 @@ def test_embed_grad_refuses():
     assert psk.psk_embed_grad_workspace_bytes(-1, 4, 4) == 0 and psk.psk_embed_grad_workspace_bytes(4, 4, 2 ** 28) == 0
 
 
+def test_a_workspace_for_more_is_one_for_fewer():
+    for rows, cols in ((1, 1), (300, 16384), (5003, 2051), (32768, 8192)):
+        last = 0
+        for n in (0, 1, 3, 4, 5, 17, 64, 300, 1000, 5000, 1 << 17, 1 << 19):
+            b = psk.psk_gemm_i8_workspace_bytes(rows, cols, n)
+            assert b >= max(last, 256)
+            last = b
+            assert psk.psk_linear_i8_workspace_bytes(rows, cols, n, psk.PSK_F16) >= b + n * cols
+    for dim in (1, 3, 4, 64, 255, 257, 515, 1027, 4096, 9000):
+        last = 0
+        for n in list(range(0, 300)) + [2 ** k + d for k in range(9, 24) for d in (-1, 0, 1)] + [1 << 24]:
+            b = psk.psk_embed_grad_workspace_bytes(n, 50000, dim)
+            assert b >= last, (n, dim)
+            last = b
+
+
 def test_binding_refuses():
     codes, scales = torch.zeros(8, 32, dtype=torch.int8), torch.zeros(8)
     for args in ((codes.int(), scales, 32), (codes, scales.half(), 32), (codes, scales[:7], 32), (codes, scales, 33), (codes[0], scales, 32),

@@ -138,6 +138,28 @@ def test_gradient_of_many_tokens(n, rows):
     assert int((got != 0).any(1).sum()) <= used.numel()
 
 
+@pytest.mark.parametrize("n", [1023, 1024, 1025, 2048, 2049, 65535, 65536, 65537])
+def test_gradient_where_the_way_changes(n):
+    """One launch, ranges of rows, several workgroups that sort; padding that is a row among the others; tokens of the last rows."""
+    rng = np.random.default_rng(n)
+    for rows, dim in ((300, 20), (1000, 5)):
+        ids, dy = tokens(rng, n, rows, "head"), torch.from_numpy(rng.standard_normal((n, dim))).half()
+        ids[-1] = 2
+        for padding in (2, rows - 1):
+            ref, bound = R.embed_grad(ids, dy, rows, 1.0, padding, torch.float32)
+            R.check(gradient(ids, dy, rows, "f32", padding=padding), ref, bound, "%d tokens, padding %d" % (n, padding))
+
+
+def test_gradient_of_one_row_among_very_many():
+    """More than 524288 rows with few tokens and with many; one row's tokens over hundreds of tiles."""
+    for n, rows in ((700, 524288), (700, 524289), (3000, 524289), (1, 3_000_000)):
+        ids = torch.full((n,), rows - 1, dtype=torch.int32)
+        ids[n // 2:n // 2 + 1] = 0
+        dy = torch.ones(n, 4)
+        got = gradient(ids, dy, rows, "f32", pad=5)
+        assert bool((got[rows - 1] == n - 1).all()) and bool((got[0] == 1).all()) and float(got.sum()) == 4 * n
+
+
 def test_gradient_without_tokens_or_rows():
     dE = torch.full((7, 20), 77.0, device="cuda")
     none = ints([]).cuda()

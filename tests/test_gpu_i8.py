@@ -159,6 +159,38 @@ def test_largest_sums(n):
     assert torch.equal(Y.cpu(), ref.float())
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,cols,n", [(301, 16384, 7), (13, 16385, 5), (70, 9000, 300), (1, 33000, 9), (600, 5000, 40), (255, 131071, 6), (18, 2200, 17), (30, 4500, 1500)])
+def test_few_tiles_of_many_columns(dtype, rows, cols, n):
+    """The columns in parts: several counts of steps to a part, parts that end in the middle of a step, rows that are no multiple of four."""
+    test_products(dtype, rows, cols, n)
+
+
+@pytest.mark.parametrize("rows,cols,n", [(9, 63488, 1), (9, 63489, 1), (30, 31744, 2), (30, 31745, 2), (21, 15872, 4), (21, 15873, 3), (5, 8, 4), (5, 7, 3), (2100, 1030, 1),
+                                         (2040, 1024, 2), (2050, 700, 3), (9000, 24, 1)])
+def test_where_the_way_for_few_tokens_changes(rows, cols, n):
+    """The longest rows that it takes and the shortest, few and many rows, workgroups that take several tasks."""
+    for dtype in ("bf16", "f32"):
+        test_products(dtype, rows, cols, n)
+
+
+def test_a_workspace_for_more_tokens():
+    """One that is made for many is enough for fewer, and what it held before does not matter."""
+    rng = np.random.default_rng(12)
+    rows, cols = 200, 9000
+    w, a = codes_of(rng, rows, cols), torch.rand(rows) / cols
+    A = psk.I8(w.cuda(), a.cuda(), cols=cols)
+    x = activations(rng, 700, cols, "bf16")
+    ws = psk.psk_linear_i8_workspace(A, x.cuda())
+    for n in (700, 5, 90, 1, 300):
+        ws.fill_(0xa5)
+        Y = torch.empty(n, rows, dtype=torch.bfloat16, device="cuda")
+        psk.psk_linear_i8(A, x[:n].cuda(), Y, ws=ws)
+        q, s = R.quantised(x[:n])
+        ref, bound = R.product(q, w[:, :cols].long(), a, s, None, torch.bfloat16)
+        R.check(Y, ref, bound, "%d tokens" % n)
+
+
 def test_no_columns_no_rows_no_tokens():
     bias, a = torch.randn(5).cuda(), torch.ones(5).cuda()
     A = psk.I8(torch.zeros((5, 0), dtype=torch.int8, device="cuda"), a, cols=0)
