@@ -69,11 +69,19 @@ __device__ __forceinline__ unsigned pack4(const int *c)
     return (unsigned)(c[0] & 255) | (unsigned)(c[1] & 255) << 8 | (unsigned)(c[2] & 255) << 16 | (unsigned)c[3] << 24;
 }
 
+// Largest of a wave, for every lane; in registers (through LDS each of the six exchanges takes a hundred cycles).
+template <int CTRL>
+__device__ __forceinline__ unsigned dpp_max(unsigned v) { return max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true)); }
 __device__ __forceinline__ unsigned wave_max(unsigned v)
 {
-#pragma unroll
-    for (int d = 1; d < WAVE; d *= 2) v = max(v, (unsigned)__shfl_xor((int)v, d, WAVE));
-    return v;
+    v = dpp_max<0xB1>(v);                                  // neighbours, pairs, eights, sixteens
+    v = dpp_max<0x4E>(v);
+    v = dpp_max<0x141>(v);
+    v = dpp_max<0x140>(v);
+    auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max(a[0], a[1]);
+    auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return max(b[0], b[1]);
 }
 
 // The first `left` of 16 bytes.
@@ -90,6 +98,7 @@ __device__ __forceinline__ v4i first_bytes(v4i v, int left)
 // What becomes of a sum.
 struct Finish {
     const float *a, *s, *bias;                             // of channels, of tokens, of channels or NULL
+    bool aside;                                            // put_result
 };
 __device__ __forceinline__ float finish(int sum, float a, float s, float b) { return (float)sum * a * s + b; }
 

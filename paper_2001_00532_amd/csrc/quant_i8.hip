@@ -6,10 +6,11 @@ namespace psk {
 namespace {
 
 // Columns from `cols` up to `fill` (a multiple of 16) become zeros.
-template <int T>
+// KEPT: pieces of 2048 columns that stay.
+template <int T, int KEPT>
 __global__ __launch_bounds__(256) void k_quant(int n, int cols, int fill, const void *X, int64_t ldx, int8_t *codes, int64_t ldc, float *scales)
 {
-    constexpr int KEPT = 4, ES = T == F32 ? 4 : 2;
+    constexpr int ES = T == F32 ? 4 : 2;
     __shared__ unsigned part[4];
     for (int64_t t = blockIdx.x; t < n; t += gridDim.x) {
         const char *row = static_cast<const char *>(X) + t * ldx * ES;
@@ -79,7 +80,7 @@ void launch(int n, int cols, int fill, const void *X, int64_t ldx, int8_t *codes
     const int64_t blocks = cols < 8 ? ((int64_t)n + 255) / 256 : n;
     const dim3 grid((unsigned)(blocks < 65536 ? blocks : 65536)), block(256);
     if (cols < 8) PSK_LAUNCH((k_quant_short<T>), grid, block, 0, s, n, cols, fill, X, ldx, codes, ldc, scales);
-    else PSK_LAUNCH((k_quant<T>), grid, block, 0, s, n, cols, fill, X, ldx, codes, ldc, scales);
+    else PSK_LAUNCH((cols <= 2048 ? k_quant<T, 1> : (cols <= 4096 ? k_quant<T, 2> : k_quant<T, 4>)), grid, block, 0, s, n, cols, fill, X, ldx, codes, ldc, scales);
 }
 
 }  // namespace

@@ -60,18 +60,32 @@ __device__ __forceinline__ void widen_raw(const Raw8<T> &r, float (&v)[8])
         for (int i = 0; i < 8; ++i) v[i] = widen<T>(r.a[i]);
     }
 }
-template <int T>
-__device__ __forceinline__ void store8(typename Bits<T>::type *p, const float (&v)[8])
-{
-    if constexpr (T == F32) {
-        *reinterpret_cast<v4f_e *>(p) = v4f{v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<v4f_e *>(p + 4) = v4f{v[4], v[5], v[6], v[7]};
-    } else {
-        v8s r;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) r[i] = narrow<T>(v[i]);
-        *reinterpret_cast<v8s_u *>(p) = r;
+// A result, past the caches if it is one that leaves them anyway.  (The empty statements keep the compiler from making one store of the two, which then goes
+// to them.  A template over the type would lose the pointer's alignment.)
+#define PSK_PUT_RESULT(V) \
+    __device__ __forceinline__ void put_result(V *p, V v, bool aside) \
+    { \
+        if (aside) { \
+            asm volatile(""); \
+            __builtin_nontemporal_store(v, p); \
+            asm volatile(""); \
+        } else { \
+            *p = v; \
+        } \
     }
+PSK_PUT_RESULT(v4f_e)
+PSK_PUT_RESULT(v4u_u)
+PSK_PUT_RESULT(v4s_u)
+PSK_PUT_RESULT(v8s_u)
+#undef PSK_PUT_RESULT
+constexpr int64_t ASIDE = 32 << 20;                        // bytes of a result from which on it goes past them
+template <int T>                                           // 16 bits
+__device__ __forceinline__ void store_row(typename Bits<T>::type *p, const float (&v)[8], bool aside)
+{
+    v8s r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = narrow<T>(v[i]);
+    put_result(reinterpret_cast<v8s_u *>(p), r, aside);
 }
 
 // Four elements: of 32 bits a wave's load or store is then one piece of 1 KB, where eight to a lane would be two with gaps.
@@ -98,13 +112,11 @@ __device__ __forceinline__ void widen_raw(const Raw4<T> &r, float (&v)[4])
     }
 }
 template <int T>
-__device__ __forceinline__ void store_row(typename Bits<T>::type *p, const float (&v)[4])
+__device__ __forceinline__ void store_row(typename Bits<T>::type *p, const float (&v)[4], bool aside)
 {
-    if constexpr (T == F32) *reinterpret_cast<v4f_e *>(p) = v4f{v[0], v[1], v[2], v[3]};
-    else *reinterpret_cast<v4s_u *>(p) = v4s{narrow<T>(v[0]), narrow<T>(v[1]), narrow<T>(v[2]), narrow<T>(v[3])};
+    if constexpr (T == F32) put_result(reinterpret_cast<v4f_e *>(p), v4f{v[0], v[1], v[2], v[3]}, aside);
+    else put_result(reinterpret_cast<v4s_u *>(p), v4s{narrow<T>(v[0]), narrow<T>(v[1]), narrow<T>(v[2]), narrow<T>(v[3])}, aside);
 }
-template <int T>
-__device__ __forceinline__ void store_row(typename Bits<T>::type *p, const float (&v)[8]) { store8<T>(p, v); }
 template <int T, int W> struct RawOf { typedef Raw8<T> type; };
 template <int T> struct RawOf<T, 4> { typedef Raw4<T> type; };
 

@@ -82,6 +82,18 @@ def test_embed_past_32_bits():
     assert bool((E[rows - 1] == 3).all()) and bool((E[1] == 2 * 2048).all()) and bool((E[0] == 0).all()) and bool((E[2:rows - 1:61] == 0).all())
 
 
+@pytest.mark.parametrize("table,dtype", [("f32", "f32"), ("i8", "f32"), ("f16", "bf16")])
+def test_results_larger_than_the_caches(table, dtype):
+    """From 32 MB on they are stored past them: rows at odd places, a last piece that is the row's last; and the gradient."""
+    test_embed(dtype, table, 5999, 40, 3001)
+    if dtype == "f32":
+        rng = np.random.default_rng(1)
+        ids, dy = tokens(rng, 900, 4001, "zipf"), torch.from_numpy(rng.standard_normal((900, 2101))).to(TYPES["bf16" if table == "i8" else "f32"])
+        for m in (900, 60):
+            ref, bound = R.embed_grad(ids[:m], dy[:m], 4001, 1.0, -1, torch.float32)
+            R.check(gradient(ids[:m], dy[:m], 4001, "f32"), ref, bound, "large gradient")
+
+
 # ------------------------------------------------------------------ the gradient
 def gradient(ids, dy, rows, gtype, factor=1.0, padding=-1, old=None, pad=3):
     n, dim = dy.shape

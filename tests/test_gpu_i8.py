@@ -174,6 +174,12 @@ def test_where_the_way_for_few_tokens_changes(rows, cols, n):
         test_products(dtype, rows, cols, n)
 
 
+@pytest.mark.parametrize("dtype,n", [("f16", 3500), ("f32", 1751)])
+def test_results_larger_than_the_caches(dtype, n):
+    """From 32 MB on these are stored past them; rows of Y that begin at odd places."""
+    test_products(dtype, 5001, 40, n)
+
+
 def test_a_workspace_for_more_tokens():
     """One that is made for many is enough for fewer, and what it held before does not matter."""
     rng = np.random.default_rng(12)
