@@ -3,6 +3,8 @@
 // A wave reads four rows in pieces of 1 KB, four steps ahead, and multiplies them by the tokens' codes, which every workgroup makes for itself in LDS while
 // its first weights are on their way; the products of a lane are four to an instruction, and the sums of 64 lanes meet in registers.  The workgroups stay.
 // Few rows: the four waves of a workgroup share the columns of the same four rows (SPLIT).
+// One bf16 token: 32768 x 8192 in 43 us, 6.2 TB/s; 4096 x 4096 in 6.6 a call, one after the other, and 7.4 in a trace.
+// Four tokens of 4096 x 4096 take 13.0 us; five, quantised by a launch of their own and multiplied by tiles, 12.5.
 #include "gemm_i8.h"
 
 namespace psk {
@@ -35,7 +37,7 @@ __global__ __launch_bounds__(THREADS, 2) void k_gemv_i8(int rows, int cols, int 
                                                         int tasks)
 {
     constexpr int WAVES = THREADS / 64, KEPT = N == 4 ? 2 : 4;
-    extern __shared__ int8_t codes[];                      // N rows of whole pieces, zeros behind the columns
+    extern __shared__ __attribute__((aligned(16))) int8_t codes[];              // N rows of whole pieces, zeros behind the columns
     __shared__ unsigned most[N][WAVES];
     __shared__ int meet[WAVES][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -221,7 +223,9 @@ hipError_t launch(int rows, int cols, int n, const int8_t *A, int64_t lda, const
 {
     const int tasks = (rows + R - 1) / R, pieces = (cols + PIECE - 1) / PIECE;
     const unsigned lds = (unsigned)(N * pieces * PIECE);
-    if (tasks < 512 && pieces > 1)
+    // few and long rows (1024 x 8192: 8.0 us, 9.5 with a task to a wave; 2040 x 8192 10.2 and 9.6,
+    // 1024 x 2048 8.2 and 7.6; the other way round at 256 x 8192, 8.2 and 7.9, where a call is little else than its launch; 8 pieces are the only ones measured above 2)
+    if (tasks <= 256 && pieces >= 8)
         PSK_LAUNCH((k_gemv_i8<XT, YT, N, true>), dim3(tasks), dim3(THREADS), lds, s, rows, cols, n, A, lda, X, ldx, a, xs, bias, Y, ldy, tasks);
     else
         PSK_LAUNCH((k_gemv_i8<XT, YT, N, false>), dim3(tasks / 4 < 512 ? (tasks + 3) / 4 : 512), dim3(THREADS), lds, s, rows, cols, n, A, lda, X, ldx, a, xs, bias, Y,
