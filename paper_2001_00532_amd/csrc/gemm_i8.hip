@@ -5,7 +5,8 @@
 // lane asks for is turned by the row, so that reading the operands' order meets each bank once.  One barrier a step: behind it the step's operands are there and
 // the stage before is free.
 //
-// 8192 tokens x 16384 channels x 4096 columns: 486 us, 2.26 POP/s; zeros for data 388: it is the power that bounds it.  2048 x 8192 x 4096: 60 us.
+// 8192 tokens x 16384 channels x 4096 columns: 427 to 436 us a call, 2.5 to 2.6 POP/s; 449 to 452 in a trace.  Power bounds it: an earlier form took 486 us,
+// and with zeros for data 388.  2048 x 8192 x 4096: 55 us, a tile to a compute unit.
 #include "gemm_i8.h"
 
 namespace psk {
