@@ -223,8 +223,8 @@ hipError_t launch(int rows, int cols, int n, const int8_t *A, int64_t lda, const
 {
     const int tasks = (rows + R - 1) / R, pieces = (cols + PIECE - 1) / PIECE;
     const unsigned lds = (unsigned)(N * pieces * PIECE);
-    // few and long rows (1024 x 8192: 8.0 us, 9.5 with a task to a wave; 2040 x 8192 10.2 and 9.6,
-    // 1024 x 2048 8.2 and 7.6; the other way round at 256 x 8192, 8.2 and 7.9, where a call is little else than its launch; 8 pieces are the only ones measured above 2)
+    // Few and long rows, one bf16 token, us against a task to a wave: 1024 x 8192 8.1 to 8.3 and 9.0, 256 x 8192 7.7 and 8.7 to 9.1, 1024 x 16384 11.9 and 15.0.
+    // Of 4 and 6 pieces either is faster, by run (1024 x 4096 7.3 to 7.4 and 6.4 to 8.1; four tokens 10.7 to 11.0 and 11.2); 2040 x 8192 10.2 and 9.6.
     if (tasks <= 256 && pieces >= 8)
         PSK_LAUNCH((k_gemv_i8<XT, YT, N, true>), dim3(tasks), dim3(THREADS), lds, s, rows, cols, n, A, lda, X, ldx, a, xs, bias, Y, ldy, tasks);
     else

@@ -167,7 +167,7 @@ def test_few_tiles_of_many_columns(dtype, rows, cols, n):
 
 
 @pytest.mark.parametrize("rows,cols,n", [(9, 63488, 1), (9, 63489, 1), (30, 31744, 2), (30, 31745, 2), (21, 15872, 4), (21, 15873, 3), (5, 8, 4), (5, 7, 3), (2100, 1030, 1),
-                                         (2040, 1024, 2), (2050, 700, 3), (9000, 24, 1)])
+                                         (2040, 1024, 2), (2050, 700, 3), (9000, 24, 1), (1024, 7169, 1), (1025, 7169, 1), (1024, 7168, 2), (1021, 8200, 4), (3, 7169, 3)])
 def test_where_the_way_for_few_tokens_changes(rows, cols, n):
     """The longest rows that it takes and the shortest, few and many rows, workgroups that take several tasks."""
     for dtype in ("bf16", "f32"):
