@@ -8,6 +8,7 @@
 // 16384 x 4096 bf16 into 32768 rows of f32: 151 us, 4.4 TB/s (sort and clearing 91, sums 54, joins 8); other tiles, waves or rows in flight
 // change nothing.  40001 x 1027 f16 into 50001 rows, a third one token: 84 us (42, 30, 13).
 #include "embed.h"
+#include "embed_plan.h"
 #include <algorithm>
 
 namespace psk {
@@ -78,7 +79,7 @@ __device__ __forceinline__ void clear_unnamed(const Clear &c, const int *__restr
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const unsigned row = (unsigned)id[i] - (unsigned)first;
+                const unsigned row = place_from(id[i], (int)first);
                 if (row < (unsigned)count && id[i] != padding) atomicOr(&bits[row >> 5], 1u << (row & 31));
             }
         }
@@ -188,7 +189,7 @@ __global__ __launch_bounds__(1024) void k_sort_ranges(const int *__restrict__ id
     int before = 0;                                        // tokens of earlier rows
     unsigned long long active = 0;                         // rounds with tokens of this range
     static_assert(NEAR / 1024 <= 64, "a bit for each round");
-    auto mine = [&](int id, int at) { return at < n && (unsigned)(id - first) < (unsigned)count && id != padding; };
+    auto mine = [&](int id, int at) { return at < n && place_from(id, first) < (unsigned)count && id != padding; };
     // Few instructions for each token, most are of no concern here: what padding and the tokens that are read again behind the last one make of `before` is
     // taken off below.
     for (int r = 0; r < rounds; r += U) {
@@ -205,11 +206,12 @@ __global__ __launch_bounds__(1024) void k_sort_ranges(const int *__restrict__ id
         for (int i = 0; i < U; ++i) {
             if (r + i >= rounds) break;
             before += (unsigned)id[i] < (unsigned)first;
-            if (__ballot((unsigned)(id[i] - first) < (unsigned)count)) {         // counts only: nothing waits for LDS
+            const int place = (int)place_from(id[i], first);
+            if (__ballot((unsigned)place < (unsigned)count)) {                   // counts only: nothing waits for LDS
                 active |= 1ull << (r + i);
                 const bool is = mine(id[i], begin + 64 * (r + i) + lane);
-                const unsigned long long same = same_digit(id[i] - first, bits, is);
-                if (is && !(same & ((1ull << lane) - 1))) atomicAdd(&seen[wave][id[i] - first], __popcll(same));
+                const unsigned long long same = same_digit(place, bits, is);
+                if (is && !(same & ((1ull << lane) - 1))) atomicAdd(&seen[wave][place], __popcll(same));
             }
         }
     }
@@ -252,7 +254,7 @@ __global__ __launch_bounds__(1024) void k_sort_ranges(const int *__restrict__ id
         for (int i = 0; i < U; ++i) {
             const bool is = mine(id[i], at[i]);
             if (!__ballot(is)) continue;
-            const int to = place_in_wave(id[i] - first, bits, is, lane, seen[wave]);
+            const int to = place_in_wave((int)place_from(id[i], first), bits, is, lane, seen[wave]);
             if (is) {
                 keys_out[to] = id[i];
                 at_out[to] = at[i];
@@ -673,9 +675,10 @@ __global__ __launch_bounds__(1024) void k_grad_few(Grad g, const int *__restrict
     const int id = (int)threadIdx.x < g.n ? ids[threadIdx.x] : -1;
     for (int d = threadIdx.x; d < WAVES * MOST_ROWS; d += 1024) (&seen[0][0])[d] = 0;
     __syncthreads();
-    const bool mine = id >= first && id < first + count && id != padding;
+    const int place = (int)place_from(id, first);
+    const bool mine = (unsigned)place < (unsigned)count && id != padding;
     int rank = 0;
-    if (__ballot(mine)) rank = place_in_wave(id - first, bits, mine, lane, seen[wave]);
+    if (__ballot(mine)) rank = place_in_wave(place, bits, mine, lane, seen[wave]);
     __syncthreads();
     int own = 0;
     if (threadIdx.x < MOST_ROWS) {
@@ -704,7 +707,7 @@ __global__ __launch_bounds__(1024) void k_grad_few(Grad g, const int *__restrict
     __syncthreads();
     const int segments = part[0];
     if (mine) {
-        const int to = seen[wave][id - first] + rank;
+        const int to = seen[wave][place] + rank;
         key[to] = id;
         at[to] = threadIdx.x;
     }
