@@ -627,8 +627,9 @@ int psk_quant_i8(int64_t n, int64_t cols, int type, const void *X, int64_t ldx, 
 
 /*
  * Y[t][i] = (sum_j q[t][j] A[i][j]) * a_i * s_t + bias[i]: n tokens by one matrix, with codes q and a scale s_t per token; A and a_i are the codes
- * and scales of `A`, bias is float[rows] or NULL for none.  Sums are whole numbers and exact; the products with the scales are made in 32 bits
- * in the order written and rounded once to `type`, the type of Y.  cols = 0 gives the bias.
+ * and scales of `A`, bias is float[rows] or NULL for none.  Sums are whole numbers and exact.  Then the sum becomes a float (one above 2^24 is rounded to
+ * 24 bits, which takes more than 1024 columns), its product with a_i is rounded to 32 bits, and that times s_t plus bias[i] is one fused multiply-add,
+ * rounded to `type`, the type of Y.  So a token's results do not depend on the tokens beside it.  cols = 0 gives the bias (with finite scales).
  * psk_gemm_i8: the codes X (laid out as those of psk_i8, ldx a multiple of 16) and scales are given.
  * psk_linear_i8: X (n x cols, of `type`, as Y) is quantised in the call, as psk_quant_i8 does.
  * A workspace for n tokens is enough for fewer.

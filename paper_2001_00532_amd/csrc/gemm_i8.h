@@ -100,6 +100,13 @@ struct Finish {
     const float *a, *s, *bias;                             // of channels, of tokens, of channels or NULL
     bool aside;                                            // put_result
 };
-__device__ __forceinline__ float finish(int sum, float a, float s, float b) { return (float)sum * a * s + b; }
+// In every way of a product the same three roundings: of the sum to 24 bits, of its product with the channel's scale, of the fused multiply-add.  To f16 the last
+// one is made at once (v_fma_mix*_f16), to bf16 from 32 bits.  (With __builtin_fmaf the compiler puts some conversions to f16 in pairs, and these round to 32 bits
+// first: tokens of one tile were then rounded in two ways.)
+__device__ __forceinline__ float finish(int sum, float a, float s, float b)
+{
+#pragma clang fp contract(fast)
+    return (float)sum * a * s + b;
+}
 
 }  // namespace psk
