@@ -19,7 +19,7 @@ constexpr int M = 16;                                      // channels and token
 __device__ __forceinline__ void to_lds(const void *base, unsigned offset, const void *to)
 {
     const unsigned at = (unsigned)reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const void *)to);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(at), "v"(offset), "s"(base) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(at), "v"(offset), "s"(base) : "m0", "memory");
 }
 // All but the last N loads of this wave are there, its LDS reads are done, and so are those of the other waves.
 template <int N>
