@@ -25,7 +25,7 @@ MARSHAL_FOR = os.path.join(OBJDIR, "marshal_built_for")
 SOURCES = ["api.hip", "partition.hip", "spmv_csr.hip", "spmm.hip", "spmv_bcsr.hip", "mttkrp.hip", "spmv_csr_f64.hip", "spmv_csr_divide.hip", "spmv_bcsr_g.hip", "spmm_narrow.hip", "spmm_blocks.hip", "slab.hip", "api_slab.hip", "calibrate.hip",
            "gemm_q4_f32.hip", "gemm_q4_f16.hip", "gemm_q4_bf16.hip", "moe_route.hip", "moe.hip", "moe_q4_f16.hip", "moe_q4_bf16.hip",
            "api_serving.hip", "quant_i8.hip", "gemm_i8.hip", "gemv_i8.hip", "embed.hip", "embed_grad.hip", "api_ends.hip"]
-HEADERS = ["psk_dev.h", "psk_mfma.h", "gemm_q4.h", "moe.h", "moe_q4.h", "row8.h", "gemm_i8.h", "embed.h", "embed_plan.h", "psk_internal.h", os.path.join("..", "..", "include", "psk.h")]
+HEADERS = ["psk_dev.h", "psk_mfma.h", "gemm_q4.h", "moe.h", "moe_q4.h", "row8.h", "gemm_i8.h", "gemm_i8_plan.h", "embed.h", "embed_plan.h", "psk_internal.h", os.path.join("..", "..", "include", "psk.h")]
 
 FLAGS = [
     "-O3", "-std=c++17", "-fPIC", "--offload-arch=gfx950",
