@@ -246,9 +246,12 @@ template <int YT>
 void launch_shape(int shape, int rows, int cols, int n, const int8_t *A, int64_t lda, const int8_t *X, int64_t ldx, const Finish &f, void *Y, int64_t ldy, int parts,
                   int part_cols, hipStream_t s)
 {
-    decltype(&tiles<YT, 16, 16, 1, 1, 8>) const go[SHAPE_COUNT] = {
+    if constexpr (YT != SUMS) {
+        if (shape == SHAPE_COUNT - 1) return tiles<YT, 256, 256, 2, 4, 2>(rows, cols, n, A, lda, X, ldx, f, Y, ldy, parts, part_cols, s);
+    }
+    decltype(&tiles<YT, 16, 16, 1, 1, 8>) const go[SHAPE_COUNT - 1] = {
         tiles<YT, 16, 16, 1, 1, 8>, tiles<YT, 16, 32, 1, 2, 8>, tiles<YT, 32, 32, 2, 2, 6>, tiles<YT, 32, 64, 1, 4, 4>, tiles<YT, 64, 32, 4, 1, 4>,
-        tiles<YT, 64, 64, 2, 2, 4>, tiles<YT, 128, 64, 4, 2, 4>, tiles<YT, 128, 128, 2, 4, 4>, tiles<YT, 256, 128, 4, 2, 3>, tiles<YT, 256, 256, 2, 4, 2>};
+        tiles<YT, 64, 64, 2, 2, 4>, tiles<YT, 128, 64, 4, 2, 4>, tiles<YT, 128, 128, 2, 4, 4>, tiles<YT, 256, 128, 4, 2, 3>};
     go[shape](rows, cols, n, A, lda, X, ldx, f, Y, ldy, parts, part_cols, s);
 }
 

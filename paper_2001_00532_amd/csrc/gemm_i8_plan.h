@@ -31,7 +31,7 @@ inline Choice choose(int rows, int cols, int n)
         const int each = (steps + parts - 1) / parts;
         if (parts > 1 && (bytes > SUM_ROOM || (int64_t)each * (parts - 1) >= steps)) break;
         const int64_t join = parts > 1 ? 4500 + bytes * 2 / 4000 : 0;            // ns
-        for (int i = 0; i < SHAPE_COUNT; ++i) {
+        for (int i = 0; i < (parts > 1 ? SHAPE_COUNT - 1 : SHAPE_COUNT); ++i) {        // SUM_ROOM is 64 of the largest tiles: smaller ones are faster, and it has no form for parts
             const int64_t all = (int64_t)((n + SHAPES[i].tokens - 1) / SHAPES[i].tokens) * ((rows + SHAPES[i].channels - 1) / SHAPES[i].channels) * parts;
             const int64_t cost = join + (SHAPES[i].first + (all - 1) / 256 * SHAPES[i].more) * 10 * (each > 0 ? each : 1);
             if (cost < least) {
