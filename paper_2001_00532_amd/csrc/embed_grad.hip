@@ -9,14 +9,11 @@
 // change nothing.  40001 x 1027 f16 into 50001 rows, a third one token: 84 us (42, 30, 13).
 #include "embed.h"
 #include "embed_plan.h"
-#include <algorithm>
 
 namespace psk {
 namespace {
 
-constexpr int SORT = 2048;                                 // positions per workgroup where several sort
 constexpr int MAX_BITS = 9;                                // of a digit
-constexpr int BASES = 128;                                 // workgroups whose counts every one of them adds up by itself
 
 // Key of a position: its token, or `rows` for one that is in no row.
 __device__ __forceinline__ int key_of(const int *ids, int64_t t, int rows, int padding)
@@ -167,8 +164,6 @@ __device__ __forceinline__ int block_exclusive(int v, int *part)
 // clear (clear_unnamed): waiting and writing go together.
 // One launch.
 // 16000 tokens, 4000 rows: 17 us; by one workgroup that sorted them in LDS while the others cleared 35.
-constexpr int NEAR = 65536, RANGES = 1024, MOST_ROWS = 512;
-
 template <int GT>
 __global__ __launch_bounds__(1024) void k_sort_ranges(const int *__restrict__ ids, int n, int padding, int per, int bits, int ranges, int *__restrict__ keys_out,
                                                       int *__restrict__ at_out, int *__restrict__ joins, Clear c)
@@ -370,8 +365,6 @@ __global__ __launch_bounds__(256) void k_sort_place(const int *__restrict__ keys
 }
 
 // ------------------------------------------------------------------ sums
-constexpr int MAX_TILE = 64;                               // positions per tile, at most one to a lane
-
 struct Grad {
     int n, rows, dim, accumulate, tile;
     const int *keys, *at;
@@ -624,42 +617,11 @@ __global__ __launch_bounds__(64 * JOIN) void k_grad_join(Grad g, int tiles, int 
     }
 }
 
-// 256 J columns to a wave: a wave's work is about J + 1 for each position.
-int quads_per_lane(int64_t dim)
-{
-    int best = 1;
-    int64_t least = INT64_MAX;
-    for (int j = 1; j <= 3; ++j) {
-        const int64_t cost = (dim + 256 * j - 1) / (256 * j) * (j + 1);
-        if (cost < least) {
-            least = cost;
-            best = j;
-        }
-    }
-    return best;
-}
-// Positions to a tile: as many as leave 4096 waves, but 16 to 64 (up to FEW tokens 8): a row of many tokens has
-// as many parts to join.  16000 tokens of 512 columns, nine tenths of them one: tiles of 8 joined in 34 us and added up in 10, of 16 in 18 and 11 (256 columns to a workgroup that joins).
-constexpr int FEW = 2048;
-int tile_of(int64_t n, int64_t dim)
-{
-    const int64_t j = 256 * quads_per_lane(dim), chunks = (dim + j - 1) / j;
-    int tile = MAX_TILE;
-    while (tile > (n <= FEW ? 8 : 16) && n * chunks < (int64_t)tile * 4096) tile /= 2;
-    return tile;
-}
-// As many tiles as n or fewer tokens are cut into at most, so that a workspace for n is one for fewer.
-int64_t most_tiles(int64_t n, int64_t dim)
-{
-    const int64_t j = 256 * quads_per_lane(dim), chunks = (dim + j - 1) / j, few = std::max((std::min(n, (int64_t)FEW) + 7) / 8, std::min((n + 15) / 16, 8192 / std::max(chunks, (int64_t)1) + 1));
-    return std::max((n + MAX_TILE - 1) / MAX_TILE, few);
-}
-
 // ------------------------------------------------------------------ few tokens
 // Up to SMALL tokens of 4 MB in all: one launch.  A workgroup owns rows and `width` of the columns, finds its tokens and their order as k_sort_ranges does, adds them
 // up, a row to a wave (rows of more than LONG tokens: a sixteenth of them to a wave, whose sums meet in LDS), and clears the other rows.
 // 512 tokens of 1024 columns, 8192 rows, f32: 11.8 us; by three launches 22.
-constexpr int SMALL = 1024, LONG = 64;
+constexpr int LONG = 64;
 
 template <int T, int GT>
 __global__ __launch_bounds__(1024) void k_grad_few(Grad g, const int *__restrict__ ids, int padding, int per, int bits, int width)
@@ -800,7 +762,8 @@ hipError_t run(int n, int rows, int dim, const int *ids, int padding, float fact
     const bool aside = (int64_t)rows * dim * (GT == F32 ? 4 : 2) >= ASIDE;
     const bool beside = !accumulate && n > 0 && n <= NEAR;
     const int *keys = ids, *at = nullptr;
-    if (n > 0 && n <= SMALL && dim >= 4 && rows <= RANGES * MOST_ROWS && (int64_t)n * dim * (T == F32 ? 4 : 2) <= 4 << 20) {
+    const Way way = way_of(n, rows, dim, T == F32 ? 4 : 2);
+    if (way == ONE_LAUNCH) {
         // as many columns to a workgroup as leave about 512 of them
         const int quads = (dim + 255) / 256, split = quads < 4 ? quads : 4, width = (quads + split - 1) / split * 256, groups = (dim + width - 1) / width;
         int per = (rows * groups + 511) / 512, bits = 1;
@@ -812,7 +775,7 @@ hipError_t run(int n, int rows, int dim, const int *ids, int padding, float fact
     }
     int per = (rows + 255) / 256;
     if (per > MOST_ROWS) per = MOST_ROWS;
-    if (n > 0 && n <= NEAR && rows <= RANGES * MOST_ROWS) {
+    if (way == BY_RANGES) {
         int bits = 1;
         while ((per - 1) >> bits) ++bits;
         const int ranges = (rows + per - 1) / per;
@@ -830,7 +793,7 @@ hipError_t run(int n, int rows, int dim, const int *ids, int padding, float fact
             const unsigned clear = beside && pass == 0 ? at_most(((int64_t)rows + 3) / 4, 1024) : 0;
             if (pass == 0) PSK_LAUNCH((k_sort_count<true, GT>), dim3(blocks + clear), dim3(256), 0, s, keys, n, padding, shift, digit, blocks, w.count, w.joins, c);
             else PSK_LAUNCH((k_sort_count<false, GT>), dim3(blocks), dim3(256), 0, s, keys, n, padding, shift, digit, blocks, w.count, w.joins, c);
-            const bool scan = blocks > BASES;
+            const bool scan = way == BY_SCANNED_DIGITS;
             if (scan) {
                 const hipError_t e = launch_exclusive_scan(w.count, w.count, (int64_t)blocks << digit, w.scan, s);
                 if (e != hipSuccess) return e;
