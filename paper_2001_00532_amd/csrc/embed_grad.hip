@@ -1,12 +1,13 @@
 // The gradient of the embedding lookup (formulas: embed.h): the product by the transpose of S.
 //
-// Tokens are sorted (a stable sort by digits, so a row's positions ascend and its sum has one order), and the sorted positions are cut into equal
-// tiles, as the stored entries of any sparse operand here: a tile adds up the rows of dY of its positions and writes the rows of dE that
-// begin and end in it.  Of a row that spans tiles, each tile leaves its part in 32 bits, and a third step adds the parts in order.
+// Tokens are sorted (stably, so a row's positions ascend), and the sorted positions are cut into equal tiles, as the stored entries of any sparse
+// operand here: a tile adds up the rows of dY of its positions and writes the rows of dE that begin and end in it.  Of a row that spans tiles, each tile leaves
+// its part in 32 bits, and a third step adds the parts.  In which order a row is added up depends on the sizes and the tokens alone.
 // Rows that no token has are cleared beside the sort, or with many tokens beside the sums.  Bound by reading dY and writing dE.
 //
 // 16384 x 4096 bf16 into 32768 rows of f32: 151 us, 4.4 TB/s (sort and clearing 91, sums 54, joins 8); other tiles, waves or rows in flight
-// change nothing.  40001 x 1027 f16 into 50001 rows, a third one token: 84 us (42, 30, 13).
+// change nothing.  Added to dE: 16, 83 and 10.  40001 x 1027 f16 into 50001 rows, a third one token: 84 us (42, 30, 13); without that token 40, 30 and 8;
+// added to dE 34, 48 and 13.  131072 x 1024 bf16 into 32768 rows of f32: sort 40, sums and clearing 90, joins 10.
 #include "embed.h"
 #include "embed_plan.h"
 
@@ -163,6 +164,7 @@ __device__ __forceinline__ int block_exclusive(int v, int *part)
 // its rows.  It counts its own, wave by wave (a wave has a sixteenth of the tokens), and puts them in their places.  Beside these, up to 256 workgroups
 // clear (clear_unnamed): waiting and writing go together.
 // One launch.
+// Bound by every workgroup's reading of all tokens: 16384 into 32768 rows 16 us, 40001 into 50001 34, and 32 without a token that a third of them are.
 // 16000 tokens, 4000 rows: 17 us; by one workgroup that sorted them in LDS while the others cleared 35.
 template <int GT>
 __global__ __launch_bounds__(1024) void k_sort_ranges(const int *__restrict__ ids, int n, int padding, int per, int bits, int ranges, int *__restrict__ keys_out,
@@ -517,9 +519,9 @@ __global__ __launch_bounds__(256) void k_grad_sum(Grad g, int chunks, int64_t su
     }
 }
 
-// A row that begins in a tile and goes on behind it: its parts in order.  Few parts: a workgroup takes the tile and 2048 columns, a wave 256 of them.  Many:
-// the tile and 64 columns (with 256 columns to a workgroup, two of them took 34 us for 3.7 MB of parts, 54 GB/s each), a wave takes an eighth of the parts, four at a time, and
-// their sums meet in LDS.
+// A row that begins in a tile and goes on behind it: its parts.  Few: a workgroup takes the tile and 2048 columns, a wave 256 of them; the parts from the second on
+// in order, four loads in flight, and the first one last.  Many: the tile and 64 columns (with 256 columns to a workgroup, two of them took 34 us for 3.7 MB of parts,
+// 54 GB/s each), 16 lanes take a 32nd of the parts, eight loads in flight, and their sums meet in LDS.
 // (Without the lists, a workgroup to every tile and 256 columns took 25 us for 16384 tokens of 4096 columns, most to find nothing.)
 constexpr int JOIN = 8;                                    // waves
 struct Part {                                              // a lane's columns
@@ -620,7 +622,7 @@ __global__ __launch_bounds__(64 * JOIN) void k_grad_join(Grad g, int tiles, int 
 // ------------------------------------------------------------------ few tokens
 // Up to SMALL tokens of 4 MB in all: one launch.  A workgroup owns rows and `width` of the columns, finds its tokens and their order as k_sort_ranges does, adds them
 // up, a row to a wave (rows of more than LONG tokens: a sixteenth of them to a wave, whose sums meet in LDS), and clears the other rows.
-// 512 tokens of 1024 columns, 8192 rows, f32: 11.8 us; by three launches 22.
+// 512 tokens of 1024 columns, 8192 rows, f32: 11.8 us; by three launches 22.  In a trace 12.8, into 1024 rows 9.6, added to dE (nothing to clear) 10.2.
 constexpr int LONG = 64;
 
 template <int T, int GT>

@@ -1,7 +1,7 @@
 // Y = X A^T in 8-bit integers (formulas: gemm_i8.h).
 //
 // Tiles of tokens x channels, 128 columns a step.  Both operands go from memory to LDS without passing registers, a step or more ahead of its use; a wave's
-// load is 8 rows of 128 bytes (in whole lines: steps of 64 columns, with twice the stages, take 477 us where these take 424), and which 16 bytes of its row a
+// load is 8 rows of 128 bytes (in whole lines: steps of 64 columns, with twice the stages, took 477 us where these took 424, both with zeros for data), and which 16 bytes of its row a
 // lane asks for is turned by the row, so that reading the operands' order meets each bank once.  One barrier a step: behind it the step's operands are there and
 // the stage before is free.
 //
@@ -282,7 +282,7 @@ size_t gemm_i8_workspace_bytes(int rows, int cols, int n)
 hipError_t launch_gemm_i8(int rows, int cols, int n, const int8_t *A, int64_t lda, const float *a, const int8_t *X, int64_t ldx, const float *xs, const float *bias,
                           int type, void *Y, int64_t ldy, void *sums, hipStream_t s)
 {
-    // (8192 tokens x 16384 channels in bf16: 474 us for 489)
+    // (8192 tokens x 16384 channels in bf16: 426 to 431 us for 448 to 450)
     const Finish f = {a, xs, bias, (int64_t)n * rows * (type == F32 ? 4 : 2) >= ASIDE};
     const auto go = type == F32 ? launch<F32> : (type == F16 ? launch<F16> : launch<BF16>);
     return go(rows, cols, n, A, lda, X, ldx, f, Y, ldy, sums, s);

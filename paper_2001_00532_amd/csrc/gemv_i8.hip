@@ -3,8 +3,8 @@
 // A wave reads four rows in pieces of 1 KB, four steps ahead, and multiplies them by the tokens' codes, which every workgroup makes for itself in LDS while
 // its first weights are on their way; the products of a lane are four to an instruction, and the sums of 64 lanes meet in registers.  The workgroups stay.
 // Few rows: the four waves of a workgroup share the columns of the same four rows (SPLIT).
-// One bf16 token: 32768 x 8192 in 43 us, 6.2 TB/s; 4096 x 4096 in 6.6 a call, one after the other, and 7.4 in a trace.
-// Four tokens of 4096 x 4096 take 13.0 us; five, quantised by a launch of their own and multiplied by tiles, 12.5.
+// One bf16 token: 32768 x 8192 in 43 us, 6.2 TB/s; 4096 x 4096 in 6.6 a call, one after the other, and 7.3 in a trace
+// (3.8 of these with 128 columns, and 6.8 with codes given).
 #include "gemm_i8.h"
 
 namespace psk {
@@ -242,6 +242,18 @@ hipError_t launch_n(int rows, int cols, int n, const int8_t *A, int64_t lda, con
 
 }  // namespace
 
+// Up to four tokens, whether or not codes are given.  us in a replayed graph, here and by tiles (with activations behind a launch that quantises them):
+//   rows x cols       one token, bf16   two           four          four, codes given
+//   256 x 1024        4.1    6.2        5.4    6.3    7.0    6.3    3.9    3.6
+//   1024 x 8192       7.0   14.2       10.0   14.7   17.7   15.5    6.5   11.0
+//   2048 x 2048       5.1    8.3        6.4    8.5    8.2    8.5    5.0    5.8
+//   4096 x 4096       7.1   16.6        8.7   12.2   11.8   12.2    7.6    8.8
+//   10240 x 4096     11.1   16.2       12.3   16.2   16.2   16.2   12.6   12.7
+//   4096 x 16384     22.9   32.5       28.6   32.4   32.9   32.9   24.4   24.3
+//   8192 x 8192      14.9   28.6       17.5   28.9   27.0   26.4   17.1   21.8
+//   32768 x 8192     43.7   63.7       46.0   64.1   56.2   63.8   46.7   59.0
+// Three tokens take what four do, f32 activations what bf16 do.  Three and four of activations and few rows are slower here (by a seventh at most): every
+// workgroup makes all codes.
 bool gemv_i8_takes(int cols, int n)
 {
     return cols >= 8 && n <= 4 && (n == 3 ? 4 : n) * ((cols + PIECE - 1) / PIECE * PIECE) <= 65536 - 2048;      // two workgroups to a compute unit

@@ -1,5 +1,6 @@
 // Tokens in 8 bits (formulas: gemm_i8.h).  A workgroup per row; the first 8192 columns stay in registers between the two passes, later ones are read
-// again.  Bound by reading the rows: 2048 x 4096 bf16 in 7.7 us, 3.3 TB/s read and written; 32 rows 3.7, a launch and one trip to memory.
+// again.  Bound by reading the rows: 2048 x 4096 bf16 in 7.7 us, 3.3 TB/s read and written; 32 rows 3.7, a launch and one trip to memory;
+// 131072 x 4096 286 us, 5.6 TB/s.
 #include "gemm_i8.h"
 
 namespace psk {
