@@ -653,8 +653,8 @@ int psk_embed_i8(const psk_i8 *E, int64_t n, const int32_t *ids, float factor, i
 /*
  * Its gradient, the product by the transpose: dE[v][:] = factor * sum of dY[t][:] over the tokens t with ids[t] = v, for every row v of the table
  * (rows without a token become zeros); with `accumulate` this is added to dE instead, and rows without a token are not touched.  Tokens outside
- * [0, rows) and those equal to `padding` (-1: none) add nothing.  Sums in 32 bits, in an order that depends on the sizes and the tokens alone;
- * rounded once to gtype, which is PSK_F32 or `type`, the type of dY.  A workspace for n tokens is enough for fewer.
+ * [0, rows) and those equal to `padding` (-1: none) add nothing.  Sums in 32 bits, in an order that depends on the sizes, the type of dY and the tokens
+ * alone; rounded once to gtype, which is PSK_F32 or `type`, the type of dY.  A workspace for n tokens is enough for fewer.
  */
 size_t psk_embed_grad_workspace_bytes(int64_t n, int64_t rows, int64_t dim);
 int psk_embed_grad(int64_t n, int64_t rows, int64_t dim, const int32_t *ids, int32_t padding, float factor, int type, const void *dY, int64_t ldy,

@@ -1014,7 +1014,7 @@ def psk_embed_grad_workspace(dY, dE, stream=None):
 
 def psk_embed_grad(ids, dY, dE, factor=1.0, padding=-1, accumulate=False, ws=None, stream=None):
     """dE (rows x dim) = (dE if accumulate) + factor * the sums of the rows of dY (n x dim) whose tokens are the same, in an order that
-    depends on the sizes and the tokens alone.  Tokens outside the table, and those equal to `padding`, add nothing."""
+    depends on the sizes, the type of dY and the tokens alone.  Tokens outside the table, and those equal to `padding`, add nothing."""
     (n, dim), rows = dY.shape, dE.shape[0]
     type, gtype = _type(dY, "psk_embed_grad"), _type(dE, "psk_embed_grad")
     i = _vector(ids, n, torch.int32, "psk_embed_grad: ids")
